@@ -244,6 +244,92 @@ int32_t ss_tree_attention(const ss_attn_desc_t* desc /* host */, void* workspace
                           void* stream);
 
 /* =========================================================================================================
+ * ss_qk_norm_rope, ss_kv_append - head rows on their way from a projection into the attention.
+ *
+ * (Part of the serving substrate of Section "Experimental Setup"; the paper prints no formula.)  A row x of 128 values at
+ * position n, with weight w:
+ *   y = x * w / sqrt(mean(x^2) + eps)            without a weight: y = x
+ *   (y_a, y_b) -> (y_a cos f - y_b sin f, y_b cos f + y_a sin f),   f = n * inv_freq[i],  i < rot_dim / 2
+ *   with (a, b) = (i, i + rot_dim/2), or (2i, 2i + 1) with SS_ROWS_INTERLEAVED; values from rot_dim on are not rotated.
+ * fp32 arithmetic (the angle fp64), one rounding to bf16.
+ *
+ * ss_rows_t holds the rows of a step: bf16, row r of head h at r * row_stride + h * head_stride (strides in elements, multiples
+ * of 8; all addresses 16-byte aligned; so q, k and v may be parts of one projection's output, and a padded one).
+ *
+ * ss_qk_norm_rope writes q_out from q and / or k_out from k (either pair may be NULL) for rows 0 .. n_rows-1.  An output may be
+ * its input (same strides); any other overlap is undefined.
+ *
+ * ss_kv_append puts the keys (normalised, rotated) and the values (as they are) of a step where ss_tree_attention and
+ * ss_draft_attention with the same descriptor expect them - token t of path p with T tokens is token node_kv_len - T + t of its
+ * leaf node, whose length already counts the step - and writes q_out from q at the same positions (q NULL: no queries).  Row of a
+ * path's token t: q_src_offsets[p] + t where the descriptor has these, else q_offsets[p] + t, in q, k, v, q_out and positions.
+ * Position: `positions`, or, where that is NULL, the token's index in the path's whole sequence.
+ * Of the descriptor it reads the heads, the pool, the tree, and the paths (q, out, lse, hints and flags are not used).  Paths are
+ * unique and leaves private, as for the attention: two paths with the same leaf race.
+ * Left alone: pool slots of other tokens; rows of no path.  Not written: keys and values of tokens in front of the leaf's first
+ * (T > node_kv_len) or on a page outside the pool or the leaf's list; rows outside [0, n_rows); paths with a leaf outside the tree.
+ *
+ * No workspace, one launch.  n_rows = 0, no paths or no tokens: nothing is launched.
+ * Errors: SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED (head_dim != 128, rot_dim not a multiple of 16 up to 128, alignment, pool layout),
+ * SS_ERR_CUDA.
+ * ======================================================================================================= */
+#define SS_ROWS_INTERLEAVED 0x1u
+typedef struct ss_rows {
+  uint32_t struct_size;              /* = sizeof(ss_rows_t) */
+  uint32_t flags;                    /* 0 or SS_ROWS_INTERLEAVED */
+  int32_t num_q_heads, num_kv_heads;
+  int32_t head_dim, rot_dim;         /* 128; 0 (no rotation) .. 128 */
+  float eps;                         /* >= 0 */
+  int32_t reserved;
+  int64_t n_rows;                    /* rows of q, k, v, q_out, k_out and positions */
+  const float* inv_freq;             /* fp32 [rot_dim / 2]; not read if rot_dim == 0 */
+  const void* q_weight;              /* bf16 [128] or NULL: queries are not normalised */
+  const void* k_weight;
+  const int32_t* positions;          /* [n_rows]; ss_kv_append: may be NULL */
+  const void* q;
+  const void* k;
+  const void* v;                     /* ss_kv_append only */
+  void* q_out;                       /* NULL iff q is */
+  void* k_out;                       /* ss_qk_norm_rope: NULL iff k is; ss_kv_append: NULL */
+  int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int64_t q_out_row_stride, q_out_head_stride, k_out_row_stride, k_out_head_stride;
+} ss_rows_t;
+
+int32_t ss_qk_norm_rope(const ss_rows_t* rows /* host */, void* stream);
+int32_t ss_kv_append(const ss_attn_desc_t* desc /* host */, const ss_rows_t* rows /* host */, void* stream);
+
+/* =========================================================================================================
+ * ss_draft_attention - attention of trees of drafted tokens over the paged cache.
+ *
+ * (Speculative decoding on the substrate of Section "Experimental Setup"; the paper prints no formula.)  The descriptor is that
+ * of ss_tree_attention: path p has the KV sequence of its chain (length L), whose last T = path_q_len tokens are now DRAFTS that
+ * form a tree of their own: draft t continues draft draft_parent[row of t] < t of the same path, or, where that is -1, the cached
+ * text.  Query token t sees the L - T cached keys, the drafts on its way to the cached text, and itself:
+ *   s_j = sm_scale * <q[t,h,:], K[j,g,:]>,   j < L - T, or j = L - T + d with d = t or an ancestor of t  (j >= 0)
+ *   out[t,h,:] = sum_j softmax(s)_j V[j,g,:],   lse[t,h] = ln sum_j exp(s_j);   no visible key  =>  out = 0, lse = -inf
+ * Keys and values that a token does not see may hold anything, NaN and infinities included, without an effect on it.
+ *
+ *   draft_parent  int32, by row of q (q_src_offsets[p] + t or q_offsets[p] + t; host bound: q_src_rows or total_q), or NULL: every
+ *                 draft continues the one before it (the causal step of ss_tree_attention)
+ *   T             0 .. SS_MAX_DRAFT (0: the path is skipped, its rows - none - are not written)
+ *   nodes         any length anywhere on a chain; pool, strides, alignments, out and lse as for ss_tree_attention; max_sms is kept to
+ *   flags         as for ss_tree_attention: SS_FLAG_FORCE_GENERIC or SS_FLAG_NO_TCGEN05 run one row per warp on the CUDA cores (a
+ *                 second opinion), the others make no difference (index arrays are always checked)
+ *   workspace     >= ss_draft_attention_workspace_bytes(desc) bytes, 256-byte aligned; its size depends on the number of SMs of
+ *                 the current device, on num_paths and total_q (and q_src_rows).  Calls that share one must not overlap
+ *
+ * Accuracy contract: that of ss_tree_attention.  Results do not depend on the run (no atomics in sums).
+ * Rows of no path are left as they were.
+ * Errors (host): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE_TOO_SMALL, SS_ERR_CUDA.  Errors (device, via
+ * ss_last_device_status; what the path concerned leaves in its rows is unspecified): SS_ERR_UNSUPPORTED (T > SS_MAX_DRAFT, depth),
+ * SS_ERR_BAD_INPUT (a leaf, parent, page, row or length out of range), SS_ERR_TIMEOUT.
+ * ======================================================================================================= */
+#define SS_MAX_DRAFT 128             /* drafted tokens of one path */
+int32_t ss_draft_attention_workspace_bytes(const ss_attn_desc_t* desc /* host */, size_t* out_bytes /* host */);
+int32_t ss_draft_attention(const ss_attn_desc_t* desc /* host */, const int32_t* draft_parent, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* =========================================================================================================
  * ss_topk_prune - keep the k best-scored candidates of every problem.
  *
  * Paper: Section "Early Pruning of Search Tree" - a candidate whose score ranks below the top-k cannot be

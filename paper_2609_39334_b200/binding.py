@@ -31,6 +31,8 @@ SS_FLAG_WEAK_HASH = 0x8
 SS_FLAG_TILES_2CTA = 0x10
 SS_MAX_DEPTH = 16
 SS_STEP_COMPACT_TRANSFERS = 0x1
+SS_ROWS_INTERLEAVED = 0x1
+SS_MAX_DRAFT = 128
 SS_DEDUP_STATIC_MAX_PATHS = 65536
 
 EXPORTS = [
@@ -41,6 +43,7 @@ EXPORTS = [
     "ss_branch_sample", "ss_gather_unique_paths", "ss_candidate_step_host_arena_bytes", "ss_candidate_step_host",
     "ss_prefix_tree_workspace_bytes", "ss_build_prefix_tree", "ss_candidate_step",
     "ss_candidate_step_host_2", "ss_branch_sample_upto",
+    "ss_qk_norm_rope", "ss_kv_append", "ss_draft_attention_workspace_bytes", "ss_draft_attention",
 ]
 PHASES = ["plan", "tiles", "leaves", "generic", "merge"]
 
@@ -88,6 +91,7 @@ _SIGNATURES = {
     "ss_prefix_tree_workspace_bytes": "iqip", "ss_build_prefix_tree": "ppiqippppppppzp",
     "ss_candidate_step": "pp", "ss_candidate_step_host_arena_bytes": "pp", "ss_candidate_step_host": "ppzp", "ss_candidate_step_host_2": "ppzpp", "ss_profile_enable": "i",
     "ss_profile_read": "pp", "ss_debug_umma_tile": "pppiiipp", "ss_debug_bounded_wait": "pp",
+    "ss_qk_norm_rope": "pp", "ss_kv_append": "ppp", "ss_draft_attention_workspace_bytes": "pp", "ss_draft_attention": "pppzp",
 }
 
 
@@ -358,6 +362,85 @@ def ss_tree_attention(desc: ss_attn_desc_t, workspace: torch.Tensor, stream=None
                                  _stream(stream))
     if check:
         _check(rc, "ss_tree_attention")
+    return rc
+
+
+# ---------------------------------------------------------------------------------------------------------
+class ss_rows_t(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+        ("eps", ctypes.c_float), ("reserved", ctypes.c_int32), ("n_rows", ctypes.c_int64),
+    ] + [(n, ctypes.c_void_p) for n in ("inv_freq", "q_weight", "k_weight", "positions", "q", "k", "v", "q_out", "k_out")] + [
+        (f"{n}_{s}_stride", ctypes.c_int64) for n in ("q", "k", "v", "q_out", "k_out") for s in ("row", "head")]
+
+
+def make_rows(*, q=None, k=None, v=None, q_out=None, k_out=None, positions=None, inv_freq=None, rot_dim=None, interleaved=False,
+              q_weight=None, k_weight=None, eps=1e-6) -> ss_rows_t:
+    """Fills ss_rows_t for ss_qk_norm_rope / ss_kv_append.  q, k, v, q_out, k_out: bf16 [rows][heads][128] of any row and head
+    strides; `rot_dim` defaults to 2 * len(inv_freq).  The returned object keeps references to the tensors."""
+    r = ss_rows_t()
+    r.struct_size = ctypes.sizeof(ss_rows_t)
+    r.flags = SS_ROWS_INTERLEAVED if interleaved else 0
+    r.head_dim, r.eps = 128, float(eps)
+    r.rot_dim = (2 * inv_freq.numel() if inv_freq is not None else 0) if rot_dim is None else int(rot_dim)
+    rows, device = None, None
+    for name, t in (("q", q), ("k", k), ("v", v), ("q_out", q_out), ("k_out", k_out)):
+        if t is None:
+            continue
+        assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and t.shape[2] == 128 and t.stride(2) == 1, name
+        assert rows is None or (t.shape[0] == rows and t.device == device), name
+        rows, device = t.shape[0], t.device
+        if name in ("q", "q_out"):
+            assert r.num_q_heads in (0, t.shape[1]), name
+            r.num_q_heads = t.shape[1]
+        else:
+            assert r.num_kv_heads in (0, t.shape[1]), name
+            r.num_kv_heads = t.shape[1]
+        setattr(r, name, t.data_ptr())
+        setattr(r, name + "_row_stride", t.stride(0))
+        setattr(r, name + "_head_stride", t.stride(1))
+    r.n_rows = rows or 0
+    assert inv_freq is None or (inv_freq.dtype == torch.float32 and 2 * inv_freq.numel() >= r.rot_dim)
+    assert positions is None or (positions.dtype == torch.int32 and positions.numel() >= r.n_rows)
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.bfloat16 and w.numel() == 128)
+    r.inv_freq, r.positions, r.q_weight, r.k_weight = _ptr(inv_freq), _ptr(positions), _ptr(q_weight), _ptr(k_weight)
+    r._keep = (q, k, v, q_out, k_out, positions, inv_freq, q_weight, k_weight)
+    return r
+
+
+def ss_qk_norm_rope(rows: ss_rows_t, stream=None, check=True) -> int:
+    """Norms of queries and / or keys per head (where there are weights) and the rotation to their positions, in one pass."""
+    rc = lib().ss_qk_norm_rope(ctypes.byref(rows), _stream(stream))
+    if check:
+        _check(rc, "ss_qk_norm_rope")
+    return rc
+
+
+def ss_kv_append(desc: ss_attn_desc_t, rows: ss_rows_t, stream=None, check=True) -> int:
+    """Keys (normalised, rotated) and values of a step into the pool slots that the attention with `desc` reads them from, queries
+    (if given) into q_out."""
+    rc = lib().ss_kv_append(ctypes.byref(desc), ctypes.byref(rows), _stream(stream))
+    if check:
+        _check(rc, "ss_kv_append")
+    return rc
+
+
+def ss_draft_attention_workspace_bytes(desc: ss_attn_desc_t) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().ss_draft_attention_workspace_bytes(ctypes.byref(desc), ctypes.byref(out)), "ss_draft_attention_workspace_bytes")
+    return int(out.value)
+
+
+def ss_draft_attention(desc: ss_attn_desc_t, draft_parent: Optional[torch.Tensor], workspace: torch.Tensor, stream=None,
+                       check=True) -> int:
+    """ss_tree_attention's paths with a TREE of tokens (int32 parent by row, -1: the cached text) in place of the causal step."""
+    assert draft_parent is None or draft_parent.dtype == torch.int32
+    rc = lib().ss_draft_attention(ctypes.byref(desc), _ptr(draft_parent), _ptr(workspace), workspace.numel(), _stream(stream))
+    if check:
+        _check(rc, "ss_draft_attention")
     return rc
 
 
