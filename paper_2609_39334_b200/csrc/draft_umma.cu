@@ -1,0 +1,563 @@
+// Tensor-core kernel of ss_draft_attention (tcgen05 + TMEM + TMA): one block per SM, 128 keys a step.
+//
+// A UNIT is a block of rows of one path and kv head - up to two tiles of 128 rows, token-major, the G heads of the group side by
+// side - against the path's whole chain.  The steps of all units in a line are dealt out evenly: block b of the grid has steps
+// [b * quota, (b + 1) * quota), so every block has the same work whatever the lengths, and at most its first and its last unit are
+// shared with its neighbours.  What a block has of a shared unit goes out as a partial result (normalised, with its log-sum),
+// merged by the kernel behind this one; everything else is written once, final.
+//
+// Two softmax STREAMS of four warps, a thread per row, each with its own scores (128 TMEM columns) and accumulator (128):
+//   a unit of two tiles: stream s has tile s, both go over every step (a key is read once for up to 256 rows);
+//   a unit of one tile:  stream s has every other step, and the two accumulators are joined at the end.
+// So while one stream is in its softmax, the tensor cores work for the other.  S = Q K^T and O += P V of a stream are issued by one
+// lane in this order, and tcgen05 instructions of one thread run in order: a step's scores may overwrite the probabilities
+// before them, and when scores are there, the product before them is in the accumulator.
+// Softmax of a step: the row's exact maximum (the reference moves when it is exceeded by 2^8 only: exponentials stay below 2^8 and
+// the accumulator is hardly ever rescaled), exponentials, their fp32 sum, probabilities in bf16 over the scores they come from.
+// Masks: from 128 bits per row (which drafts it sees) and the page's place in the chain, in steps that reach the drafts only.
+// Keys that nobody may read (behind a node's end) have their V rows cleared in shared memory; a draft that holds NaN or an infinity
+// and is hidden from some rows reaches them as 0 * NaN: a row that is not finite is computed again, key by key, without it.
+// Roles: warps 0-3, 4-7 streams; 8 K and Q through TMA and the next unit's description; 9 V through TMA; 10, 11 issue the streams'
+// products.  Every wait is bounded (see umma.cuh).
+#include "draft_attn.cuh"
+#include "umma.cuh"
+
+namespace ss {
+namespace draft {
+
+using namespace umma;
+
+constexpr int kSoftmaxWarps = 8;
+constexpr int kThreads = (kSoftmaxWarps + 4) * 32;
+constexpr int kStageBytes = kTile * 256;       // one K or V step: [2 halves of 64 dims][128 rows][128 B]
+constexpr int kStagesK = 3, kStagesV = 2;
+constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
+constexpr int kOffQ = 0, kOffK = 65536, kOffV = kOffK + kStagesK * kStageBytes;
+constexpr int kSmem = kOffV + kStagesV * kStageBytes;
+constexpr float kLazyLog2 = 8.0f;
+
+struct Unit {
+  int valid;                                   // 0: the block's work is done
+  int g, n_tok, dual;
+  int tile0, n_tiles;                          // this block's steps of it
+  int slot;                                    // of its partial result; -1: the unit is this block's alone
+  int drafts0;                                 // index of the first draft in the path's sequence
+  int holes, clear_last;                       // a node that ends inside a page: anywhere, or in the last step
+  int64_t src, dst;                            // rows of q and out of its first token
+  Chain C;
+};
+struct Ctrl {
+  uint64_t q_full, k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV], v_land, s_full[2], p_full[2], o_final[2];
+  uint32_t tmem_slot;
+  int abort_flag;
+  int redo[2];                                 // by unit slot: some row is to be computed again
+  alignas(16) int coord[2][32];                // pool rows of the pages of four steps, by producer warp
+  long long warp_total[kThreads / 32];
+  long long pos, end, quota, off;              // this block's place in the line; off: in the steps of path `path`
+  int path;
+  Unit unit[2];
+};
+static_assert(sizeof(Ctrl) + kSmem <= 232448, "shared memory of a block");
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 pk = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&pk);
+}
+__device__ __forceinline__ void store_32B(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+
+__device__ __forceinline__ long long path_cost(const PathInfo& I, int Hkv) {
+  return I.T > 0 ? static_cast<long long>(I.tiles) * I.blocks * Hkv : 0;
+}
+
+// The next unit of this block's line into slot `dst` (one thread).
+__device__ __noinline__ void fetch_unit(Ctrl& C, const Params& P, int dst) {
+  Unit& U = C.unit[dst];
+  U.valid = 0;
+  if (C.pos >= C.end || C.abort_flag) return;
+  PathInfo I = P.paths[C.path];
+  while (C.off >= path_cost(I, P.Hkv)) {       // (ends: steps are left)
+    C.off -= path_cost(I, P.Hkv);
+    I = P.paths[++C.path];
+  }
+  const int u = static_cast<int>(C.off / I.tiles);
+  U.tile0 = static_cast<int>(C.off - static_cast<long long>(u) * I.tiles);
+  U.n_tiles = static_cast<int>(min(static_cast<long long>(I.tiles - U.tile0), C.end - C.pos));
+  U.g = u / I.blocks;
+  const int tok0 = (u - U.g * I.blocks) * I.per_block;
+  U.n_tok = min(I.per_block, I.T - tok0);
+  U.dual = U.n_tok > P.tok_per_tile;
+  U.drafts0 = I.L - I.T;
+  U.holes = I.holes;
+  U.clear_last = I.L % kTile != 0 || I.L == 0;
+  U.src = I.src + tok0;
+  U.dst = I.dst + tok0;
+  chain_of(U.C, P, I.leaf);
+  const bool first = C.pos == C.quota * blockIdx.x, whole = U.n_tiles == I.tiles;
+  U.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (first ? 0 : 1);
+  if (!whole && U.tile0 == 0) {                // it starts here and ends with block `last`: the merge begins at this block
+    const int last = static_cast<int>((C.pos + I.tiles - 1) / C.quota);
+    P.cuts[blockIdx.x] = CutUnit{last - static_cast<int>(blockIdx.x) + 1, U.slot, U.g, U.n_tok, U.dst};
+  }
+  C.pos += U.n_tiles;
+  C.off += U.n_tiles;
+  U.valid = 1;
+}
+
+// The rows of a unit's part once more, a warp per row, key by key: what a row does not see is not touched.
+__device__ __noinline__ void unit_rows_exact(const Params& P, const Unit& U, int warp, int lane) {
+  const int rows = U.n_tok * P.G;
+  for (int x = warp; x < rows; x += kThreads / 32) {
+    const int t = x / P.G, h = U.g * P.G + x - t * P.G;
+    Row r;
+    row_start(r, P.q + ((U.src + t) * P.Hq + h) * kDim, lane);
+    row_visit(r, U.C, P, U.g, U.tile0 * kTilePages, (U.tile0 + U.n_tiles) * kTilePages, U.drafts0, P.seen[U.dst + t], lane);
+    const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+    float o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = r.l == 0.f ? 0.f : r.acc[i] * inv;
+    if (U.slot < 0) {
+      store_out(P, U.dst + t, h, lane, o, row_lse(r.m, r.l));
+    } else {
+      const int64_t at = static_cast<int64_t>(U.slot) * (2 * kRows) + (t < P.tok_per_tile ? x : kRows + x - P.tok_per_tile * P.G);
+      *reinterpret_cast<float4*>(P.part_o + at * kDim + 4 * lane) = make_float4(o[0], o[1], o[2], o[3]);
+      if (lane == 0) P.part_lse[at] = row_lse(r.m, r.l);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                  const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ Params P) {
+  ss::grid_dependency_enter();
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ Ctrl C;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int* abort_flag = &C.abort_flag;
+
+  if (tid == 0) {
+    C.abort_flag = (smem_u32(smem) & 1023u) ? 1 : 0;
+    C.redo[0] = C.redo[1] = 0;
+    mbar_init(&C.q_full, 1);
+    for (int s = 0; s < kStagesK; ++s) { mbar_init(&C.k_full[s], 1); mbar_init(&C.k_empty[s], 2); }
+    for (int s = 0; s < kStagesV; ++s) { mbar_init(&C.v_full[s], 1); mbar_init(&C.v_empty[s], 2); }
+    mbar_init(&C.v_land, 1);
+    for (int s = 0; s < 2; ++s) { mbar_init(&C.s_full[s], 1); mbar_init(&C.p_full[s], 128); mbar_init(&C.o_final[s], 1); }
+    fence_barrier_init();
+    prefetch_tensormap(&tmap_k);
+    prefetch_tensormap(&tmap_v);
+    prefetch_tensormap(&tmap_q);
+    P.cuts[blockIdx.x].n = 0;
+  }
+  // (What shared memory holds in rows that no box of Q rows reaches comes out in rows that nobody reads.)
+  if (warp == kSoftmaxWarps) tmem_alloc(&C.tmem_slot, kTmemCols);
+
+  // ---- this block's place in the line: sums over the paths, a stretch of them per thread
+  const int chunk = (P.num_paths + kThreads - 1) / kThreads;
+  const int p0 = min(tid * chunk, P.num_paths), p1 = min(p0 + chunk, P.num_paths);
+  long long mine = 0;
+  for (int p = p0; p < p1; ++p) {
+    const PathInfo I = P.paths[p];
+    if (I.status != SS_OK && blockIdx.x == 0) set_status(&P.hdr->status, I.status);
+    mine += path_cost(I, P.Hkv);
+  }
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) C.warp_total[warp] = incl;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += C.warp_total[w];
+    total += C.warp_total[w];
+  }
+  incl += before;
+  const long long quota = max((total + gridDim.x - 1) / gridDim.x, 1LL), start = quota * blockIdx.x;
+  if (tid == 0) { C.pos = start; C.end = min(start + quota, total); C.quota = quota; C.path = 0; C.off = 0; }
+  __syncthreads();
+  if (start < total && incl - mine <= start && start < incl) {
+    C.path = p0;
+    C.off = start - (incl - mine);
+  }
+  __syncthreads();
+  if (tid == kSoftmaxWarps * 32) fetch_unit(C, P, 0);
+  __syncthreads();
+
+  const uint32_t tmem = C.tmem_slot;
+  const int G = P.G, tpt = P.tok_per_tile;
+  uint32_t g_tile = 0;                         // steps behind this block (the same in every role)
+  uint32_t n_s[2] = {0, 0}, n_o[2] = {0, 0};   // steps, and units with a step, behind each stream
+  uint32_t n_land = 0;                         // V producer: cleared steps so far
+  uint32_t seq = 0;
+
+  for (;; ++seq) {
+    const Unit& U = C.unit[seq & 1];
+    if (!U.valid) break;
+    const int n_tiles = U.n_tiles, dual = U.dual;
+    const int steps[2] = {dual ? n_tiles : (n_tiles + 1) / 2, dual ? n_tiles : n_tiles / 2};
+
+    if (warp < kSoftmaxWarps) {
+      // =================================================== softmax + epilogue ==================================
+      const int s = warp >> 2, row = tid & 127, mine_steps = steps[s];
+      const int tok_base = dual && s ? tpt : 0, tok_here = dual ? (s ? U.n_tok - tpt : tpt) : U.n_tok;
+      const int i = row / G, hl = row - i * G;
+      const bool row_valid = i < tok_here;
+      const uint4 seen = row_valid ? P.seen[U.dst + tok_base + i] : make_uint4(0, 0, 0, 0);
+      const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+      const uint32_t t_s = tmem + lanes + kColS + s * 128, t_o = tmem + lanes + kColO + s * 128;
+      const float cl2 = P.scale_log2, lazy_raw = kLazyLog2 / cl2;
+      const int pages = U.C.first[U.C.n];
+      float m = -INFINITY, l = 0.f;
+      bool ok = true;
+      for (int k = 0; k < mine_steps; ++k) {
+        const int jt = U.tile0 + (dual ? k : 2 * k + s);
+        uint32_t mask[4];
+        const bool masked = U.holes || (jt + 1) * kTile > U.drafts0;             // (block-uniform)
+        if (masked) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            mask[w] = 0;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int vp = jt * kTilePages + 2 * w + x;
+              if (vp < pages) mask[w] |= page_mask(U.C, segment_of(U.C, vp), vp, U.drafts0, seen) << (16 * x);
+            }
+          }
+        }
+        if (!mbar_wait(&C.s_full[s], (n_s[s] + k) & 1, abort_flag)) ok = false;
+        tc_fence_after();
+        uint32_t sr[64];
+        auto load64 = [&](int c0) {
+          tmem_ld32(t_s + c0, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
+          tmem_ld32(t_s + c0 + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
+          tmem_wait_ld();
+          if (masked) {
+            const uint32_t w0 = c0 ? mask[2] : mask[0], w1 = c0 ? mask[3] : mask[1];
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+              if (!((w0 >> c) & 1u)) sr[c] = 0xff800000u;                        // -inf
+              if (!((w1 >> c) & 1u)) sr[32 + c] = 0xff800000u;
+            }
+          }
+        };
+        auto max64 = [&]() {
+          float e[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < 64; c += 2) e[(c >> 1) & 3] = max3(e[(c >> 1) & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
+          return fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
+        };
+        load64(0);
+        float mx = max64();
+        load64(64);
+        mx = fmaxf(mx, max64());
+        float alpha = 1.f;
+        const bool move = mx > m + lazy_raw;                                     // (also for a row's first visible key)
+        if (move) {
+          alpha = ex2((m - mx) * cl2);                                           // 0 for the first
+          m = mx;
+          l *= alpha;
+        }
+        const float mc = m == -INFINITY ? 0.f : m * cl2;
+        const f32x2 cl2_2 = pack2(cl2, cl2), nmc2 = pack2(-mc, -mc);
+        f32x2 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+        uint32_t pr[32];
+        auto exp64 = [&]() {
+#pragma unroll
+          for (int c = 0; c < 64; c += 2) {
+            float x0, x1;
+            unpack2(fma2(pack2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), cl2_2, nmc2), x0, x1);
+            const float e0 = ex2(x0), e1 = ex2(x1);
+            sum2[(c >> 1) & 1] = add2(sum2[(c >> 1) & 1], pack2(e0, e1));
+            pr[c >> 1] = pack_bf16(e0, e1);
+          }
+        };
+        exp64();                                                                 // keys 64 .. 127: over the columns they are in
+        tmem_st32(t_s + 64, pr);
+        load64(0);
+        exp64();
+        tmem_st32(t_s, pr);
+        float a0, a1, a2, a3;
+        unpack2(sum2[0], a0, a1);
+        unpack2(sum2[1], a2, a3);
+        l += (a0 + a1) + (a2 + a3);
+        if (__any_sync(0xffffffffu, move && k > 0)) {                            // rescale O (warp-collective)
+#pragma unroll 1
+          for (int c0 = 0; c0 < kDim; c0 += 32) {
+            uint32_t o[32];
+            tmem_ld32(t_o + c0, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
+            tmem_st32(t_o + c0, o);
+          }
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&C.p_full[s]);
+      }
+      // ---- epilogue
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (steps[x] > 0 && (x == s || !dual)) ok = mbar_wait(&C.o_final[x], n_o[x] & 1, abort_flag) && ok;
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      float w_own = 1.f, w_oth = 0.f;
+      if (!dual) {                                                               // the two streams of a row become one
+        float* xm = reinterpret_cast<float*>(smem + kOffQ + 32768);              // (the second tile's rows of Q: not in use)
+        xm[s * 128 + row] = m;
+        xm[256 + s * 128 + row] = l;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const float m2 = xm[(s ^ 1) * 128 + row], l2 = xm[256 + (s ^ 1) * 128 + row];
+        const float top = fmaxf(m, m2);
+        w_own = m == -INFINITY ? 0.f : ex2((m - top) * cl2);
+        w_oth = m2 == -INFINITY ? 0.f : ex2((m2 - top) * cl2);
+        l = s == 0 ? l * w_own + l2 * w_oth : l2 * w_oth + l * w_own;
+        m = top;
+        fence_proxy_async_smem();                                                // (TMA writes here again, for a unit of two tiles)
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float lse = l == 0.f ? -INFINITY : m * P.scale + __logf(l);
+      w_own *= inv;
+      w_oth *= inv;
+      const int c_begin = dual ? 0 : s * 64, c_end = dual ? kDim : s * 64 + 64;
+      const uint32_t t_oth = tmem + lanes + kColO + (s ^ 1) * 128;
+      const bool has_own = steps[s] > 0, has_oth = !dual && steps[s ^ 1] > 0;
+      bool finite = lse < INFINITY;                                              // (not for a NaN)
+      if (ok) {
+#pragma unroll 1
+        for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+          uint32_t o[32];
+          __syncwarp();
+          if (has_own) {
+            tmem_ld32(t_o + c0, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * w_own);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = 0u;
+          }
+          if (has_oth) {
+            uint32_t o2[32];
+            tmem_ld32(t_oth + c0, o2);
+            tmem_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(fmaf(__uint_as_float(o2[x]), w_oth, __uint_as_float(o[x])));
+          }
+#pragma unroll
+          for (int x = 0; x < 32; ++x) finite = finite && fabsf(__uint_as_float(o[x])) < INFINITY;
+          if (!row_valid) continue;
+          if (U.slot < 0) {
+            __nv_bfloat16* dst = P.out + ((U.dst + tok_base + i) * P.Hq + U.g * G + hl) * kDim + c0;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              uint32_t w[8];
+#pragma unroll
+              for (int y = 0; y < 8; ++y) w[y] = pack_bf16(__uint_as_float(o[16 * x + 2 * y]), __uint_as_float(o[16 * x + 2 * y + 1]));
+              store_32B(dst + 16 * x, w);
+            }
+          } else {
+            float* dst = P.part_o + (static_cast<int64_t>(U.slot) * (2 * kRows) + (dual && s ? kRows : 0) + row) * kDim + c0;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t w[8] = {o[8 * x], o[8 * x + 1], o[8 * x + 2], o[8 * x + 3], o[8 * x + 4], o[8 * x + 5], o[8 * x + 6], o[8 * x + 7]};
+              store_32B(dst + 8 * x, w);
+            }
+          }
+        }
+        if (row_valid && !finite) C.redo[seq & 1] = 1;
+        if (row_valid && (dual || s == 0)) {
+          if (U.slot >= 0) P.part_lse[static_cast<int64_t>(U.slot) * (2 * kRows) + (dual && s ? kRows : 0) + row] = lse;
+          else if (P.lse) P.lse[(U.dst + tok_base + i) * P.Hq + U.g * G + hl] = lse;
+        }
+      }
+    } else if (warp < kSoftmaxWarps + 2) {
+      // =================================================== producers ==============================================
+      const int which = warp - kSoftmaxWarps;                    // 0: K (and Q), 1: V
+      const int n_stages = which ? kStagesV : kStagesK;
+      const CUtensorMap* tm = which ? &tmap_v : &tmap_k;
+      uint64_t* full = which ? C.v_full : C.k_full;
+      uint64_t* empty = which ? C.v_empty : C.k_empty;
+      uint8_t* ring = smem + (which ? kOffV : kOffK);
+      const int pages = U.C.first[U.C.n];
+      bool ok = true;
+      if (which == 0 && elect_one()) {
+        mbar_arrive_expect_tx(&C.q_full, static_cast<uint32_t>((dual ? 2 : 1) * 2 * 128 * G * tpt));
+        for (int x = 0; x < 1 + dual; ++x) {
+          uint8_t* dst = smem + kOffQ + x * 32768;
+          const int src = static_cast<int>(U.src) + x * tpt;
+          tma_load_3d(dst, &tmap_q, 0, U.g * G, src, &C.q_full);
+          tma_load_3d(dst + 16384, &tmap_q, 64, U.g * G, src, &C.q_full);
+        }
+      }
+      __syncwarp();
+      // The pages of four steps at a time, one a lane, a block ahead of their use; one elected lane issues the copies.
+      auto pool_row = [&](int j, int pg) -> int {
+        const int vp = (U.tile0 + j) * kTilePages + pg;
+        if (j >= n_tiles || vp >= pages) return 0;
+        return static_cast<int>((physical_page(U.C, P, segment_of(U.C, vp), vp) * P.page_stride + static_cast<int64_t>(U.g) * P.head_stride) >> 7);
+      };
+      int* coord = C.coord[which];
+      int cur = pool_row(lane >> 3, lane & 7);
+      for (int j0 = 0; j0 < n_tiles && ok; j0 += 4) {
+        const int nxt = pool_row(j0 + 4 + (lane >> 3), lane & 7);
+        coord[lane] = cur;
+        __syncwarp();
+        for (int t = 0; t < 4 && j0 + t < n_tiles && ok; ++t) {
+          const uint32_t gj = g_tile + j0 + t;
+          const int st = gj % n_stages, jt = U.tile0 + j0 + t;
+          const uint32_t u = gj / n_stages;
+          const int n_pages = max(0, min(kTilePages, pages - jt * kTilePages));
+          const bool last = (jt + 1) * kTilePages >= pages;
+          const bool clear = which == 1 && (U.holes || (last && U.clear_last));
+          if (u > 0) ok = mbar_wait(&empty[st], (u - 1) & 1, abort_flag);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          uint8_t* dst = ring + st * kStageBytes;
+          if (elect_one()) {
+            uint64_t* bar = clear ? &C.v_land : &full[st];
+            mbar_arrive_expect_tx(bar, static_cast<uint32_t>(n_pages) * 4096u);
+#pragma unroll
+            for (int pg = 0; pg < kTilePages; ++pg) {
+              if (pg < n_pages) {
+                const int y = coord[t * 8 + pg];
+                tma_load_2d(dst + pg * 2048, tm, 0, y, bar);
+                tma_load_2d(dst + 16384 + pg * 2048, tm, 64, y, bar);
+              }
+            }
+          }
+          __syncwarp();
+          if (clear) {                                           // V rows of keys that are none
+            ok = mbar_wait(&C.v_land, n_land & 1, abort_flag);
+            ++n_land;
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            for (int r = lane; r < kTile; r += 32) {
+              const int vp = jt * kTilePages + (r >> 4);
+              bool there = false;
+              if (vp < pages) {
+                const int sg = segment_of(U.C, vp);
+                there = (vp - U.C.first[sg]) * kPage + (r & 15) < U.C.len[sg];
+              }
+              if (!there) {
+#pragma unroll
+                for (int x = 0; x < 16; ++x) *reinterpret_cast<uint4*>(dst + (x >> 3) * 16384 + r * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+              }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&full[st]);
+          }
+        }
+        __syncwarp();
+        cur = nxt;
+      }
+      if (which == 0 && lane == 0) fetch_unit(C, P, (seq & 1) ^ 1);
+    } else {
+      // =================================================== products of stream s =================================
+      const int s = warp - (kSoftmaxWarps + 2);
+      if (steps[s] > 0 && elect_one()) {
+        constexpr uint32_t idesc_qk = instr_desc_bf16(128, kTile, false), idesc_pv = instr_desc_bf16(128, kDim, true);
+        const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + kOffQ + (dual ? s : 0) * 32768), 0, 1024);
+        const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem + kOffK), 0, 1024);
+        const uint64_t v_desc0 = smem_desc_sw128(smem_u32(smem + kOffV), 16384, 1024);
+        const uint32_t t_s = tmem + kColS + s * 128, t_o = tmem + kColO + s * 128;
+        bool ok = mbar_wait(&C.q_full, seq & 1, abort_flag);
+        for (int k = 0; k < steps[s] && ok; ++k) {
+          const uint32_t gj = g_tile + (dual ? k : 2 * k + s);
+          const int sk = gj % kStagesK, sv = gj % kStagesV;
+          ok = mbar_wait(&C.k_full[sk], (gj / kStagesK) & 1, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t k_desc = smem_desc_advance(k_desc0, static_cast<uint32_t>(sk) * kStageBytes);
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)
+            mma_bf16_ss(t_s, smem_desc_advance(q_desc, (kk >> 2) * 16384 + (kk & 3) * 32),
+                        smem_desc_advance(k_desc, (kk >> 2) * 16384 + (kk & 3) * 32), idesc_qk, kk > 0 ? 1u : 0u);
+          mma_commit(&C.s_full[s]);
+          mma_commit(&C.k_empty[sk]);
+          if (!dual) mma_commit(&C.k_empty[sk]);
+          ok = mbar_wait(&C.v_full[sv], (gj / kStagesV) & 1, abort_flag) && mbar_wait(&C.p_full[s], (n_s[s] + k) & 1, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t v_desc = smem_desc_advance(v_desc0, static_cast<uint32_t>(sv) * kStageBytes);
+#pragma unroll
+          for (int kk = 0; kk < kTile / 16; ++kk)                // P of keys 0..63 at columns 0..31, of keys 64..127 at 64..95
+            mma_bf16_ts(t_o, t_s + (kk >> 2) * 64 + (kk & 3) * 8, smem_desc_advance(v_desc, kk * 2048), idesc_pv,
+                        (k > 0 || kk > 0) ? 1u : 0u);
+          mma_commit(&C.v_empty[sv]);
+          if (!dual) mma_commit(&C.v_empty[sv]);
+          if (k + 1 == steps[s]) mma_commit(&C.o_final[s]);
+        }
+      }
+    }
+    // ---- the unit's end: every role meets here, the pipeline is empty
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (C.redo[seq & 1]) {
+      unit_rows_exact(P, U, warp, lane);
+      __syncthreads();
+      if (tid == 0) C.redo[seq & 1] = 0;
+    }
+    g_tile += n_tiles;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      n_s[x] += steps[x];
+      n_o[x] += steps[x] > 0 ? 1 : 0;
+    }
+  }
+
+  __syncthreads();
+  if (C.abort_flag) {
+    if (tid == 0) set_status(&P.hdr->status, SS_ERR_TIMEOUT);
+    const long long t0 = clock64();                              // let copies and products that are in flight land
+    while (clock64() - t0 < 4000000LL) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == kSoftmaxWarps) tmem_dealloc(tmem, kTmemCols);
+}
+
+int32_t launch_tiles(const Params& P, cudaStream_t st, int blocks) {
+  static bool configured[kDeviceSlots] = {false};
+  const int dev_slot = current_device_slot();
+  if (dev_slot < 0 || !configured[dev_slot]) {
+    if (cudaFuncSetAttribute(draft_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return SS_ERR_CUDA;
+    }
+    if (dev_slot >= 0) configured[dev_slot] = true;
+  }
+  const int64_t rows = ((P.num_pages > 0 ? P.num_pages - 1 : 0) * P.page_stride + (P.Hkv - 1) * P.head_stride) / 128 + kPage;
+  if (rows >= 0x7fffffffLL) return SS_ERR_UNSUPPORTED;
+  CUtensorMap tk, tv, tq;
+  if (!tmap::encode_2d_bf16(&tk, P.k_pool, kDim, static_cast<uint64_t>(rows), kDim * 2, kPage) ||
+      !tmap::encode_2d_bf16(&tv, P.v_pool, kDim, static_cast<uint64_t>(rows), kDim * 2, kPage) ||
+      !tmap::encode_q_bf16(&tq, P.q, static_cast<uint64_t>(P.Hq), static_cast<uint64_t>(P.q_rows > 0 ? P.q_rows : 1),
+                           static_cast<uint32_t>(P.G), static_cast<uint32_t>(P.tok_per_tile)))
+    return SS_ERR_CUDA;
+  SS_LAUNCH(draft_umma_kernel, blocks, kThreads, kSmem, st, tk, tv, tq, P);
+  return SS_OK;
+}
+
+}  // namespace draft
+}  // namespace ss
