@@ -409,6 +409,56 @@ int32_t ss_branch_sample_upto(const float* logits, const int64_t* draw_offsets, 
                               void* stream);
 
 /* =========================================================================================================
+ * ss_filtered_sample - the draws of on-demand branching behind top-k, top-p and min-p filters.
+ *
+ * (Paper: as for ss_branch_sample, whose distribution is the whole softmax; the filters are those of the paper's samplers, Section
+ * "Experimental Setup", which prints no formula.)  Per sequence s, with M its largest logit and e_v = exp((logit_v - M) / T):
+ *   order      tokens by logit, largest first, equal ones by index; logits of -inf are never kept
+ *   top-k      n_k = the first k tokens                                                 k <= 0 or k >= vocab: all
+ *   top-p      n_p = the smallest n >= 1 with  e_1 + .. + e_n >= p * (e_1 + .. + e_{n_k})    p >= 1 (or NaN): n_k
+ *   min-p      n_m = the tokens with  e >= m, at least one                             m <= 0 (or NaN): all
+ *   kept       the first min(n_k, n_p, n_m) tokens
+ *   a draw     with uniform u is the smallest kept v with  C_v > u * C,  C_v = sum of e over kept tokens up to index v, C over all
+ * all evaluated in fp64 (so that a decision is that of the definition but for differences of about 1e-12 of a sum).  T = 0 keeps
+ * the first token alone.  A row that holds a NaN or +inf, or no finite logit, or whose T is negative, NaN or infinite, has no
+ * distribution: its draws are -1 and 0 tokens are kept.  A uniform outside [0, 1) counts as the nearer end, a NaN as the upper one.
+ *
+ *   logits        fp32 or bf16 [n_seq], rows of `vocab` at row_stride elements; any alignment of a row
+ *   draw_offsets, uniforms, tokens_out, seq_out  as for ss_branch_sample; seq_out may be NULL; tokens_out and seq_out hold draws
+ *                 draw_offsets[0] .. draw_offsets[n_seq]-1 at their own index
+ *   temperature, top_k, top_p, min_p   [n_seq] on the device, or NULL: the scalar of that name for every sequence
+ *   kept_out      int32 [n_seq] or NULL: tokens kept
+ *   workspace     >= ss_filtered_sample_workspace_bytes(desc) bytes, 256-byte aligned.  Calls that share one must not overlap
+ * vocab <= 2097152 (else SS_ERR_UNSUPPORTED).  A sequence without draws is worked on only for kept_out.
+ * Errors: SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE_TOO_SMALL, SS_ERR_CUDA.
+ * ======================================================================================================= */
+#define SS_LOGITS_FP32 0
+#define SS_LOGITS_BF16 1
+typedef struct ss_sample_desc {
+  uint32_t struct_size;              /* = sizeof(ss_sample_desc_t) */
+  uint32_t flags;                    /* 0 */
+  int32_t n_seq, vocab;
+  int32_t logits_type;               /* SS_LOGITS_* */
+  int32_t top_k_all;                 /* the scalars are used where the array of the same name is NULL */
+  float temperature_all, top_p_all, min_p_all;
+  int32_t reserved;
+  int64_t row_stride;                /* elements, >= vocab */
+  const void* logits;
+  const int64_t* draw_offsets;       /* [n_seq + 1] */
+  const float* uniforms;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* tokens_out;
+  int64_t* seq_out;
+  int32_t* kept_out;
+} ss_sample_desc_t;
+
+int32_t ss_filtered_sample_workspace_bytes(const ss_sample_desc_t* desc /* host */, size_t* out_bytes /* host */);
+int32_t ss_filtered_sample(const ss_sample_desc_t* desc /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
+/* =========================================================================================================
  * ss_build_prefix_tree - radix tree of candidate paths over whole KV pages, from raw token ids.
  *
  * Paper: Section "Computation Deduplication" (a quarter to a half of the tokens that the candidates of a step

@@ -33,6 +33,7 @@ SS_MAX_DEPTH = 16
 SS_STEP_COMPACT_TRANSFERS = 0x1
 SS_ROWS_INTERLEAVED = 0x1
 SS_MAX_DRAFT = 128
+SS_LOGITS_FP32, SS_LOGITS_BF16 = 0, 1
 SS_DEDUP_STATIC_MAX_PATHS = 65536
 
 EXPORTS = [
@@ -44,6 +45,7 @@ EXPORTS = [
     "ss_prefix_tree_workspace_bytes", "ss_build_prefix_tree", "ss_candidate_step",
     "ss_candidate_step_host_2", "ss_branch_sample_upto",
     "ss_qk_norm_rope", "ss_kv_append", "ss_draft_attention_workspace_bytes", "ss_draft_attention",
+    "ss_filtered_sample_workspace_bytes", "ss_filtered_sample",
 ]
 PHASES = ["plan", "tiles", "leaves", "generic", "merge"]
 
@@ -92,6 +94,7 @@ _SIGNATURES = {
     "ss_candidate_step": "pp", "ss_candidate_step_host_arena_bytes": "pp", "ss_candidate_step_host": "ppzp", "ss_candidate_step_host_2": "ppzpp", "ss_profile_enable": "i",
     "ss_profile_read": "pp", "ss_debug_umma_tile": "pppiiipp", "ss_debug_bounded_wait": "pp",
     "ss_qk_norm_rope": "pp", "ss_kv_append": "ppp", "ss_draft_attention_workspace_bytes": "pp", "ss_draft_attention": "pppzp",
+    "ss_filtered_sample_workspace_bytes": "pp", "ss_filtered_sample": "ppzp",
 }
 
 
@@ -481,6 +484,60 @@ def ss_branch_sample(logits, draw_offsets, uniforms, n_seq, vocab, temperature, 
                                      _stream(stream))
     if check:
         _check(rc, "ss_branch_sample")
+    return rc
+
+
+class ss_sample_desc_t(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+        ("n_seq", ctypes.c_int32), ("vocab", ctypes.c_int32),
+        ("logits_type", ctypes.c_int32), ("top_k_all", ctypes.c_int32),
+        ("temperature_all", ctypes.c_float), ("top_p_all", ctypes.c_float), ("min_p_all", ctypes.c_float),
+        ("reserved", ctypes.c_int32), ("row_stride", ctypes.c_int64),
+    ] + [(n, ctypes.c_void_p) for n in ("logits", "draw_offsets", "uniforms", "temperature", "top_k", "top_p", "min_p", "tokens_out",
+                                        "seq_out", "kept_out")]
+
+
+def make_sample_desc(*, logits, draw_offsets, uniforms, tokens_out, seq_out=None, kept_out=None, temperature=1.0, top_k=0, top_p=1.0,
+                     min_p=0.0) -> ss_sample_desc_t:
+    """Fills ss_sample_desc_t.  logits: fp32 or bf16 [n_seq][vocab] of any row stride; temperature, top_k, top_p, min_p: a number for
+    every sequence, or a device tensor with one each.  The returned object keeps references to the tensors."""
+    d = ss_sample_desc_t()
+    d.struct_size = ctypes.sizeof(ss_sample_desc_t)
+    assert logits.is_cuda and logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] <= 1)
+    assert logits.dtype in (torch.float32, torch.bfloat16)
+    d.n_seq, d.vocab = logits.shape
+    d.logits_type = SS_LOGITS_BF16 if logits.dtype == torch.bfloat16 else SS_LOGITS_FP32
+    d.row_stride = max(logits.stride(0), d.vocab)
+    d.logits = logits.data_ptr()
+    assert draw_offsets.dtype == torch.int64 and draw_offsets.numel() == d.n_seq + 1
+    assert uniforms.dtype == torch.float32 and tokens_out.dtype == torch.int32
+    assert seq_out is None or seq_out.dtype == torch.int64
+    assert kept_out is None or (kept_out.dtype == torch.int32 and kept_out.numel() >= d.n_seq)
+    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                               ("min_p", min_p, torch.float32)):
+        if isinstance(value, torch.Tensor):
+            assert value.dtype == dtype and value.numel() >= d.n_seq, name
+            setattr(d, name, _ptr(value))
+        else:
+            setattr(d, name + "_all", value)
+    d.draw_offsets, d.uniforms, d.tokens_out = _ptr(draw_offsets), _ptr(uniforms), _ptr(tokens_out)
+    d.seq_out, d.kept_out = _ptr(seq_out), _ptr(kept_out)
+    d._keep = (logits, draw_offsets, uniforms, tokens_out, seq_out, kept_out, temperature, top_k, top_p, min_p)
+    return d
+
+
+def ss_filtered_sample_workspace_bytes(desc: ss_sample_desc_t) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().ss_filtered_sample_workspace_bytes(ctypes.byref(desc), ctypes.byref(out)), "ss_filtered_sample_workspace_bytes")
+    return int(out.value)
+
+
+def ss_filtered_sample(desc: ss_sample_desc_t, workspace: torch.Tensor, stream=None, check=True) -> int:
+    """Draws behind temperature, top-k, top-p and min-p (see the header), any number for each sequence."""
+    rc = lib().ss_filtered_sample(ctypes.byref(desc), _ptr(workspace), workspace.numel(), _stream(stream))
+    if check:
+        _check(rc, "ss_filtered_sample")
     return rc
 
 

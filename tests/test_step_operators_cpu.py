@@ -121,3 +121,36 @@ def test_draft_arguments(lib):
     assert size % 256 == 0 and call(nbytes=size - 1) == B.SS_ERR_WORKSPACE_TOO_SMALL
     assert B.ss_draft_attention_workspace_bytes(desc(num_paths=5000, total_q=70000)) > size
     assert lib.ss_draft_attention_workspace_bytes(ctypes.byref(desc()), None) == B.SS_ERR_INVALID_ARG
+
+
+def sample(**kw):
+    d = B.ss_sample_desc_t()
+    d.struct_size = ctypes.sizeof(B.ss_sample_desc_t)
+    d.n_seq, d.vocab, d.row_stride, d.temperature_all, d.top_p_all = 4, 1000, 1000, 1.0, 1.0
+    d.logits = d.draw_offsets = d.uniforms = d.tokens_out = OK
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(struct_size=4), B.SS_ERR_INVALID_ARG), (dict(flags=1), B.SS_ERR_INVALID_ARG), (dict(n_seq=-1), B.SS_ERR_INVALID_ARG),
+    (dict(vocab=0), B.SS_ERR_INVALID_ARG), (dict(row_stride=999), B.SS_ERR_INVALID_ARG), (dict(logits_type=2), B.SS_ERR_INVALID_ARG),
+    (dict(vocab=2097153, row_stride=2097153), B.SS_ERR_UNSUPPORTED)])
+def test_sample_descriptor(lib, kw, rc):
+    out = ctypes.c_size_t(0)
+    assert lib.ss_filtered_sample_workspace_bytes(ctypes.byref(sample(**kw)), ctypes.byref(out)) == rc
+    assert lib.ss_filtered_sample(ctypes.byref(sample(**kw)), OK, 1 << 40, None) == rc
+
+
+def test_sample_arguments(lib):
+    call = lambda ws=OK, nbytes=1 << 40, **kw: lib.ss_filtered_sample(ctypes.byref(sample(**kw)), ws, nbytes, None)
+    assert call(ws=None) == B.SS_ERR_INVALID_ARG
+    assert call(ws=OK + 16) == B.SS_ERR_INVALID_ARG
+    assert call(logits=None) == B.SS_ERR_INVALID_ARG
+    assert call(draw_offsets=None) == B.SS_ERR_INVALID_ARG
+    assert call(logits=OK + 2) == B.SS_ERR_UNSUPPORTED
+    assert call(n_seq=0, logits=None) == B.SS_OK
+    size = B.ss_filtered_sample_workspace_bytes(sample())
+    assert size % 256 == 0 and call(nbytes=size - 1) == B.SS_ERR_WORKSPACE_TOO_SMALL
+    assert lib.ss_filtered_sample_workspace_bytes(ctypes.byref(sample()), None) == B.SS_ERR_INVALID_ARG
