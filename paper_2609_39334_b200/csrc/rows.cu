@@ -10,7 +10,8 @@
 // the heads of ONE token (or, with few tokens, through a part of them), so the eight angles of a lane are made once a token: the
 // product in fp64 (a position of a million times a frequency of one has no bits behind the point left in fp32), the whole turns
 // off, the rest through sincospif.  Sums, norm and rotation are fp32.
-// Bound: HBM, every row read and written once.  The loads of kAhead head rows are issued before the first is used.
+// Bound: HBM, every row read and written once.  The loads of kAhead head rows are issued before the first is used; the weights are
+// in shared memory, which leaves room for kBlocks blocks an SM.
 #include "common.cuh"
 
 namespace ss {
@@ -18,7 +19,8 @@ namespace rows {
 
 constexpr int kDim = 128, kPage = 16;
 constexpr int kWarps = 8;                    // of a block
-constexpr int kAhead = 3;                    // head rows of a lane group in flight
+constexpr int kBlocks = 3;                   // per SM
+constexpr int kAhead = 2;                    // head rows of a lane group in flight
 
 struct Tensor { const __nv_bfloat16* p; int64_t row, head; };
 struct TensorOut { __nv_bfloat16* p; int64_t row, head; };
@@ -37,17 +39,15 @@ struct Place {                               // where the rows of a step go
   const int32_t *node_parent, *node_kv_len, *node_pages, *path_leaf_node, *path_q_len, *num_paths_dev;
   const int64_t *node_page_offsets, *q_offsets, *q_src_offsets;
   __nv_bfloat16 *k_pool, *v_pool;
-  int64_t num_pages, page_stride, head_stride, total_node_pages;
+  int64_t num_pages, page_stride, head_stride, total_node_pages, total_q;
   int num_nodes, num_paths;
-  int warps_per_path;                        // tokens of a path are dealt to this many (groups of `split`) warps
+  int run;                                   // tokens in a row that a warp takes
 };
 
-template <bool INTER>
 struct Lane {
   int c0, c1;                                // this lane's chunks of 8 values
   bool turn0, turn1;                         // which of them are rotated
   float cs[8], sn[8];                        // INTER: four pairs of chunk c0, then of c1; else pair j = value j of both
-  uint4 wq0, wq1, wk0, wk1;
 };
 
 __device__ __forceinline__ void unpack8(const uint4& u, float (&f)[8]) {
@@ -69,7 +69,7 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
 }
 
 template <bool INTER>
-__device__ __forceinline__ void lane_setup(Lane<INTER>& L, const Args& A, int sub) {
+__device__ __forceinline__ void lane_setup(Lane& L, const Args& A, int sub) {
   if (INTER) {
     L.c0 = sub; L.c1 = sub + 8;
     L.turn0 = L.c0 < A.rot / 8; L.turn1 = L.c1 < A.rot / 8;
@@ -79,20 +79,19 @@ __device__ __forceinline__ void lane_setup(Lane<INTER>& L, const Args& A, int su
     L.c0 = sub < half ? sub : 2 * sub;       // (behind the 2 * half rotated chunks the others follow two by two)
     L.c1 = sub < half ? sub + half : 2 * sub + 1;
   }
-  const uint4 one = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-  L.wq0 = L.wq1 = L.wk0 = L.wk1 = one;
-  if (A.q_weight) {
-    L.wq0 = __ldg(reinterpret_cast<const uint4*>(A.q_weight) + L.c0);
-    L.wq1 = __ldg(reinterpret_cast<const uint4*>(A.q_weight) + L.c1);
+}
+// The weights of queries and keys, [2][16] chunks (whole block).
+__device__ __forceinline__ void load_weights(uint4 (&w)[32], const Args& A) {
+  const int t = threadIdx.x;
+  if (t < 32) {
+    const __nv_bfloat16* p = t < 16 ? A.q_weight : A.k_weight;
+    if (p) w[t] = __ldg(reinterpret_cast<const uint4*>(p) + (t & 15));
   }
-  if (A.k_weight) {
-    L.wk0 = __ldg(reinterpret_cast<const uint4*>(A.k_weight) + L.c0);
-    L.wk1 = __ldg(reinterpret_cast<const uint4*>(A.k_weight) + L.c1);
-  }
+  __syncthreads();
 }
 
 template <bool INTER>
-__device__ __forceinline__ void lane_angles(Lane<INTER>& L, const Args& A, double position) {
+__device__ __forceinline__ void lane_angles(Lane& L, const Args& A, double position) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const int chunk = INTER ? (j < 4 ? L.c0 : L.c1) : L.c0;
@@ -109,9 +108,9 @@ __device__ __forceinline__ void lane_angles(Lane<INTER>& L, const Args& A, doubl
   }
 }
 
-// One head row (its two chunks in a, b): norm and rotation.
+// One head row (its two chunks in a, b): norm (with the weights at w, if any) and rotation.
 template <bool INTER>
-__device__ __forceinline__ void turn_row(const Lane<INTER>& L, bool norm, const uint4& w0, const uint4& w1, float eps, uint4& a, uint4& b) {
+__device__ __forceinline__ void turn_row(const Lane& L, const uint4* w, float eps, uint4& a, uint4& b) {
   float x0[8], x1[8];
   unpack8(a, x0);
   unpack8(b, x1);
@@ -120,42 +119,44 @@ __device__ __forceinline__ void turn_row(const Lane<INTER>& L, bool norm, const 
   for (int j = 0; j < 8; ++j) sum = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], sum));
 #pragma unroll
   for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (norm) {
+  if (w) {
     const float r = rsqrtf(sum * (1.f / kDim) + eps);
-    float w[8];
-    unpack8(w0, w);
+    float f[8];
+    unpack8(w[L.c0], f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x0[j] = x0[j] * r * w[j];
-    unpack8(w1, w);
+    for (int j = 0; j < 8; ++j) x0[j] = x0[j] * r * f[j];
+    unpack8(w[L.c1], f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x1[j] = x1[j] * r * w[j];
+    for (int j = 0; j < 8; ++j) x1[j] = x1[j] * r * f[j];
   }
   // (values that are not rotated stay as they are: a product with a sine of 0 would carry an infinity over)
-  float y0[8], y1[8];
+  if (INTER) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (INTER) {
-      const int e = j & ~1, i = j >> 1;
-      y0[j] = (j & 1) ? x0[e + 1] * L.cs[i] + x0[e] * L.sn[i] : x0[e] * L.cs[i] - x0[e + 1] * L.sn[i];
-      y1[j] = (j & 1) ? x1[e + 1] * L.cs[4 + i] + x1[e] * L.sn[4 + i] : x1[e] * L.cs[4 + i] - x1[e + 1] * L.sn[4 + i];
-    } else {
-      y0[j] = x0[j] * L.cs[j] - x1[j] * L.sn[j];
-      y1[j] = x1[j] * L.cs[j] + x0[j] * L.sn[j];
+    for (int i = 0; i < 4; ++i) {
+      const float a0 = x0[2 * i], b0 = x0[2 * i + 1], a1 = x1[2 * i], b1 = x1[2 * i + 1];
+      if (L.turn0) { x0[2 * i] = a0 * L.cs[i] - b0 * L.sn[i]; x0[2 * i + 1] = b0 * L.cs[i] + a0 * L.sn[i]; }
+      if (L.turn1) { x1[2 * i] = a1 * L.cs[4 + i] - b1 * L.sn[4 + i]; x1[2 * i + 1] = b1 * L.cs[4 + i] + a1 * L.sn[4 + i]; }
     }
-    if (!L.turn0) y0[j] = x0[j];
-    if (!L.turn1) y1[j] = x1[j];
+  } else if (L.turn0) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float p = x0[j], q = x1[j];
+      x0[j] = p * L.cs[j] - q * L.sn[j];
+      x1[j] = q * L.cs[j] + p * L.sn[j];
+    }
   }
-  a = pack8(y0);
-  b = pack8(y1);
+  a = pack8(x0);
+  b = pack8(x1);
 }
 
 // The heads part, part + split, ... (in units of four: one per lane group) of row `row`: queries, then keys, then values.
-// `kd` / `vd`: where the row's keys and values go (head h at + h * kd_head); null: nowhere.
+// `kd` / `vd`: where the row's keys and values go (head h at + h * d_head); null: nowhere.
 template <bool INTER>
-__device__ __forceinline__ void token_heads(const Lane<INTER>& L, const Args& A, int64_t row, int part, int lane, __nv_bfloat16* kd,
-                                            __nv_bfloat16* vd, int64_t d_head) {
+__device__ __forceinline__ void token_heads(const Lane& L, const Args& A, const uint4* weights, int64_t row, int part, int lane,
+                                            __nv_bfloat16* kd, __nv_bfloat16* vd, int64_t d_head) {
   const int n_heads = A.hq + A.hk + A.hv;
   const int step = 4 * A.split;
+#pragma unroll 1
   for (int h0 = 4 * part; h0 < n_heads; h0 += step * kAhead) {                    // (warp-uniform)
     uint4 a[kAhead], b[kAhead];
     __nv_bfloat16* dst[kAhead];
@@ -182,50 +183,82 @@ __device__ __forceinline__ void token_heads(const Lane<INTER>& L, const Args& A,
     }
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) {
-      if (h0 + x * step >= n_heads) break;                                        // (warp-uniform)
-      const int h = h0 + x * step + (lane >> 3);
-      const bool is_q = h < A.hq;
-      uint4 y0 = a[x], y1 = b[x];
-      turn_row<INTER>(L, is_q ? A.q_weight != nullptr : A.k_weight != nullptr, is_q ? L.wq0 : L.wk0, is_q ? L.wq1 : L.wk1, A.eps, y0, y1);
-      if (h >= A.hq + A.hk) { y0 = a[x]; y1 = b[x]; }
+      const int h1 = h0 + x * step, h = h1 + (lane >> 3);
+      if (h1 >= n_heads) break;                                                   // (warp-uniform, as the next)
+      if (h1 < A.hq + A.hk) {
+        const bool is_q = h < A.hq;
+        const uint4* w = is_q ? (A.q_weight ? weights : nullptr) : (A.k_weight ? weights + 16 : nullptr);
+        uint4 y0 = a[x], y1 = b[x];
+        turn_row<INTER>(L, w, A.eps, y0, y1);
+        if (h < A.hq + A.hk) { a[x] = y0; b[x] = y1; }
+      }
       if (dst[x]) {
-        *(reinterpret_cast<uint4*>(dst[x]) + L.c0) = y0;
-        *(reinterpret_cast<uint4*>(dst[x]) + L.c1) = y1;
+        *(reinterpret_cast<uint4*>(dst[x]) + L.c0) = a[x];
+        *(reinterpret_cast<uint4*>(dst[x]) + L.c1) = b[x];
       }
     }
   }
 }
 
 template <bool INTER>
-__global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kWarps * 32, kBlocks) norm_rope_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
+  __shared__ uint4 weights[32];
+  load_weights(weights, A);
   const int lane = threadIdx.x & 31;
   const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps;
-  Lane<INTER> L;
-  lane_setup(L, A, lane & 7);
+  Lane L;
+  lane_setup<INTER>(L, A, lane & 7);
   for (int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); w < A.n_rows * A.split; w += warps) {
     const int64_t row = w / A.split;
-    lane_angles(L, A, A.positions ? static_cast<double>(__ldg(A.positions + row)) : 0.0);
-    token_heads<INTER>(L, A, row, static_cast<int>(w - row * A.split), lane, A.k_out.p ? A.k_out.p + row * A.k_out.row : nullptr,
-                       nullptr, A.k_out.head);
+    lane_angles<INTER>(L, A, A.positions ? static_cast<double>(__ldg(A.positions + row)) : 0.0);
+    token_heads<INTER>(L, A, weights, row, static_cast<int>(w - row * A.split), lane,
+                       A.k_out.p ? A.k_out.p + row * A.k_out.row : nullptr, nullptr, A.k_out.head);
   }
 }
 
+// Number of offsets[0 .. n] that are <= r, less one: the path of row r (whole warp; 32 probes a round).
+__device__ __forceinline__ int path_of(const int64_t* offsets, int n, int64_t r, int lane) {
+  int lo = 0, hi = n;                                          // offsets[lo] <= r < offsets[hi]
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, at = min(lo + (lane + 1) * step, hi);
+    const unsigned over = __ballot_sync(0xffffffffu, at >= hi || __ldg(offsets + at) > r);
+    const int first = __ffs(over) - 1;                         // (the last lane's probe is hi)
+    hi = min(lo + (first + 1) * step, hi);
+    lo = lo + first * step;
+  }
+  return lo;
+}
+
+// A warp takes `run` tokens in a row (of a part of their heads): it looks for the first one's path, the others follow it.
 template <bool INTER>
-__global__ void __launch_bounds__(kWarps * 32) append_kernel(const __grid_constant__ Args A, const __grid_constant__ Place P) {
+__global__ void __launch_bounds__(kWarps * 32, kBlocks) append_kernel(const __grid_constant__ Args A, const __grid_constant__ Place P) {
   ss::grid_dependency_enter();
+  __shared__ uint4 weights[32];
+  load_weights(weights, A);
   const int lane = threadIdx.x & 31;
   const int live = P.num_paths_dev ? min(max(__ldg(P.num_paths_dev), 0), P.num_paths) : P.num_paths;
-  const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps;
-  const int per_path = P.warps_per_path * A.split;
-  Lane<INTER> L;
-  lane_setup(L, A, lane & 7);
-  for (int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); w < static_cast<int64_t>(live) * per_path; w += warps) {
-    const int p = static_cast<int>(w / per_path), in_path = static_cast<int>(w - static_cast<int64_t>(p) * per_path);
-    const int part = in_path % A.split, t0 = in_path / A.split;
+  if (live == 0) return;
+  const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t first_row = __ldg(P.q_offsets), rows = min(__ldg(P.q_offsets + live) - first_row, P.total_q);
+  int64_t r = first_row + w / A.split * P.run;
+  const int part = static_cast<int>(w % A.split);
+  const int64_t r_end = min(r + P.run, first_row + rows);
+  if (r >= r_end) return;
+  Lane L;
+  lane_setup<INTER>(L, A, lane & 7);
+  int p = path_of(P.q_offsets, live, r, lane);
+  while (r < r_end) {
+    const int64_t q0 = __ldg(P.q_offsets + p), q1 = __ldg(P.q_offsets + p + 1);
     const int leaf = __ldg(P.path_leaf_node + p), T = __ldg(P.path_q_len + p);
-    const int64_t src0 = __ldg((P.q_src_offsets ? P.q_src_offsets : P.q_offsets) + p);
-    if (leaf < 0 || leaf >= P.num_nodes || t0 >= T) continue;
+    const int64_t src0 = P.q_src_offsets ? __ldg(P.q_src_offsets + p) : q0;
+    ++p;
+    if (r >= q1) {
+      if (p == live) break;
+      continue;
+    }
+    const int64_t stop = min(r_end, q1);
+    if (leaf < 0 || leaf >= P.num_nodes) { r = stop; if (p == live) break; continue; }
     const int len = __ldg(P.node_kv_len + leaf);
     const int64_t page0 = __ldg(P.node_page_offsets + leaf), page1 = __ldg(P.node_page_offsets + leaf + 1);
     int64_t before = 0;                                        // tokens in front of the leaf
@@ -236,10 +269,10 @@ __global__ void __launch_bounds__(kWarps * 32) append_kernel(const __grid_consta
         a = __ldg(P.node_parent + a);
       }
     }
-    for (int t = t0; t < T; t += P.warps_per_path) {
-      const int64_t row = src0 + t;
-      if (row < 0 || row >= A.n_rows) continue;
-      const int at = len - T + t;                              // token of the leaf
+    for (; r < stop; ++r) {
+      const int64_t t = r - q0, row = src0 + t;
+      if (t >= T || row < 0 || row >= A.n_rows) continue;
+      const int at = len - T + static_cast<int>(t);            // token of the leaf
       __nv_bfloat16 *kd = nullptr, *vd = nullptr;
       if (at >= 0) {
         const int64_t entry = page0 + at / kPage;
@@ -252,9 +285,10 @@ __global__ void __launch_bounds__(kWarps * 32) append_kernel(const __grid_consta
           }
         }
       }
-      lane_angles(L, A, A.positions ? static_cast<double>(__ldg(A.positions + row)) : static_cast<double>(before + at));
-      token_heads<INTER>(L, A, row, part, lane, kd, vd, P.head_stride);
+      lane_angles<INTER>(L, A, A.positions ? static_cast<double>(__ldg(A.positions + row)) : static_cast<double>(before + at));
+      token_heads<INTER>(L, A, weights, row, part, lane, kd, vd, P.head_stride);
     }
+    if (p == live) break;
   }
 }
 
@@ -362,14 +396,16 @@ extern "C" int32_t ss_kv_append(const ss_attn_desc_t* d, const ss_rows_t* rows, 
   P.total_node_pages = d->total_node_pages;
   P.num_nodes = d->num_nodes;
   P.num_paths = d->num_paths;
-  // The longest step is not known here, the mean one is: twice as many warps as the mean step has tokens, each then has a token or
-  // two of a step like the others, more of a long one.
-  const int64_t mean = ss::ceil_div64(d->total_q, d->num_paths);
-  const int64_t enough = static_cast<int64_t>(ss::sm_count_of_current_device()) * 64 / d->num_paths + 1;
-  const int64_t per_path = mean == 1 ? 1 : 2 * mean < enough ? 2 * mean : enough;
-  P.warps_per_path = static_cast<int>(per_path < 1 ? 1 : per_path > 1024 ? 1024 : per_path);
+  P.total_q = d->total_q;
   A.split = heads_split(d->total_q, A.hq + A.hk + A.hv);
-  const unsigned grid = grid_of(static_cast<int64_t>(d->num_paths) * P.warps_per_path * A.split);
+  // Tokens of a step lie side by side in their pages: a warp takes up to four in a row once there are enough of them for all warps
+  // four times over.
+  const int64_t resident = static_cast<int64_t>(ss::sm_count_of_current_device()) * kBlocks * kWarps;
+  const int64_t run = d->total_q * A.split / (resident * 4);
+  P.run = static_cast<int>(run < 1 ? 1 : run > 4 ? 4 : run);
+  const int64_t blocks = ss::ceil_div64(ss::ceil_div64(d->total_q, P.run) * A.split, kWarps);
+  if (blocks > 0x7fffffffLL) return SS_ERR_UNSUPPORTED;
+  const unsigned grid = static_cast<unsigned>(blocks);
   if (rows->flags & SS_ROWS_INTERLEAVED) {
     SS_LAUNCH(append_kernel<true>, grid, kWarps * 32, 0, ss::as_stream(stream), A, P);
   } else {
