@@ -254,7 +254,7 @@ int32_t ss_tree_attention(const ss_attn_desc_t* desc /* host */, void* workspace
  * fp32 arithmetic (the angle fp64), one rounding to bf16.
  *
  * ss_rows_t holds the rows of a step: bf16, row r of head h at r * row_stride + h * head_stride (strides in elements, multiples
- * of 8; all addresses 16-byte aligned; so q, k and v may be parts of one projection's output, and a padded one).
+ * of 8, not negative; all addresses 16-byte aligned; so q, k and v may be parts of one projection's output, and a padded one).
  *
  * ss_qk_norm_rope writes q_out from q and / or k_out from k (either pair may be NULL) for rows 0 .. n_rows-1.  An output may be
  * its input (same strides); any other overlap is undefined.

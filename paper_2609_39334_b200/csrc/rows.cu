@@ -7,11 +7,13 @@
 //
 // Eight lanes share a head row: each has two chunks of 8 values (16 bytes) that hold both members of its 8 pairs, so that a
 // rotation needs no exchange, and a row's sum of squares takes three shuffles.  A warp has four rows at a time and goes through
-// the heads of ONE token (or, with few tokens, through a part of them), so the eight angles of a lane are made once a token: the
-// product in fp64 (a position of a million times a frequency of one has no bits behind the point left in fp32), the whole turns
-// off, the rest through sincospif.  Sums, norm and rotation are fp32.
-// Bound: HBM, every row read and written once.  The loads of kAhead head rows are issued before the first is used; the weights are
-// in shared memory, which leaves room for kBlocks blocks an SM.
+// the heads of ONE token after the other (or, with few tokens, through a part of them): queries, keys, values.  The angles are made
+// once a token, two a lane: the product in fp64 (a position of a million times a frequency of one has no bits behind the point left
+// in fp32), the whole turns off, the rest through sincospif.  Sums, norm and rotation are fp32, two values an instruction, with
+// weight and angle in one factor per lane: y = r (x A + x' B), r the norm's.
+// Bound: HBM, every row read and written once, and issue slots not far behind (a row takes 22 clocks of an SM's share of the
+// bandwidth, and about 30 warp instructions).  What a token needs - row, place, position - is looked up by one lane each, for a
+// warp's whole run of tokens at once.
 #include "common.cuh"
 
 namespace ss {
@@ -19,8 +21,10 @@ namespace rows {
 
 constexpr int kDim = 128, kPage = 16;
 constexpr int kWarps = 8;                    // of a block
-constexpr int kBlocks = 3;                   // per SM
-constexpr int kAhead = 2;                    // head rows of a lane group in flight
+constexpr int kBlocks = 2;                   // per SM
+constexpr int kStages = 8;                   // head rows of a lane group in shared memory or on their way there
+constexpr int kSmem = kWarps * kStages * 1024;
+constexpr int kMostRun = 8;                  // tokens in a row that a warp takes
 
 struct Tensor { const __nv_bfloat16* p; int64_t row, head; };
 struct TensorOut { __nv_bfloat16* p; int64_t row, head; };
@@ -34,6 +38,7 @@ struct Args {
   float eps;
   int rot, hq, hk, hv;                       // heads to go through (0: tensor absent)
   int split;                                 // warps that share a token's heads
+  int run;                                   // tokens in a row that a warp takes
 };
 struct Place {                               // where the rows of a step go
   const int32_t *node_parent, *node_kv_len, *node_pages, *path_leaf_node, *path_q_len, *num_paths_dev;
@@ -41,28 +46,46 @@ struct Place {                               // where the rows of a step go
   __nv_bfloat16 *k_pool, *v_pool;
   int64_t num_pages, page_stride, head_stride, total_node_pages, total_q;
   int num_nodes, num_paths;
-  int run;                                   // tokens in a row that a warp takes
+};
+// What is to be known of a token; lane t of a warp has that of the run's token t.
+struct Token {
+  int64_t row;                               // of the inputs (and q_out); -1: skipped
+  int64_t kv;                                // where its keys and values go, relative to kd / vd (elements); -1: nowhere
+  double position;
 };
 
+// Fused factors of a lane's 16 values: y = x A + x' B, x' the other member of the pair.  Not INTER: pairs (value j of chunk c0, of
+// chunk c1), A and B hold c0's four pairs of values, then c1's; INTER: pairs within a chunk.
+typedef unsigned long long f32x2;
 struct Lane {
   int c0, c1;                                // this lane's chunks of 8 values
   bool turn0, turn1;                         // which of them are rotated
-  float cs[8], sn[8];                        // INTER: four pairs of chunk c0, then of c1; else pair j = value j of both
+  f32x2 a[8], b[8];
+};
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+struct WarpShared {
+  float cs[64], sn[64];
 };
 
-__device__ __forceinline__ void unpack8(const uint4& u, float (&f)[8]) {
+__device__ __forceinline__ f32x2 pack2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 swap2(f32x2 v) { float a, b; unpack2(v, a, b); return pack2(b, a); }
+
+__device__ __forceinline__ void unpack8(const uint4& u, f32x2 (&f)[4]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
+  for (int i = 0; i < 4; ++i) f[i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+__device__ __forceinline__ uint4 pack8(const f32x2 (&f)[4]) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    float x, y;
+    unpack2(f[i], x, y);
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
     w[i] = *reinterpret_cast<const uint32_t*>(&b);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
@@ -80,141 +103,210 @@ __device__ __forceinline__ void lane_setup(Lane& L, const Args& A, int sub) {
     L.c1 = sub < half ? sub + half : 2 * sub + 1;
   }
 }
-// The weights of queries and keys, [2][16] chunks (whole block).
+// The weights of queries and keys, [2][16] chunks, ones where there are none (whole block).
 __device__ __forceinline__ void load_weights(uint4 (&w)[32], const Args& A) {
   const int t = threadIdx.x;
   if (t < 32) {
     const __nv_bfloat16* p = t < 16 ? A.q_weight : A.k_weight;
-    if (p) w[t] = __ldg(reinterpret_cast<const uint4*>(p) + (t & 15));
+    w[t] = p ? __ldg(reinterpret_cast<const uint4*>(p) + (t & 15)) : make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
   }
   __syncthreads();
 }
 
-template <bool INTER>
-__device__ __forceinline__ void lane_angles(Lane& L, const Args& A, double position) {
+// Sines and cosines of a token's angles (whole warp).
+__device__ __forceinline__ void token_angles(WarpShared& W, const Args& A, double position, int lane) {
+  __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int chunk = INTER ? (j < 4 ? L.c0 : L.c1) : L.c0;
-    const int i = INTER ? chunk * 4 + (j & 3) : chunk * 8 + j;
-    const bool turn = INTER ? (j < 4 ? L.turn0 : L.turn1) : L.turn0;
-    if (turn) {
+  for (int x = 0; x < 2; ++x) {
+    const int i = lane + 32 * x;
+    if (i < A.rot / 2) {
       double turns = position * static_cast<double>(__ldg(A.inv_freq + i)) * 0.15915494309189533577;   // / (2 pi)
       turns -= rint(turns);
-      sincospif(static_cast<float>(2.0 * turns), &L.sn[j], &L.cs[j]);
-    } else {
-      L.cs[j] = 1.f;
-      L.sn[j] = 0.f;
+      sincospif(static_cast<float>(2.0 * turns), &W.sn[i], &W.cs[i]);
     }
   }
+  __syncwarp();
 }
-
-// One head row (its two chunks in a, b): norm (with the weights at w, if any) and rotation.
+// A lane's factors for rows with the weights at w.
 template <bool INTER>
-__device__ __forceinline__ void turn_row(const Lane& L, const uint4* w, float eps, uint4& a, uint4& b) {
-  float x0[8], x1[8];
-  unpack8(a, x0);
-  unpack8(b, x1);
-  float sum = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) sum = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], sum));
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (w) {
-    const float r = rsqrtf(sum * (1.f / kDim) + eps);
-    float f[8];
-    unpack8(w[L.c0], f);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x0[j] = x0[j] * r * f[j];
-    unpack8(w[L.c1], f);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x1[j] = x1[j] * r * f[j];
-  }
-  // (values that are not rotated stay as they are: a product with a sine of 0 would carry an infinity over)
+__device__ __forceinline__ void lane_factors(Lane& L, const WarpShared& W, const uint4* w) {
+  f32x2 w0[4], w1[4];
+  unpack8(w[L.c0], w0);
+  unpack8(w[L.c1], w1);
   if (INTER) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a0 = x0[2 * i], b0 = x0[2 * i + 1], a1 = x1[2 * i], b1 = x1[2 * i + 1];
-      if (L.turn0) { x0[2 * i] = a0 * L.cs[i] - b0 * L.sn[i]; x0[2 * i + 1] = b0 * L.cs[i] + a0 * L.sn[i]; }
-      if (L.turn1) { x1[2 * i] = a1 * L.cs[4 + i] - b1 * L.sn[4 + i]; x1[2 * i + 1] = b1 * L.cs[4 + i] + a1 * L.sn[4 + i]; }
+      const float c0 = L.turn0 ? W.cs[4 * L.c0 + i] : 1.f, s0 = L.turn0 ? W.sn[4 * L.c0 + i] : 0.f;
+      const float c1 = L.turn1 ? W.cs[4 * L.c1 + i] : 1.f, s1 = L.turn1 ? W.sn[4 * L.c1 + i] : 0.f;
+      L.a[i] = mul2(w0[i], pack2(c0, c0));
+      L.b[i] = mul2(swap2(w0[i]), pack2(-s0, s0));
+      L.a[4 + i] = mul2(w1[i], pack2(c1, c1));
+      L.b[4 + i] = mul2(swap2(w1[i]), pack2(-s1, s1));
     }
-  } else if (L.turn0) {
+  } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float p = x0[j], q = x1[j];
-      x0[j] = p * L.cs[j] - q * L.sn[j];
-      x1[j] = q * L.cs[j] + p * L.sn[j];
+    for (int i = 0; i < 4; ++i) {
+      const float2 c = L.turn0 ? *reinterpret_cast<const float2*>(W.cs + 8 * L.c0 + 2 * i) : make_float2(1.f, 1.f);
+      const float2 s = L.turn0 ? *reinterpret_cast<const float2*>(W.sn + 8 * L.c0 + 2 * i) : make_float2(0.f, 0.f);
+      L.a[i] = mul2(w0[i], pack2(c.x, c.y));
+      L.b[i] = mul2(w1[i], pack2(-s.x, -s.y));
+      L.a[4 + i] = mul2(w1[i], pack2(c.x, c.y));
+      L.b[4 + i] = mul2(w0[i], pack2(s.x, s.y));
     }
   }
-  a = pack8(x0);
-  b = pack8(x1);
 }
 
-// The heads part, part + split, ... (in units of four: one per lane group) of row `row`: queries, then keys, then values.
-// `kd` / `vd`: where the row's keys and values go (head h at + h * d_head); null: nowhere.
+// One head row (its two chunks in a, b).
 template <bool INTER>
-__device__ __forceinline__ void token_heads(const Lane& L, const Args& A, const uint4* weights, int64_t row, int part, int lane,
-                                            __nv_bfloat16* kd, __nv_bfloat16* vd, int64_t d_head) {
-  const int n_heads = A.hq + A.hk + A.hv;
-  const int step = 4 * A.split;
+__device__ __forceinline__ void turn_row(const Lane& L, bool norm, float eps, uint4& a, uint4& b) {
+  f32x2 x0[4], x1[4], y0[4], y1[4];
+  unpack8(a, x0);
+  unpack8(b, x1);
+  f32x2 r = pack2(1.f, 1.f);
+  if (norm) {
+    f32x2 sq = mul2(x0[0], x0[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) sq = fma2(x0[i], x0[i], sq);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sq = fma2(x1[i], x1[i], sq);
+    float s0, s1;
+    unpack2(sq, s0, s1);
+    float sum = s0 + s1;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float f = rsqrtf(sum * (1.f / kDim) + eps);
+    r = pack2(f, f);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y0[i] = mul2(x0[i], L.a[i]);
+    y1[i] = mul2(x1[i], L.a[4 + i]);
+  }
+  // (values that are not rotated stay as they are: a product with a sine of 0 would carry an infinity over)
+  if (L.turn0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y0[i] = fma2(INTER ? swap2(x0[i]) : x1[i], L.b[i], y0[i]);
+  }
+  if (L.turn1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y1[i] = fma2(INTER ? swap2(x1[i]) : x0[i], L.b[4 + i], y1[i]);
+  }
+  if (norm) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y0[i] = mul2(y0[i], r);
+      y1[i] = mul2(y1[i], r);
+    }
+  }
+  a = pack8(y0);
+  b = pack8(y1);
+}
+
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// The heads of the run's tokens that are this warp's: of every tensor those part, part + split, .. in units of four, a lane group
+// each.  Keys of head h go to kd + kv + h * d_head, values to vd + kv + h * d_head.  Copies run kStages - 1 head rows ahead of
+// their use, across tensors and tokens; a lane reads only what it copied itself, so no barrier is needed.
+template <bool INTER>
+__device__ __forceinline__ void run_heads(const Args& A, const uint4* weights, WarpShared& W, uint4* ring, const Token& mine, int n_tok,
+                                          int part, int lane, __nv_bfloat16* kd, __nv_bfloat16* vd, int64_t d_head) {
+  Lane L;
+  lane_setup<INTER>(L, A, lane & 7);
+  const int step = 4 * A.split, h0 = 4 * part + (lane >> 3);
+  auto rounds = [&](int n) { return n > 4 * part ? (n - 4 * part + step - 1) / step : 0; };
+  const int q_rounds = rounds(A.hq), k_rounds = rounds(A.hk), v_rounds = rounds(A.hv);
+  ring += lane;
+  const uint32_t ring_at = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+
+  // the next copy
+  int pt = -1, pwhich = 2, pleft = 0, ph = 0, pn = 0, ps = 0;
+  const __nv_bfloat16* pp = nullptr;
+  int64_t pstep = 0;
+  auto ahead = [&]() {
+    while (pleft == 0 && pt < n_tok) {                                            // (warp-uniform: the next tensor, the next token)
+      if (++pwhich == 3) { pwhich = 0; ++pt; }
+      if (pt == n_tok) break;
+      const int64_t row = __shfl_sync(0xffffffffu, mine.row, pt), kv = __shfl_sync(0xffffffffu, mine.kv, pt);
+      if (row < 0 || (pwhich && kv < 0)) continue;
+      const Tensor& T = pwhich == 0 ? A.q : pwhich == 1 ? A.k : A.v;
+      pn = pwhich == 0 ? A.hq : pwhich == 1 ? A.hk : A.hv;
+      pleft = pwhich == 0 ? q_rounds : pwhich == 1 ? k_rounds : v_rounds;
+      ph = h0;
+      pp = T.p + row * T.row + h0 * T.head + 8 * L.c0;
+      pstep = step * T.head;
+    }
+    if (pleft > 0) {
+      if (ph < pn) {
+        copy_16(ring_at + ps * 1024, pp);
+        copy_16(ring_at + ps * 1024 + 512, pp + 8 * (L.c1 - L.c0));
+      }
+      ph += step;
+      pp += pstep;
+      --pleft;
+      ps = ps + 1 == kStages ? 0 : ps + 1;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int cs = 0;
+  auto through = [&](auto turn, __nv_bfloat16* dst, int64_t dst_step, int n, int rounds_here, bool norm) {
+    dst += 8 * L.c0;
+    int h = h0;
 #pragma unroll 1
-  for (int h0 = 4 * part; h0 < n_heads; h0 += step * kAhead) {                    // (warp-uniform)
-    uint4 a[kAhead], b[kAhead];
-    __nv_bfloat16* dst[kAhead];
-#pragma unroll
-    for (int x = 0; x < kAhead; ++x) {
-      const int h = h0 + x * step + (lane >> 3);
-      const __nv_bfloat16* src = nullptr;
-      dst[x] = nullptr;
-      if (h < A.hq) {
-        src = A.q.p + row * A.q.row + h * A.q.head;
-        dst[x] = A.q_out.p + row * A.q_out.row + h * A.q_out.head;
-      } else if (h < A.hq + A.hk) {
-        src = A.k.p + row * A.k.row + (h - A.hq) * A.k.head;
-        if (kd) dst[x] = kd + (h - A.hq) * d_head;
-      } else if (h < n_heads) {
-        src = A.v.p + row * A.v.row + (h - A.hq - A.hk) * A.v.head;
-        if (vd) dst[x] = vd + (h - A.hq - A.hk) * d_head;
+    for (int g = 0; g < rounds_here; ++g) {
+      ahead();
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      uint4 a = ring[cs * 64], b = ring[cs * 64 + 32];
+      cs = cs + 1 == kStages ? 0 : cs + 1;
+      if (decltype(turn)::value) turn_row<INTER>(L, norm, A.eps, a, b);
+      if (h < n) {
+        *reinterpret_cast<uint4*>(dst) = a;
+        *reinterpret_cast<uint4*>(dst + 8 * (L.c1 - L.c0)) = b;
       }
-      a[x] = b[x] = make_uint4(0, 0, 0, 0);
-      if (dst[x]) {
-        a[x] = *(reinterpret_cast<const uint4*>(src) + L.c0);                     // (not __ldg: q_out may be q)
-        b[x] = *(reinterpret_cast<const uint4*>(src) + L.c1);
-      }
+      dst += dst_step;
+      h += step;
     }
-#pragma unroll
-    for (int x = 0; x < kAhead; ++x) {
-      const int h1 = h0 + x * step, h = h1 + (lane >> 3);
-      if (h1 >= n_heads) break;                                                   // (warp-uniform, as the next)
-      if (h1 < A.hq + A.hk) {
-        const bool is_q = h < A.hq;
-        const uint4* w = is_q ? (A.q_weight ? weights : nullptr) : (A.k_weight ? weights + 16 : nullptr);
-        uint4 y0 = a[x], y1 = b[x];
-        turn_row<INTER>(L, w, A.eps, y0, y1);
-        if (h < A.hq + A.hk) { a[x] = y0; b[x] = y1; }
-      }
-      if (dst[x]) {
-        *(reinterpret_cast<uint4*>(dst[x]) + L.c0) = a[x];
-        *(reinterpret_cast<uint4*>(dst[x]) + L.c1) = b[x];
-      }
+  };
+#pragma unroll 1
+  for (int x = 0; x < kStages - 1; ++x) ahead();
+#pragma unroll 1
+  for (int t = 0; t < n_tok; ++t) {
+    const int64_t row = __shfl_sync(0xffffffffu, mine.row, t), kv = __shfl_sync(0xffffffffu, mine.kv, t);
+    const double position = __shfl_sync(0xffffffffu, mine.position, t);
+    if (row < 0) continue;                                                        // (warp-uniform)
+    if (q_rounds | k_rounds) token_angles(W, A, position, lane);
+    if (q_rounds) {
+      lane_factors<INTER>(L, W, weights);
+      through(Yes(), A.q_out.p + row * A.q_out.row + h0 * A.q_out.head, step * A.q_out.head, A.hq, q_rounds, A.q_weight != nullptr);
     }
+    if (kv < 0) continue;
+    if (k_rounds) {
+      lane_factors<INTER>(L, W, weights + 16);
+      through(Yes(), kd + kv + h0 * d_head, step * d_head, A.hk, k_rounds, A.k_weight != nullptr);
+    }
+    if (v_rounds) through(No(), vd + kv + h0 * d_head, step * d_head, A.hv, v_rounds, false);
   }
 }
 
 template <bool INTER>
 __global__ void __launch_bounds__(kWarps * 32, kBlocks) norm_rope_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
+  extern __shared__ uint4 ring[];
   __shared__ uint4 weights[32];
+  __shared__ WarpShared W[kWarps];
   load_weights(weights, A);
-  const int lane = threadIdx.x & 31;
-  const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps;
-  Lane L;
-  lane_setup<INTER>(L, A, lane & 7);
-  for (int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); w < A.n_rows * A.split; w += warps) {
-    const int64_t row = w / A.split;
-    lane_angles<INTER>(L, A, A.positions ? static_cast<double>(__ldg(A.positions + row)) : 0.0);
-    token_heads<INTER>(L, A, weights, row, static_cast<int>(w - row * A.split), lane,
-                       A.k_out.p ? A.k_out.p + row * A.k_out.row : nullptr, nullptr, A.k_out.head);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + warp, r0 = w / A.split * A.run;
+  const int n_tok = static_cast<int>(min(static_cast<int64_t>(A.run), A.n_rows - r0));
+  if (n_tok <= 0) return;
+  Token mine{-1, 0, 0.0};
+  if (lane < n_tok) {
+    mine.row = r0 + lane;
+    mine.kv = mine.row * A.k_out.row;
+    if (A.positions) mine.position = static_cast<double>(__ldg(A.positions + mine.row));
   }
+  run_heads<INTER>(A, weights, W[warp], ring + warp * (kStages * 64), mine, n_tok, static_cast<int>(w % A.split), lane, A.k_out.p, nullptr, A.k_out.head);
 }
 
 // Number of offsets[0 .. n] that are <= r, less one: the path of row r (whole warp; 32 probes a round).
@@ -230,66 +322,54 @@ __device__ __forceinline__ int path_of(const int64_t* offsets, int n, int64_t r,
   return lo;
 }
 
-// A warp takes `run` tokens in a row (of a part of their heads): it looks for the first one's path, the others follow it.
 template <bool INTER>
 __global__ void __launch_bounds__(kWarps * 32, kBlocks) append_kernel(const __grid_constant__ Args A, const __grid_constant__ Place P) {
   ss::grid_dependency_enter();
+  extern __shared__ uint4 ring[];
   __shared__ uint4 weights[32];
+  __shared__ WarpShared W[kWarps];
   load_weights(weights, A);
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int live = P.num_paths_dev ? min(max(__ldg(P.num_paths_dev), 0), P.num_paths) : P.num_paths;
   if (live == 0) return;
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  const int64_t first_row = __ldg(P.q_offsets), rows = min(__ldg(P.q_offsets + live) - first_row, P.total_q);
-  int64_t r = first_row + w / A.split * P.run;
-  const int part = static_cast<int>(w % A.split);
-  const int64_t r_end = min(r + P.run, first_row + rows);
-  if (r >= r_end) return;
-  Lane L;
-  lane_setup<INTER>(L, A, lane & 7);
-  int p = path_of(P.q_offsets, live, r, lane);
-  while (r < r_end) {
-    const int64_t q0 = __ldg(P.q_offsets + p), q1 = __ldg(P.q_offsets + p + 1);
+  const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
+  const int64_t first = __ldg(P.q_offsets), rows = min(__ldg(P.q_offsets + live) - first, P.total_q);
+  const int64_t r0 = w / A.split * A.run;
+  const int n_tok = static_cast<int>(min(static_cast<int64_t>(A.run), rows - r0));
+  if (n_tok <= 0) return;
+  // the first token's path by the whole warp, the others' from there on
+  int p = path_of(P.q_offsets, live, first + r0, lane);
+  Token mine{-1, -1, 0.0};
+  if (lane < n_tok) {
+    const int64_t r = first + r0 + lane;
+    while (p + 1 < live && __ldg(P.q_offsets + p + 1) <= r) ++p;
+    const int64_t q0 = __ldg(P.q_offsets + p), t = r - q0, row = (P.q_src_offsets ? __ldg(P.q_src_offsets + p) : q0) + t;
     const int leaf = __ldg(P.path_leaf_node + p), T = __ldg(P.path_q_len + p);
-    const int64_t src0 = P.q_src_offsets ? __ldg(P.q_src_offsets + p) : q0;
-    ++p;
-    if (r >= q1) {
-      if (p == live) break;
-      continue;
-    }
-    const int64_t stop = min(r_end, q1);
-    if (leaf < 0 || leaf >= P.num_nodes) { r = stop; if (p == live) break; continue; }
-    const int len = __ldg(P.node_kv_len + leaf);
-    const int64_t page0 = __ldg(P.node_page_offsets + leaf), page1 = __ldg(P.node_page_offsets + leaf + 1);
-    int64_t before = 0;                                        // tokens in front of the leaf
-    if (!A.positions && A.rot) {
-      int a = __ldg(P.node_parent + leaf);
-      for (int d = 1; d < SS_MAX_DEPTH && a >= 0 && a < P.num_nodes; ++d) {
-        before += __ldg(P.node_kv_len + a);
-        a = __ldg(P.node_parent + a);
-      }
-    }
-    for (; r < stop; ++r) {
-      const int64_t t = r - q0, row = src0 + t;
-      if (t >= T || row < 0 || row >= A.n_rows) continue;
-      const int at = len - T + static_cast<int>(t);            // token of the leaf
-      __nv_bfloat16 *kd = nullptr, *vd = nullptr;
+    if (leaf >= 0 && leaf < P.num_nodes && t < T && row >= 0 && row < A.n_rows) {
+      const int at = __ldg(P.node_kv_len + leaf) - T + static_cast<int>(t);       // token of the leaf
+      mine.row = row;
       if (at >= 0) {
-        const int64_t entry = page0 + at / kPage;
-        if (entry >= 0 && entry < page1 && entry < P.total_node_pages) {
+        const int64_t entry = __ldg(P.node_page_offsets + leaf) + at / kPage;
+        if (entry >= 0 && entry < __ldg(P.node_page_offsets + leaf + 1) && entry < P.total_node_pages) {
           const int64_t page = __ldg(P.node_pages + entry);
-          if (page >= 0 && page < P.num_pages) {
-            const int64_t off = page * P.page_stride + static_cast<int64_t>(at % kPage) * kDim;
-            kd = P.k_pool + off;
-            vd = P.v_pool + off;
-          }
+          if (page >= 0 && page < P.num_pages) mine.kv = page * P.page_stride + static_cast<int64_t>(at % kPage) * kDim;
         }
       }
-      lane_angles<INTER>(L, A, A.positions ? static_cast<double>(__ldg(A.positions + row)) : static_cast<double>(before + at));
-      token_heads<INTER>(L, A, weights, row, part, lane, kd, vd, P.head_stride);
+      int64_t position = at;
+      if (A.positions) {
+        position = __ldg(A.positions + row);
+      } else if (A.rot) {
+        int a = __ldg(P.node_parent + leaf);
+        for (int d = 1; d < SS_MAX_DEPTH && a >= 0 && a < P.num_nodes; ++d) {
+          position += __ldg(P.node_kv_len + a);
+          a = __ldg(P.node_parent + a);
+        }
+      }
+      mine.position = static_cast<double>(position);
     }
-    if (p == live) break;
   }
+  __syncwarp();
+  run_heads<INTER>(A, weights, W[warp], ring + warp * (kStages * 64), mine, n_tok, static_cast<int>(w % A.split), lane, P.k_pool, P.v_pool, P.head_stride);
 }
 
 // Checks what both calls share and fills the kernel's arguments.
@@ -307,7 +387,7 @@ static int32_t rows_args(const ss_rows_t* r, Args* A) {
   const uintptr_t addresses = reinterpret_cast<uintptr_t>(r->q) | reinterpret_cast<uintptr_t>(r->k) | reinterpret_cast<uintptr_t>(r->v) |
                               reinterpret_cast<uintptr_t>(r->q_out) | reinterpret_cast<uintptr_t>(r->k_out) |
                               reinterpret_cast<uintptr_t>(r->q_weight) | reinterpret_cast<uintptr_t>(r->k_weight);
-  if (strides % 8 || addresses % 16) return SS_ERR_UNSUPPORTED;
+  if (strides % 8 || strides < 0 || addresses % 16) return SS_ERR_UNSUPPORTED;   // (< 0: one of them is)
   const auto bf16 = [](const void* p) { return static_cast<const __nv_bfloat16*>(p); };
   A->q = {bf16(r->q), r->q_row_stride, r->q_head_stride};
   A->k = {bf16(r->k), r->k_row_stride, r->k_head_stride};
@@ -335,9 +415,43 @@ static int heads_split(int64_t tokens, int heads) {
   const int64_t split = tokens > 0 ? ceil_div64(want, tokens) : 1;
   return static_cast<int>(split < 1 ? 1 : split > most ? most : split);
 }
-static unsigned grid_of(int64_t warps) {
-  const int64_t blocks = ceil_div64(warps, kWarps), most = static_cast<int64_t>(sm_count_of_current_device()) * 64;
-  return static_cast<unsigned>(blocks < 1 ? 1 : blocks > most ? most : blocks);
+// Tokens of a warp's run: one, until there are enough of them to go round all resident warps four times.
+static int run_of(int64_t tokens, int split) {
+  const int64_t run = tokens * split / (static_cast<int64_t>(sm_count_of_current_device()) * kBlocks * kWarps * 4);
+  return static_cast<int>(run < 1 ? 1 : run > kMostRun ? kMostRun : run);
+}
+template <typename Kernel>
+static int32_t prepare(Kernel kernel, bool (&done)[kDeviceSlots]) {
+  const int slot = current_device_slot();
+  if (slot >= 0 && done[slot]) return SS_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SS_ERR_CUDA;
+  }
+  if (slot >= 0) done[slot] = true;
+  return SS_OK;
+}
+template <bool INTER>
+static int32_t launch_norm_rope(const Args& A, unsigned grid, cudaStream_t st) {
+  static bool done[kDeviceSlots] = {false};
+  const int32_t rc = prepare(norm_rope_kernel<INTER>, done);
+  if (rc != SS_OK) return rc;
+  SS_LAUNCH(norm_rope_kernel<INTER>, grid, kWarps * 32, kSmem, st, A);
+  return SS_OK;
+}
+template <bool INTER>
+static int32_t launch_append(const Args& A, const Place& P, unsigned grid, cudaStream_t st) {
+  static bool done[kDeviceSlots] = {false};
+  const int32_t rc = prepare(append_kernel<INTER>, done);
+  if (rc != SS_OK) return rc;
+  SS_LAUNCH(append_kernel<INTER>, grid, kWarps * 32, kSmem, st, A, P);
+  return SS_OK;
+}
+static int32_t grid_of(int64_t tokens, const Args& A, unsigned* grid) {
+  const int64_t blocks = ceil_div64(ceil_div64(tokens, A.run) * A.split, kWarps);
+  if (blocks > 0x7fffffffLL) return SS_ERR_UNSUPPORTED;
+  *grid = static_cast<unsigned>(blocks);
+  return SS_OK;
 }
 
 }  // namespace rows
@@ -350,13 +464,12 @@ extern "C" int32_t ss_qk_norm_rope(const ss_rows_t* rows, void* stream) {
   if (rc != SS_OK || rows->n_rows == 0) return rc;
   if ((!rows->q && !rows->k) || (rows->k != nullptr) != (rows->k_out != nullptr) || (rows->rot_dim && !rows->positions)) return SS_ERR_INVALID_ARG;
   A.split = heads_split(rows->n_rows, A.hq + A.hk);
-  const unsigned grid = grid_of(rows->n_rows * A.split);
-  if (rows->flags & SS_ROWS_INTERLEAVED) {
-    SS_LAUNCH(norm_rope_kernel<true>, grid, kWarps * 32, 0, ss::as_stream(stream), A);
-  } else {
-    SS_LAUNCH(norm_rope_kernel<false>, grid, kWarps * 32, 0, ss::as_stream(stream), A);
-  }
-  return SS_OK;
+  A.run = run_of(rows->n_rows, A.split);
+  unsigned grid = 0;
+  const int32_t gc = grid_of(rows->n_rows, A, &grid);
+  if (gc != SS_OK) return gc;
+  return rows->flags & SS_ROWS_INTERLEAVED ? launch_norm_rope<true>(A, grid, ss::as_stream(stream))
+                                           : launch_norm_rope<false>(A, grid, ss::as_stream(stream));
 }
 
 extern "C" int32_t ss_kv_append(const ss_attn_desc_t* d, const ss_rows_t* rows, void* stream) {
@@ -398,18 +511,10 @@ extern "C" int32_t ss_kv_append(const ss_attn_desc_t* d, const ss_rows_t* rows, 
   P.num_paths = d->num_paths;
   P.total_q = d->total_q;
   A.split = heads_split(d->total_q, A.hq + A.hk + A.hv);
-  // Tokens of a step lie side by side in their pages: a warp takes up to four in a row once there are enough of them for all warps
-  // four times over.
-  const int64_t resident = static_cast<int64_t>(ss::sm_count_of_current_device()) * kBlocks * kWarps;
-  const int64_t run = d->total_q * A.split / (resident * 4);
-  P.run = static_cast<int>(run < 1 ? 1 : run > 4 ? 4 : run);
-  const int64_t blocks = ss::ceil_div64(ss::ceil_div64(d->total_q, P.run) * A.split, kWarps);
-  if (blocks > 0x7fffffffLL) return SS_ERR_UNSUPPORTED;
-  const unsigned grid = static_cast<unsigned>(blocks);
-  if (rows->flags & SS_ROWS_INTERLEAVED) {
-    SS_LAUNCH(append_kernel<true>, grid, kWarps * 32, 0, ss::as_stream(stream), A, P);
-  } else {
-    SS_LAUNCH(append_kernel<false>, grid, kWarps * 32, 0, ss::as_stream(stream), A, P);
-  }
-  return SS_OK;
+  A.run = run_of(d->total_q, A.split);
+  unsigned grid = 0;
+  const int32_t gc = grid_of(d->total_q, A, &grid);
+  if (gc != SS_OK) return gc;
+  return rows->flags & SS_ROWS_INTERLEAVED ? launch_append<true>(A, P, grid, ss::as_stream(stream))
+                                           : launch_append<false>(A, P, grid, ss::as_stream(stream));
 }
