@@ -407,17 +407,16 @@ static int32_t rows_args(const ss_rows_t* r, Args* A) {
   return SS_OK;
 }
 
-// Warps that share a token: as many as it takes to occupy the machine, at most one for four heads.  A token on one warp makes its
-// angles once.
+static int64_t resident_warps() { return static_cast<int64_t>(sm_count_of_current_device()) * kBlocks * kWarps; }
+// Warps that share a token: as many as are resident at once, at most one for four heads.  A token on one warp makes its angles once.
 static int heads_split(int64_t tokens, int heads) {
-  const int64_t want = static_cast<int64_t>(sm_count_of_current_device()) * 16;
   const int most = ceil_div(heads, 4);
-  const int64_t split = tokens > 0 ? ceil_div64(want, tokens) : 1;
+  const int64_t split = tokens > 0 ? resident_warps() / tokens : 1;
   return static_cast<int>(split < 1 ? 1 : split > most ? most : split);
 }
-// Tokens of a warp's run: one, until there are enough of them to go round all resident warps four times.
+// Tokens of a warp's run: all warps resident at once as long as a run has no more than kMostRun, which then go in several waves.
 static int run_of(int64_t tokens, int split) {
-  const int64_t run = tokens * split / (static_cast<int64_t>(sm_count_of_current_device()) * kBlocks * kWarps * 4);
+  const int64_t run = ceil_div64(tokens * split, resident_warps());
   return static_cast<int>(run < 1 ? 1 : run > kMostRun ? kMostRun : run);
 }
 template <typename Kernel>
