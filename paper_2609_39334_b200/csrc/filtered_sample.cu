@@ -5,12 +5,16 @@
 // counting, top-p one by adding up probabilities, min-p one by a bound on the logit; the least of the three holds.  A draw then
 // goes by the running sum over the kept tokens in index order.  Logits are compared as order-preserving integers (bf16 ones are
 // widened: exact); probabilities are fp64 relative to the row's maximum.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include "common.cuh"
+#include "quick_exp2.cuh"
 
 namespace ss {
 namespace filtered {
+
+namespace cg = cooperative_groups;
 
 constexpr int kMaxVocab = 2097152;
 constexpr int kThreads = 1024, kWarps = kThreads / 32;         // of a block that goes through whole rows
@@ -30,6 +34,8 @@ struct Args {
   float temperature_all, top_p_all, min_p_all;
   int top_k_all;
   int n_seq, vocab;
+  int row0;                                    // first row of this launch
+  int32_t* marks;                              // [n_seq]: rows that the list is not enough for
 };
 struct RowParams {
   float temperature, top_p, min_p;
@@ -417,9 +423,495 @@ __global__ void __launch_bounds__(kThreads) whole_rows_kernel(const __grid_const
   ss::grid_dependency_enter();
   __shared__ WholeShared S;
   for (int s = blockIdx.x; s < A.n_seq; s += gridDim.x) {
+    if (A.marks[s] == 0) continue;
     whole_row<HALF>(A, S, s);
     __syncthreads();
   }
+}
+
+// ---- most rows: one pass over the row, the rest on a short list --------------------------------------------------------------------
+// What is kept is nearly always among the few largest logits, so one pass collects those above a THRESHOLD in shared memory (the
+// list) and, where top-p is over the whole row, adds up all terms in fp32 with a proven bound (quick_exp2.cuh).  The threshold comes from a
+// sample spread over the row: of the maxima of 64 groups of n sampled tokens a share e^(-n f) lies below the value that a share f of
+// the row exceeds.  Nothing rests on it: a border found on the list is the row's if it does not lie below the threshold, and where
+// the list is too short or too long, or a sum comes too close to top-p's target to tell, the row is marked and made again by the
+// kernel behind this one.  (Short rows are on the list as a whole.)
+// On the list: borders by histograms of 512 bins over the range of keys that is left, counts or terms in 64-bit fixed point (any
+// order, the same sums), three rounds for a range of 2^24 keys; the kept ones sorted by index; their running sum in fp64; a thread per draw.
+// Two blocks an SM, so that one is in its pass while the other is on its list.
+constexpr int kListThreads = 512, kListWarps = kListThreads / 32;
+constexpr int kCap = 8192;                                     // entries of a list
+constexpr int kBins = 512;
+constexpr int kGroups = 64;                                    // of sampled tokens: 8 lanes each
+constexpr double kFix = 1125899906842624.0;                    // 2^50: kCap terms of at most 1 stay below 2^63
+constexpr double kFixError = 1e-11;                            // kCap * 2^-51 of the largest term, and the sums' own roundings
+constexpr double kSumError = 4e-7;                             // of the quick sum of a row, kQuickError and what is added to it
+constexpr float kLowest = -3.4028235e38f;
+
+struct ListShared {
+  unsigned long long list[kCap];                               // key, token; then token, key; then running sums
+  uint32_t token[kCap];
+  unsigned long long mass[kBins];
+  unsigned count[kBins];
+  double d[kListWarps];
+  float f[kListWarps];
+  float group[kGroups];
+  float low;                                                   // threshold
+  unsigned n;                                                  // entries offered to the list
+  unsigned bin, moved;
+  unsigned long long above, in_bin;
+  // for the cluster's first block
+  double z;
+  float max, base;
+};
+
+struct Found {                                                 // where a running count or sum over falling keys reaches its target
+  bool there;
+  uint32_t key;
+  unsigned long long above, at_key;                            // over the larger keys, over this one
+};
+// `entry(i)`: key of list entry i and whether it counts; `weight(key)`: what it counts for.  Whole block; keys of [lo, hi].
+template <bool MASS, typename Entry, typename Weight>
+__device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo, uint32_t hi, unsigned long long target, Entry entry, Weight weight) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  unsigned long long above = 0;
+  for (;;) {
+    const uint32_t range = hi - lo;
+    const int shift = range < kBins ? 0 : 32 - __clz(range) - 9;
+    __syncthreads();
+    for (int b = tid; b < kBins; b += kListThreads) { S.count[b] = 0; S.mass[b] = 0; }
+    __syncthreads();
+    for (int i = tid; i < n; i += kListThreads) {
+      uint32_t k;
+      if (entry(i, k) && k >= lo && k <= hi) {
+        const uint32_t b = (k - lo) >> shift;
+        if (MASS) atomicAdd(&S.mass[b], weight(k));
+        else atomicAdd(&S.count[b], 1u);
+      }
+    }
+    __syncthreads();
+    if (tid < 32) {                                            // 16 bins a lane, from the top
+      unsigned long long sum = 0;
+#pragma unroll
+      for (int x = 0; x < kBins / 32; ++x) {
+        const int b = kBins - 1 - (lane * (kBins / 32) + x);
+        sum += MASS ? S.mass[b] : static_cast<unsigned long long>(S.count[b]);
+      }
+      unsigned long long incl = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      const unsigned over = __ballot_sync(0xffffffffu, above + incl >= target);
+      if (over == 0) {
+        if (lane == 31) { S.bin = kBins; S.above = above + incl; }
+      } else if (lane == __ffs(over) - 1) {
+        unsigned long long run = above + incl - sum;
+        for (int x = 0; x < kBins / 32; ++x) {
+          const int b = kBins - 1 - (lane * (kBins / 32) + x);
+          const unsigned long long here = MASS ? S.mass[b] : static_cast<unsigned long long>(S.count[b]);
+          if (run + here >= target) { S.bin = b; S.in_bin = here; break; }
+          run += here;
+        }
+        S.above = run;
+      }
+    }
+    __syncthreads();
+    above = S.above;
+    if (S.bin == kBins) return Found{false, lo, above, 0};
+    lo += S.bin << shift;
+    if (shift == 0) return Found{true, lo, above, S.in_bin};
+    hi = min(hi, lo + ((1u << shift) - 1u));
+  }
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// Logits of one 16-byte vector.
+template <bool HALF>
+__device__ __forceinline__ void unpack(const uint4& u, float* x) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (HALF) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+      x[i] = __uint_as_float(w[i]);
+    }
+  }
+}
+
+template <bool HALF, int CL>
+__device__ void list_row(const Args& A, ListShared& S, int s) {
+  constexpr int kVec = HALF ? 8 : 4;                           // tokens of a vector
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = A.vocab;
+  cg::cluster_group cl = cg::this_cluster();
+  const int rank = CL > 1 ? static_cast<int>(cl.block_rank()) : 0;
+  const int64_t d0 = __ldg(A.draw_offsets + s), d1 = __ldg(A.draw_offsets + s + 1);
+  if (d1 <= d0 && !A.kept_out) {
+    if (tid == 0 && rank == 0) A.marks[s] = 0;
+    return;
+  }
+  const void* row = row_of<HALF>(A, s);
+  const RowParams R = row_params(A, s);
+  const bool fine = R.temperature >= 0.f && R.temperature < INFINITY;
+  const bool greedy = R.temperature == 0.f || R.top_k == 1 || R.top_p <= 0.f;
+  const bool by_k = R.top_k > 0 && R.top_k < V;
+  // this block's slice, from 16-byte boundary to 16-byte boundary but for the row's ends
+  const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16) / (HALF ? 2 : 4);
+  const int lead = skew ? min(kVec - skew, V) : 0;             // tokens in front of the first whole vector
+  const int n_vec = (V - lead) / kVec, per = (n_vec + CL - 1) / CL;
+  const int vec0 = min(rank * per, n_vec), vec1 = min(vec0 + per, n_vec);
+  const uint4* vecs = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + lead * (HALF ? 2 : 4));
+  const int here = (vec1 - vec0) * kVec;
+  const bool whole = V <= kCap;                                // every finite logit goes on the list
+  const bool add_up = fine && !greedy && !whole && !by_k && R.top_p < 1.f;
+  // ---- threshold
+  if (tid == 0) { S.n = 0; S.low = kLowest; }
+  if (!whole) {
+    float m = -INFINITY;
+    if (here > 0) {
+      float x[kVec];
+      unpack<HALF>(__ldg(vecs + vec0 + static_cast<int>(static_cast<int64_t>(tid) * (vec1 - vec0) / kListThreads)), x);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) m = fmaxf(m, x[i]);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((lane & 7) == 0) S.group[tid >> 3] = m;
+  }
+  __syncthreads();
+  if (!whole && warp == 0) {
+    // (a list for the cluster's first block has to take them all)
+    const float want = fmaxf(2048.f, fminf(4096.f, 2.f * static_cast<float>(by_k ? R.top_k : 0))) / CL;
+    const float share = fminf(want / static_cast<float>(max(here, 1)), 1.f);
+    const int at = min(static_cast<int>(kGroups * __expf(-8.f * kVec * share)), kGroups - 1);
+#pragma unroll
+    for (int x = 0; x < kGroups; x += 32) {
+      const float m = S.group[lane + x];
+      int below = 0;
+      for (int i = 0; i < kGroups; ++i) {
+        const float o = S.group[i];
+        below += o < m || (o == m && i < lane + x) ? 1 : 0;
+      }
+      if (below == at && m > kLowest) S.low = m;
+    }
+  }
+  __syncthreads();
+  const float low = S.low;
+  float base = 0.f, c_hi = 0.f, c_lo = 0.f;
+  double c = 0.0;
+  if (add_up) {
+    c = 1.4426950408889634 / static_cast<double>(R.temperature);
+    c_hi = static_cast<float>(c);
+    c_lo = static_cast<float>(c - static_cast<double>(c_hi));
+    float top = S.group[lane];
+    top = warp_max(fmaxf(top, S.group[lane + 32]));
+    base = rintf(fminf(fmaxf(top * c_hi, -1e6f), 1e6f));       // (the same in all lanes)
+  }
+  const QuickBase quick = quick_base(base, c_hi);
+
+  // ---- the pass
+  float mx = -INFINITY;
+  double z = 0.0;
+  auto offer = [&](float x, int v) {                           // (a NaN is not taken)
+    const unsigned at = atomicAdd(&S.n, 1u);
+    if (at < kCap) S.list[at] = (static_cast<unsigned long long>(key_of(x)) << 32) | static_cast<uint32_t>(v);
+  };
+  auto single = [&](int v) {
+    const float x = load_logit<HALF>(row, v);
+    mx = max_nan(mx, x);
+    if (x >= low) offer(x, v);
+    if (add_up) {
+      float a, b;
+      unpack2(quick_pair(x, -INFINITY, quick, c_hi, c_lo), a, b);
+      z += static_cast<double>(a);
+    }
+  };
+  if (rank == 0 && tid < lead) single(tid);
+  if (rank == CL - 1 && tid < V - lead - n_vec * kVec) single(lead + n_vec * kVec + tid);
+  constexpr int kVecs = HALF ? 2 : 4;                          // vectors of a lane at a time: 16 tokens
+  for (int v0 = vec0 + warp * (32 * kVecs); v0 < vec1; v0 += kListWarps * 32 * kVecs) {
+    uint4 u[kVecs];
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      const int at = v0 + j * 32 + lane;
+      u[j] = at < vec1 ? __ldg(vecs + at) : HALF ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
+                                                 : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+    }
+    float x[16];
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) unpack<HALF>(u[j], x + j * kVec);
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = max_nan(top, x[i]);
+    mx = max_nan(mx, top);
+    if (!(top < low)) {                                        // (a NaN hides what else is there, but no row that holds one is kept)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (x[i] >= low) offer(x[i], lead + (v0 + (i / kVec) * 32 + lane) * kVec + i % kVec);
+    }
+    if (add_up) {
+#pragma unroll
+      for (int h = 0; h < 16; h += 8) {
+        const f32x2 t = add2(add2(quick_pair(x[h], x[h + 1], quick, c_hi, c_lo), quick_pair(x[h + 2], x[h + 3], quick, c_hi, c_lo)),
+                             add2(quick_pair(x[h + 4], x[h + 5], quick, c_hi, c_lo), quick_pair(x[h + 6], x[h + 7], quick, c_hi, c_lo)));
+        float a, b;
+        unpack2(t, a, b);
+        z += static_cast<double>(a + b);
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  z = warp_sum_d(z);
+  if (lane == 0) { S.f[warp] = mx; S.d[warp] = z; }
+  __syncthreads();
+  mx = S.f[0];
+  z = S.d[0];
+#pragma unroll
+  for (int w = 1; w < kListWarps; ++w) { mx = max_nan(mx, S.f[w]); z += S.d[w]; }
+  if (add_up && !(mx * c_hi <= base + 100.f)) z = NAN;         // (terms out of range: the sample was far off)
+  unsigned n = S.n;
+  bool fits = n <= kCap;
+  uint32_t low_key = whole ? kNegInf + 1 : key_of(low);
+  if (CL > 1) {                                                // to the first block, in the order of the blocks
+    if (tid == 0) { S.z = z; S.max = mx; S.base = base; }
+    cl.sync();
+    if (rank == 0) {
+      for (int b = 1; b < CL; ++b) {
+        ListShared* o = cl.map_shared_rank(&S, b);
+        const unsigned m = o->n;
+        if (add_up) z += o->z * exp2(static_cast<double>(o->base) - static_cast<double>(base));
+        mx = max_nan(mx, o->max);
+        if (!whole) low_key = max(low_key, key_of(o->low));
+        fits = fits && m <= kCap && n + m <= kCap;
+        if (fits)
+          for (unsigned i = tid; i < m; i += kListThreads) S.list[n + i] = o->list[i];
+        n += m;
+      }
+    }
+    cl.sync();
+    if (rank) return;
+    __syncthreads();
+  }
+
+  // ---- the border
+  auto give_all = [&](int token, int kept) {
+    for (int64_t d = d0 + tid; d < d1; d += kListThreads) {
+      A.tokens_out[d] = token;
+      if (A.seq_out) A.seq_out[d] = s;
+    }
+    if (tid == 0) {
+      if (A.kept_out) A.kept_out[s] = kept;
+      A.marks[s] = 0;
+    }
+  };
+  if (!fine || !(mx < INFINITY) || mx == -INFINITY) {          // (a NaN is not less)
+    give_all(-1, 0);
+    return;
+  }
+  const uint32_t max_key = key_of(mx);
+  bool sure = fits;
+  Border border{kNegInf, 0};
+  bool known = false;
+  auto take = [&](const Border& b) {
+    if (!known || less(b, border)) border = b;
+    known = true;
+  };
+  const int m_list = static_cast<int>(n);
+  auto by_key = [&](int i, uint32_t& k) { k = static_cast<uint32_t>(S.list[i] >> 32); return true; };
+  Term e;
+  e.max = static_cast<double>(mx);
+  e.inv_t = greedy ? 1.0 : 1.0 / static_cast<double>(R.temperature);
+  auto fixed = [&](uint32_t k) { return __double2ull_rn(e(logit_of(k)) * kFix); };
+  auto one = [](uint32_t) { return 1ull; };
+  if (greedy) {
+    take(Border{max_key, 1});
+  } else if (sure) {
+    const bool limit = by_k && !(whole && R.top_k >= m_list);  // top-k leaves something out
+    bool k_known = !limit;
+    Border by_count{low_key, 0x7fffffff};
+    if (limit) {
+      const Found f = find_on_list<false>(S, m_list, low_key, max_key, static_cast<unsigned long long>(R.top_k), by_key, one);
+      if (f.there) {
+        by_count = Border{f.key, static_cast<int>(R.top_k - f.above)};
+        take(by_count);
+        k_known = true;
+      }
+    }
+    const uint32_t size_key = min_p_key(e, R.temperature, R.min_p, max_key);
+    const bool by_m = R.min_p > 0.f;
+    if (by_m && (whole || size_key >= low_key)) take(R.min_p > 1.f ? Border{max_key, 1} : Border{max(size_key, low_key), 0x7fffffff});
+    if (R.top_p < 1.f) {
+      if (!k_known || (!limit && !whole && !add_up)) {
+        sure = false;                                          // (the sum that top-p is a share of is not known)
+      } else {
+        double total, error = kFixError;
+        if (limit || whole) {
+          // (a sum over the list: everything down to the border by count, or to the end)
+          const Found f = find_on_list<true>(S, m_list, by_count.key, max_key, ~0ull, by_key, fixed);
+          double sum = static_cast<double>(f.above);
+          if (limit) {
+            const unsigned long long each = fixed(by_count.key);
+            // (the list holds all that have the border's key: take those off that are not kept)
+            unsigned long long same = 0;
+            for (int i = tid; i < m_list; i += kListThreads) same += static_cast<uint32_t>(S.list[i] >> 32) == by_count.key ? 1 : 0;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) same += __shfl_xor_sync(0xffffffffu, same, o);
+            __syncthreads();
+            if (lane == 0) S.d[warp] = static_cast<double>(same);
+            __syncthreads();
+            double all = 0.0;
+#pragma unroll
+            for (int w = 0; w < kListWarps; ++w) all += S.d[w];
+            sum -= (all - static_cast<double>(by_count.ties)) * static_cast<double>(each);
+          }
+          total = sum / kFix;
+        } else {
+          total = z * exp2(static_cast<double>(base) - e.max * c);
+          error = kSumError;
+        }
+        const double target = static_cast<double>(R.top_p) * total;
+        const double t_lo = target * (1.0 - error) * kFix, t_hi = target * (1.0 + error) * kFix;
+        if (!(t_hi < 9.0e18)) {
+          sure = false;
+        } else {
+          const unsigned long long need = t_lo > 1.0 ? __double2ull_ru(t_lo) : 1ull;
+          const Found f = find_on_list<true>(S, m_list, by_count.key, max_key, need, by_key, fixed);
+          if (!f.there) {
+            sure = known && !limit && !whole && border.key >= low_key;    // below the list: another border is on it
+          } else {
+            const unsigned long long each = max(fixed(f.key), 1ull);
+            const unsigned long long ties = (need - f.above + each - 1) / each;
+            const Border by_sum{f.key, static_cast<int>(min(ties, 0x7ffffffeull))};
+            const bool clear = static_cast<double>(f.above + ties * each) >= t_hi;
+            if (clear) take(by_sum);
+            else if (!known || !less(border, by_sum)) sure = false;
+          }
+        }
+      }
+    }
+    if (!known) {
+      if (whole) take(Border{low_key, 0x7fffffff});
+      else sure = false;
+    }
+  }
+  if (!sure || !fits) {
+    if (greedy && !fits) sure = false;
+    if (tid == 0) A.marks[s] = 1;
+    return;
+  }
+
+  // ---- the kept ones: to the front of the list, lowest indices first among those with the border's key
+  uint32_t cut = 0xffffffffu;
+  {
+    const Found f = border.ties == 0x7fffffff
+                        ? Found{false, 0, 0, 0}
+                        : find_on_list<false>(S, m_list, 0, 0xffffffffu, static_cast<unsigned long long>(border.ties),
+                                              [&](int i, uint32_t& k) {
+                                                k = ~static_cast<uint32_t>(S.list[i]);
+                                                return static_cast<uint32_t>(S.list[i] >> 32) == border.key;
+                                              }, one);
+    if (f.there) cut = ~f.key;
+  }
+  __syncthreads();
+  if (tid == 0) S.moved = 0;
+  __syncthreads();
+  for (int i0 = 0; i0 < m_list; i0 += kListThreads) {
+    const int i = i0 + tid;
+    const unsigned long long x = i < m_list ? S.list[i] : 0;
+    const uint32_t k = static_cast<uint32_t>(x >> 32), v = static_cast<uint32_t>(x);
+    const bool keep = i < m_list && (k > border.key || (k == border.key && v <= cut));
+    __syncthreads();
+    const unsigned who = __ballot_sync(0xffffffffu, keep);
+    unsigned at = 0;
+    if (lane == 0 && who) at = atomicAdd(&S.moved, static_cast<unsigned>(__popc(who)));
+    at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+    if (keep) S.list[at] = (static_cast<unsigned long long>(v) << 32) | k;      // (at <= i0: read by all already)
+    __syncthreads();
+  }
+  const int kept = static_cast<int>(S.moved);
+  if (tid == 0) {
+    if (A.kept_out) A.kept_out[s] = kept;
+    A.marks[s] = 0;
+  }
+  if (d1 <= d0) return;
+  int n2 = 1;
+  while (n2 < kept) n2 *= 2;
+  for (int i = kept + tid; i < n2; i += kListThreads) S.list[i] = ~0ull;
+  for (int size = 2; size <= n2; size *= 2) {
+    for (int stride = size / 2; stride > 0; stride /= 2) {
+      __syncthreads();
+      for (int x = tid; x < n2 / 2; x += kListThreads) {
+        const int i = 2 * x - (x & (stride - 1)), j = i + stride;
+        const unsigned long long a = S.list[i], b = S.list[j];
+        if ((a > b) == ((i & size) == 0)) { S.list[i] = b; S.list[j] = a; }
+      }
+    }
+  }
+  __syncthreads();
+  // ---- running sums, a stretch per thread
+  const int stretch = (kept + kListThreads - 1) / kListThreads, i0 = min(tid * stretch, kept), i1 = min(i0 + stretch, kept);
+  double mine = 0.0;
+  for (int i = i0; i < i1; ++i) mine += e(logit_of(static_cast<uint32_t>(S.list[i])));
+  const double incl = warp_scan_d(mine, lane);
+  if (lane == 31) S.d[warp] = incl;
+  __syncthreads();
+  double run = incl - mine;
+  for (int w = 0; w < warp; ++w) run += S.d[w];
+  double* sums = reinterpret_cast<double*>(S.list);
+  for (int i = i0; i < i1; ++i) {
+    const unsigned long long x = S.list[i];
+    run += e(logit_of(static_cast<uint32_t>(x)));
+    S.token[i] = static_cast<uint32_t>(x >> 32);
+    sums[i] = run;
+  }
+  __syncthreads();
+  const double total = sums[kept - 1];
+  for (int64_t d = d0 + tid; d < d1; d += kListThreads) {
+    const float u = __ldg(A.uniforms + d);
+    const double target = (u < 1.f ? fmaxf(u, 0.f) : 1.f) * total;
+    int a = 0, b = kept;
+    while (a < b) {
+      const int mid = (a + b) >> 1;
+      if (sums[mid] > target) b = mid; else a = mid + 1;
+    }
+    if (a == kept) {                                           // none: the last one that adds something
+      --a;
+      while (a > 0 && !(sums[a] > sums[a - 1])) --a;
+    }
+    A.tokens_out[d] = static_cast<int32_t>(S.token[a]);
+    if (A.seq_out) A.seq_out[d] = s;
+  }
+}
+
+template <bool HALF, int CL>
+__device__ __forceinline__ void list_rows(const Args& A) {
+  extern __shared__ __align__(16) unsigned char list_smem[];
+  ListShared& S = *reinterpret_cast<ListShared*>(list_smem);
+  const int clusters = gridDim.x / CL;
+  for (int s = A.row0 + blockIdx.x / CL; s < A.n_seq; s += clusters) {
+    list_row<HALF, CL>(A, S, s);
+    __syncthreads();
+    if (CL > 1) cg::this_cluster().sync();
+  }
+}
+template <bool HALF>
+__global__ void __launch_bounds__(kListThreads, 2) list_rows_kernel(const __grid_constant__ Args A) {
+  ss::grid_dependency_enter();
+  list_rows<HALF, 1>(A);
+}
+template <bool HALF, int CL>
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(kListThreads, 2) list_cluster_kernel(const __grid_constant__ Args A) {
+  ss::grid_dependency_enter();
+  list_rows<HALF, CL>(A);
 }
 
 static int32_t check(const ss_sample_desc_t* d) {
@@ -430,6 +922,57 @@ static int32_t check(const ss_sample_desc_t* d) {
   return SS_OK;
 }
 static size_t workspace_bytes_of(const ss_sample_desc_t* d) { return align_up(sizeof(int32_t) * (static_cast<size_t>(d->n_seq) + 64)); }
+
+template <typename Kernel>
+static int32_t prepare(Kernel kernel, bool (&done)[kDeviceSlots]) {
+  const int slot = current_device_slot();
+  if (slot >= 0 && done[slot]) return SS_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(ListShared))) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SS_ERR_CUDA;
+  }
+  if (slot >= 0) done[slot] = true;
+  return SS_OK;
+}
+template <bool HALF, int CL>
+static int32_t launch_clusters(const Args& A, int rows, cudaStream_t st) {
+  static bool done[kDeviceSlots] = {false};
+  const int32_t rc = prepare(list_cluster_kernel<HALF, CL>, done);
+  if (rc != SS_OK) return rc;
+  SS_LAUNCH((list_cluster_kernel<HALF, CL>), rows * CL, kListThreads, sizeof(ListShared), st, A);
+  return SS_OK;
+}
+// Whole rounds of a row per block, what is left over on clusters that fill the machine, then the marked rows.
+template <bool HALF>
+static int32_t launch(Args A, cudaStream_t st) {
+  const int blocks = 2 * sm_count_of_current_device();
+  const int whole = A.n_seq / blocks * blocks, n_seq = A.n_seq;
+  int rest = n_seq - whole;
+  int size = rest * 8 <= blocks ? 8 : rest * 4 <= blocks ? 4 : rest * 2 <= blocks ? 2 : 1;
+  while (size > 1 && A.vocab < 4096 * size) size /= 2;         // (a slice of a short row is not worth a block)
+  const int first = size == 1 ? n_seq : whole;                 // rows of one block each
+  int32_t rc = SS_OK;
+  if (first > 0) {
+    static bool done[kDeviceSlots] = {false};
+    rc = prepare(list_rows_kernel<HALF>, done);
+    if (rc != SS_OK) return rc;
+    A.row0 = 0;
+    A.n_seq = first;
+    SS_LAUNCH(list_rows_kernel<HALF>, first < blocks ? first : blocks, kListThreads, sizeof(ListShared), st, A);
+  }
+  rest = n_seq - first;
+  if (rest > 0) {
+    A.row0 = first;
+    A.n_seq = n_seq;
+    rc = size == 8 ? launch_clusters<HALF, 8>(A, rest, st) : size == 4 ? launch_clusters<HALF, 4>(A, rest, st) : launch_clusters<HALF, 2>(A, rest, st);
+    if (rc != SS_OK) return rc;
+  }
+  A.row0 = 0;
+  A.n_seq = n_seq;
+  const int most = sm_count_of_current_device();
+  SS_LAUNCH(whole_rows_kernel<HALF>, n_seq < most ? n_seq : most, kThreads, 0, st, A);
+  return SS_OK;
+}
 
 }  // namespace filtered
 }  // namespace ss
@@ -470,12 +1013,6 @@ extern "C" int32_t ss_filtered_sample(const ss_sample_desc_t* d, void* workspace
   A.top_k_all = d->top_k_all;
   A.n_seq = d->n_seq;
   A.vocab = d->vocab;
-  const int sms = ss::sm_count_of_current_device();
-  const int grid = d->n_seq < 2 * sms ? d->n_seq : 2 * sms;
-  if (d->logits_type == SS_LOGITS_BF16) {
-    SS_LAUNCH(whole_rows_kernel<true>, grid, kThreads, 0, ss::as_stream(stream), A);
-  } else {
-    SS_LAUNCH(whole_rows_kernel<false>, grid, kThreads, 0, ss::as_stream(stream), A);
-  }
-  return SS_OK;
+  A.marks = static_cast<int32_t*>(workspace);
+  return d->logits_type == SS_LOGITS_BF16 ? launch<true>(A, ss::as_stream(stream)) : launch<false>(A, ss::as_stream(stream));
 }
