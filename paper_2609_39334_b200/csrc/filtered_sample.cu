@@ -68,6 +68,10 @@ __device__ __forceinline__ const void* row_of(const Args& A, int s) {
   return static_cast<const char*>(A.logits) + static_cast<int64_t>(s) * A.row_stride * (HALF ? 2 : 4);
 }
 
+__device__ __forceinline__ unsigned long long entry_of(float x, int v) {
+  return (static_cast<unsigned long long>(key_of(x)) << 32) | static_cast<uint32_t>(v);
+}
+
 struct Border {
   uint32_t key;                                // tokens above it are kept,
   int ties;                                    // and so many with exactly this key
@@ -459,28 +463,45 @@ struct ListShared {
   float low;                                                   // threshold
   unsigned n;                                                  // entries offered to the list
   unsigned bin, moved;
-  unsigned long long above, in_bin;
+  uint32_t min_key;                                            // of the list
+  unsigned long long above, in_bin, all;
+  unsigned long long u[kListWarps];
   // for the cluster's first block
   double z;
   float max, base;
 };
+
+// Sum of the first `warp` of kListWarps values.
+template <typename T>
+__device__ __forceinline__ T warps_before(const T* per_warp, int warp, int lane) {
+  T v = lane < warp ? per_warp[lane] : T(0);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return __shfl_sync(0xffffffffu, v, 0);
+}
+// Inclusive sum over the block's threads (a barrier inside; `per_warp` is free again behind the next one).
+__device__ __forceinline__ double block_scan_d(double* per_warp, double v, int warp, int lane) {
+  const double incl = warp_scan_d(v, lane);
+  if (lane == 31) per_warp[warp] = incl;
+  __syncthreads();
+  return incl + warps_before(per_warp, warp, lane);
+}
 
 struct Found {                                                 // where a running count or sum over falling keys reaches its target
   bool there;
   uint32_t key;
   unsigned long long above, at_key;                            // over the larger keys, over this one
 };
-// `entry(i)`: key of list entry i and whether it counts; `weight(key)`: what it counts for.  Whole block; keys of [lo, hi].
+// `entry(i, k)`: key of list entry i, and whether it counts; `weight(key)`: what it counts for.  Whole block; keys of [lo, hi].  The
+// bins are zero before and after.
 template <bool MASS, typename Entry, typename Weight>
 __device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo, uint32_t hi, unsigned long long target, Entry entry, Weight weight) {
-  const int tid = threadIdx.x, lane = tid & 31;
+  static_assert(kBins == kListThreads, "a bin per thread");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   unsigned long long above = 0;
   for (;;) {
     const uint32_t range = hi - lo;
     const int shift = range < kBins ? 0 : 32 - __clz(range) - 9;
-    __syncthreads();
-    for (int b = tid; b < kBins; b += kListThreads) { S.count[b] = 0; S.mass[b] = 0; }
-    __syncthreads();
     for (int i = tid; i < n; i += kListThreads) {
       uint32_t k;
       if (entry(i, k) && k >= lo && k <= hi) {
@@ -490,37 +511,26 @@ __device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo,
       }
     }
     __syncthreads();
-    if (tid < 32) {                                            // 16 bins a lane, from the top
-      unsigned long long sum = 0;
+    const int bin = kBins - 1 - tid;                           // from the top
+    const unsigned long long here = MASS ? S.mass[bin] : static_cast<unsigned long long>(S.count[bin]);
+    if (MASS) S.mass[bin] = 0; else S.count[bin] = 0;
+    unsigned long long incl = here;
 #pragma unroll
-      for (int x = 0; x < kBins / 32; ++x) {
-        const int b = kBins - 1 - (lane * (kBins / 32) + x);
-        sum += MASS ? S.mass[b] : static_cast<unsigned long long>(S.count[b]);
-      }
-      unsigned long long incl = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += up;
-      }
-      const unsigned over = __ballot_sync(0xffffffffu, above + incl >= target);
-      if (over == 0) {
-        if (lane == 31) { S.bin = kBins; S.above = above + incl; }
-      } else if (lane == __ffs(over) - 1) {
-        unsigned long long run = above + incl - sum;
-        for (int x = 0; x < kBins / 32; ++x) {
-          const int b = kBins - 1 - (lane * (kBins / 32) + x);
-          const unsigned long long here = MASS ? S.mass[b] : static_cast<unsigned long long>(S.count[b]);
-          if (run + here >= target) { S.bin = b; S.in_bin = here; break; }
-          run += here;
-        }
-        S.above = run;
-      }
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
     }
+    if (lane == 31) S.u[warp] = incl;
+    if (tid == 0) S.bin = kBins;
     __syncthreads();
+    incl += warps_before(S.u, warp, lane) + above;
+    if (incl >= target && incl - here < target) { S.bin = bin; S.above = incl - here; S.in_bin = here; }
+    if (tid == kListThreads - 1) S.all = incl;
+    __syncthreads();
+    const uint32_t at = S.bin;
+    if (at == kBins) return Found{false, lo, S.all, 0};
     above = S.above;
-    if (S.bin == kBins) return Found{false, lo, above, 0};
-    lo += S.bin << shift;
+    lo += at << shift;
     if (shift == 0) return Found{true, lo, above, S.in_bin};
     hi = min(hi, lo + ((1u << shift) - 1u));
   }
@@ -545,6 +555,152 @@ __device__ __forceinline__ void unpack(const uint4& u, float* x) {
       x[i] = __uint_as_float(w[i]);
     }
   }
+}
+
+// Many candidates, or an end that is none of a few: borders by find_on_list, the kept ones sorted by index, running sums in their
+// places.  Returns how many are kept; 0: the list cannot tell.
+__device__ __noinline__ int wide_list(ListShared& S, const RowParams R, const Term e, int m_list, uint32_t low_key, uint32_t max_key, bool limit,
+                                      bool greedy, bool whole, bool add_up, double total_quick) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  bool sure = true;
+  __syncthreads();
+  Border border{kNegInf, 0};
+  bool known = false;
+  auto take = [&](const Border& b) {
+    if (!known || less(b, border)) border = b;
+    known = true;
+  };
+  auto by_key = [&](int i, uint32_t& k) { k = static_cast<uint32_t>(S.list[i] >> 32); return true; };
+  auto fixed = [&](uint32_t k) { return __double2ull_rn(e(logit_of(k)) * kFix); };
+  auto one = [](uint32_t) { return 1ull; };
+  if (greedy) {
+    take(Border{max_key, 1});
+  } else {
+    bool k_known = !limit;
+    Border by_count{low_key, 0x7fffffff};
+    if (limit) {
+      const Found f = find_on_list<false>(S, m_list, low_key, max_key, static_cast<unsigned long long>(R.top_k), by_key, one);
+      if (f.there) {
+        const unsigned long long ties = R.top_k - f.above;
+        by_count = Border{f.key, ties < f.at_key ? static_cast<int>(ties) : 0x7fffffff};
+        take(by_count);
+        k_known = true;
+      }
+    }
+    const uint32_t size_key = min_p_key(e, R.temperature, R.min_p, max_key);
+    const bool by_m = R.min_p > 0.f;
+    if (by_m && (whole || size_key >= low_key)) take(R.min_p > 1.f ? Border{max_key, 1} : Border{max(size_key, low_key), 0x7fffffff});
+    if (R.top_p < 1.f) {
+      if (!k_known || (!limit && !whole && !add_up)) {
+        sure = false;                                          // (the sum that top-p is a share of is not known)
+      } else {
+        double total, error = kFixError;
+        if (limit || whole) {
+          // (a sum over the list: everything down to the border by count, or to the end)
+          const Found f = find_on_list<true>(S, m_list, by_count.key, max_key, ~0ull, by_key, fixed);
+          double sum = static_cast<double>(f.above);
+          if (by_count.ties != 0x7fffffff) {
+            const unsigned long long each = fixed(by_count.key);
+            // (the list holds all that have the border's key: take those off that are not kept)
+            unsigned long long same = 0;
+            for (int i = tid; i < m_list; i += kListThreads) same += static_cast<uint32_t>(S.list[i] >> 32) == by_count.key ? 1 : 0;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) same += __shfl_xor_sync(0xffffffffu, same, o);
+            __syncthreads();
+            if (lane == 0) S.d[warp] = static_cast<double>(same);
+            __syncthreads();
+            double all = 0.0;
+#pragma unroll
+            for (int w = 0; w < kListWarps; ++w) all += S.d[w];
+            sum -= (all - static_cast<double>(by_count.ties)) * static_cast<double>(each);
+          }
+          total = sum / kFix;
+        } else {
+          total = total_quick;
+          error = kSumError;
+        }
+        const double target = static_cast<double>(R.top_p) * total;
+        const double t_lo = target * (1.0 - error) * kFix, t_hi = target * (1.0 + error) * kFix;
+        if (!(t_hi < 9.0e18)) {
+          sure = false;
+        } else {
+          const unsigned long long need = t_lo > 1.0 ? __double2ull_ru(t_lo) : 1ull;
+          const Found f = find_on_list<true>(S, m_list, by_count.key, max_key, need, by_key, fixed);
+          if (!f.there) {
+            sure = known && !limit && !whole && border.key >= low_key;    // below the list: another border is on it
+          } else {
+            const unsigned long long each = max(fixed(f.key), 1ull);
+            const unsigned long long ties = (need - f.above + each - 1) / each;
+            const Border by_sum{f.key, ties * each < f.at_key ? static_cast<int>(ties) : 0x7fffffff};
+            const bool clear = static_cast<double>(f.above + ties * each) >= t_hi;
+            if (clear) take(by_sum);
+            else if (!known || !less(border, by_sum)) sure = false;
+          }
+        }
+      }
+    }
+    if (!known) {
+      if (whole) take(Border{low_key, 0x7fffffff});
+      else sure = false;
+    }
+  }
+  if (!sure) return 0;
+
+  // ---- the kept ones: to the front of the list, lowest indices first among those with the border's key
+  uint32_t cut = 0xffffffffu;
+  {
+    const Found f = border.ties == 0x7fffffff
+                        ? Found{false, 0, 0, 0}
+                        : find_on_list<false>(S, m_list, 0, 0xffffffffu, static_cast<unsigned long long>(border.ties),
+                                              [&](int i, uint32_t& k) {
+                                                k = ~static_cast<uint32_t>(S.list[i]);
+                                                return static_cast<uint32_t>(S.list[i] >> 32) == border.key;
+                                              }, one);
+    if (f.there) cut = ~f.key;
+  }
+  if (tid == 0) S.moved = 0;
+  __syncthreads();
+  auto keeps = [&](unsigned long long x) {
+    const uint32_t k = static_cast<uint32_t>(x >> 32), v = static_cast<uint32_t>(x);
+    return k > border.key || (k == border.key && v <= cut);
+  };
+  auto turned = [](unsigned long long x) { return (x << 32) | (x >> 32); };
+  for (int i0 = 0; i0 < m_list; i0 += kListThreads) {
+    const unsigned long long x = i0 + tid < m_list ? S.list[i0 + tid] : 0;
+    const bool keep = i0 + tid < m_list && keeps(x);
+    __syncthreads();
+    if (keep) S.list[atomicAdd(&S.moved, 1u)] = turned(x);     // (not behind i0 + kListThreads: read by all already)
+    __syncthreads();
+  }
+  const int kept = static_cast<int>(S.moved);
+  int n2 = 1;
+  while (n2 < kept) n2 *= 2;
+  for (int i = kept + tid; i < n2; i += kListThreads) S.list[i] = ~0ull;
+  for (int size = 2; size <= n2; size *= 2) {
+    for (int stride = size / 2; stride > 0; stride /= 2) {
+      __syncthreads();
+      for (int x = tid; x < n2 / 2; x += kListThreads) {
+        const int i = 2 * x - (x & (stride - 1)), j = i + stride;
+        const unsigned long long a = S.list[i], b = S.list[j];
+        if ((a > b) == ((i & size) == 0)) { S.list[i] = b; S.list[j] = a; }
+      }
+    }
+  }
+  __syncthreads();
+  // ---- running sums, a stretch per thread
+  const int stretch = (kept + kListThreads - 1) / kListThreads, i0 = min(tid * stretch, kept), i1 = min(i0 + stretch, kept);
+  double mine = 0.0;
+  for (int i = i0; i < i1; ++i) mine += e(logit_of(static_cast<uint32_t>(S.list[i])));
+  double run = block_scan_d(S.d, mine, warp, lane) - mine;
+  double* sums = reinterpret_cast<double*>(S.list);
+  for (int i = i0; i < i1; ++i) {
+    const unsigned long long x = S.list[i];
+    run += e(logit_of(static_cast<uint32_t>(x)));
+    S.token[i] = static_cast<uint32_t>(x >> 32);
+    sums[i] = run;
+  }
+  __syncthreads();
+  return kept;
 }
 
 template <bool HALF, int CL>
@@ -620,14 +776,13 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
   // ---- the pass
   float mx = -INFINITY;
   double z = 0.0;
-  auto offer = [&](float x, int v) {                           // (a NaN is not taken)
-    const unsigned at = atomicAdd(&S.n, 1u);
-    if (at < kCap) S.list[at] = (static_cast<unsigned long long>(key_of(x)) << 32) | static_cast<uint32_t>(v);
-  };
   auto single = [&](int v) {
     const float x = load_logit<HALF>(row, v);
     mx = max_nan(mx, x);
-    if (x >= low) offer(x, v);
+    if (x >= low) {                                            // (a NaN is not taken)
+      const unsigned at = atomicAdd(&S.n, 1u);
+      if (at < kCap) S.list[at] = entry_of(x, v);
+    }
     if (add_up) {
       float a, b;
       unpack2(quick_pair(x, -INFINITY, quick, c_hi, c_lo), a, b);
@@ -652,10 +807,18 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = max_nan(top, x[i]);
     mx = max_nan(mx, top);
-    if (!(top < low)) {                                        // (a NaN hides what else is there, but no row that holds one is kept)
+    unsigned hits = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (x[i] >= low) offer(x[i], lead + (v0 + (i / kVec) * 32 + lane) * kVec + i % kVec);
+    for (int i = 0; i < 16; ++i) hits += x[i] >= low ? 1 : 0;
+    if (hits) {
+      unsigned at = atomicAdd(&S.n, hits);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (x[i] >= low) {
+          if (at < kCap) S.list[at] = entry_of(x[i], lead + (v0 + (i / kVec) * 32 + lane) * kVec + i % kVec);
+          ++at;
+        }
+      }
     }
     if (add_up) {
 #pragma unroll
@@ -685,16 +848,31 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
     if (tid == 0) { S.z = z; S.max = mx; S.base = base; }
     cl.sync();
     if (rank == 0) {
+      unsigned first[CL + 1];                                  // of every block's entries
+      first[0] = 0;
+      first[1] = n;
+#pragma unroll
       for (int b = 1; b < CL; ++b) {
-        ListShared* o = cl.map_shared_rank(&S, b);
+        const ListShared* o = cl.map_shared_rank(&S, b);
         const unsigned m = o->n;
         if (add_up) z += o->z * exp2(static_cast<double>(o->base) - static_cast<double>(base));
         mx = max_nan(mx, o->max);
         if (!whole) low_key = max(low_key, key_of(o->low));
-        fits = fits && m <= kCap && n + m <= kCap;
-        if (fits)
-          for (unsigned i = tid; i < m; i += kListThreads) S.list[n + i] = o->list[i];
-        n += m;
+        fits = fits && m <= kCap;
+        first[b + 1] = first[b] + m;
+      }
+      n = first[CL];
+      fits = fits && n <= kCap;
+      if (fits) {
+        for (unsigned i = first[1] + tid; i < n; i += kListThreads) {
+          int b = 1;
+#pragma unroll
+          for (int x = 2; x < CL; ++x) b += i >= first[x] ? 1 : 0;
+          unsigned from = first[1];
+#pragma unroll
+          for (int x = 2; x < CL; ++x) from = b == x ? first[x] : from;
+          S.list[i] = cl.map_shared_rank(&S, b)->list[i - from];
+        }
       }
     }
     cl.sync();
@@ -718,162 +896,162 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
     return;
   }
   const uint32_t max_key = key_of(mx);
-  bool sure = fits;
-  Border border{kNegInf, 0};
-  bool known = false;
-  auto take = [&](const Border& b) {
-    if (!known || less(b, border)) border = b;
-    known = true;
-  };
   const int m_list = static_cast<int>(n);
-  auto by_key = [&](int i, uint32_t& k) { k = static_cast<uint32_t>(S.list[i] >> 32); return true; };
   Term e;
   e.max = static_cast<double>(mx);
   e.inv_t = greedy ? 1.0 : 1.0 / static_cast<double>(R.temperature);
   auto fixed = [&](uint32_t k) { return __double2ull_rn(e(logit_of(k)) * kFix); };
-  auto one = [](uint32_t) { return 1ull; };
-  if (greedy) {
-    take(Border{max_key, 1});
-  } else if (sure) {
-    const bool limit = by_k && !(whole && R.top_k >= m_list);  // top-k leaves something out
-    bool k_known = !limit;
-    Border by_count{low_key, 0x7fffffff};
-    if (limit) {
-      const Found f = find_on_list<false>(S, m_list, low_key, max_key, static_cast<unsigned long long>(R.top_k), by_key, one);
-      if (f.there) {
-        by_count = Border{f.key, static_cast<int>(R.top_k - f.above)};
-        take(by_count);
-        k_known = true;
+  const bool limit = !greedy && by_k && !(whole && R.top_k >= m_list);            // top-k leaves something out
+  const bool by_p = !greedy && R.top_p < 1.f, by_m = !greedy && R.min_p > 0.f;
+  const double total_quick = add_up ? z * exp2(static_cast<double>(base) - e.max * c) : 0.0;
+  double* sums = reinterpret_cast<double*>(S.list);            // (behind the borders: running sums of the kept ones, beside S.token)
+  int kept = 0;
+
+  // ---- few candidates (what no filter can keep left out): in order, a thread each
+  bool sure = fits && (!by_p || limit || whole || add_up);
+  if (sure) {
+    uint32_t head = greedy ? max_key : low_key, m_key = 0;     // they have at least the key `head`
+    double total = total_quick, error = by_p && !limit ? kSumError : 0.0;
+    if (whole) {
+      if (tid == 0) S.min_key = max_key;
+      __syncthreads();
+      uint32_t lowest = max_key;
+      for (int i = tid; i < m_list; i += kListThreads) lowest = min(lowest, static_cast<uint32_t>(S.list[i] >> 32));
+      lowest = __reduce_min_sync(0xffffffffu, lowest);
+      if (lane == 0) atomicMin(&S.min_key, lowest);
+      __syncthreads();
+      low_key = S.min_key;
+      if (!greedy) head = low_key;
+    }
+    if (by_m) {                                                // (a bound that is sure; the definition decides below)
+      const double x = e.max + static_cast<double>(R.temperature) * log(fmin(static_cast<double>(R.min_p), 1.0));
+      const double y = x - 1e-6 * (fabs(x) + fabs(e.max)) - 1e-30;
+      if (y > -3.4e38) m_key = min(key_of(static_cast<float>(y)), max_key);
+      head = max(head, m_key);
+    }
+    if ((limit || by_p) && m_list > kListThreads) {            // one histogram: the bin that top-k or top-p ends in
+      const uint32_t range = max_key - low_key;
+      const int shift = range < kBins ? 0 : 32 - __clz(range) - 9;
+      for (int i = tid; i < m_list; i += kListThreads) {
+        const uint32_t k = static_cast<uint32_t>(S.list[i] >> 32);
+        if (k < low_key) continue;
+        const uint32_t b = (k - low_key) >> shift;
+        if (limit) atomicAdd(&S.count[b], 1u);
+        else atomicAdd(&S.mass[b], fixed(k));
+      }
+      if (tid == 0) S.bin = 0;
+      __syncthreads();
+      const int bin = kBins - 1 - tid;
+      const unsigned long long here = limit ? static_cast<unsigned long long>(S.count[bin]) : S.mass[bin];
+      S.count[bin] = 0;
+      S.mass[bin] = 0;
+      unsigned long long incl = here;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      if (lane == 31) S.u[warp] = incl;
+      __syncthreads();
+      incl += warps_before(S.u, warp, lane);
+      if (whole && !limit) {                                   // (the list is all there is)
+        if (tid == kListThreads - 1) S.all = incl;
+        __syncthreads();
+        total = static_cast<double>(S.all) / kFix;
+        error = kFixError;
+      }
+      const double far = static_cast<double>(R.top_p) * total * (1.0 + 2.0 * error) * kFix;
+      const unsigned long long target = limit ? static_cast<unsigned long long>(R.top_k) : far < 1.8e19 ? __double2ull_ru(far) : ~0ull;
+      if (incl >= target && incl - here < target) S.bin = bin;
+      __syncthreads();
+      // (top-p's share is of all that top-k keeps: min-p must not shorten those then)
+      const uint32_t to = low_key + (S.bin << shift);
+      head = limit && by_p ? to : max(head, to);
+    } else if (by_p) {
+      head = low_key;                                          // (all of a short list)
+    }
+    if (tid == 0) S.moved = 0;
+    __syncthreads();
+    for (int i = tid; i < m_list; i += kListThreads) {
+      if (static_cast<uint32_t>(S.list[i] >> 32) >= head) {
+        const unsigned at = atomicAdd(&S.moved, 1u);
+        if (at < kListThreads) S.token[at] = static_cast<uint32_t>(i);
       }
     }
-    const uint32_t size_key = min_p_key(e, R.temperature, R.min_p, max_key);
-    const bool by_m = R.min_p > 0.f;
-    if (by_m && (whole || size_key >= low_key)) take(R.min_p > 1.f ? Border{max_key, 1} : Border{max(size_key, low_key), 0x7fffffff});
-    if (R.top_p < 1.f) {
-      if (!k_known || (!limit && !whole && !add_up)) {
-        sure = false;                                          // (the sum that top-p is a share of is not known)
-      } else {
-        double total, error = kFixError;
-        if (limit || whole) {
-          // (a sum over the list: everything down to the border by count, or to the end)
-          const Found f = find_on_list<true>(S, m_list, by_count.key, max_key, ~0ull, by_key, fixed);
-          double sum = static_cast<double>(f.above);
-          if (limit) {
-            const unsigned long long each = fixed(by_count.key);
-            // (the list holds all that have the border's key: take those off that are not kept)
-            unsigned long long same = 0;
-            for (int i = tid; i < m_list; i += kListThreads) same += static_cast<uint32_t>(S.list[i] >> 32) == by_count.key ? 1 : 0;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) same += __shfl_xor_sync(0xffffffffu, same, o);
-            __syncthreads();
-            if (lane == 0) S.d[warp] = static_cast<double>(same);
-            __syncthreads();
-            double all = 0.0;
-#pragma unroll
-            for (int w = 0; w < kListWarps; ++w) all += S.d[w];
-            sum -= (all - static_cast<double>(by_count.ties)) * static_cast<double>(each);
-          }
-          total = sum / kFix;
-        } else {
-          total = z * exp2(static_cast<double>(base) - e.max * c);
-          error = kSumError;
-        }
-        const double target = static_cast<double>(R.top_p) * total;
-        const double t_lo = target * (1.0 - error) * kFix, t_hi = target * (1.0 + error) * kFix;
-        if (!(t_hi < 9.0e18)) {
+    __syncthreads();
+    const int h = static_cast<int>(S.moved);
+    if (h <= kListThreads) {
+      // in order: largest logit first, equal ones by index
+      unsigned long long y = tid < h ? S.list[S.token[tid]] ^ 0xffffffffull : 0;
+      if (tid < h) S.mass[tid] = y;
+      __syncthreads();
+      int at = 0;
+      if (tid < h)
+        for (int j = 0; j < h; ++j) at += S.mass[j] > y ? 1 : 0;
+      __syncthreads();
+      if (tid < h) S.mass[at] = y;
+      __syncthreads();
+      y = tid < h ? S.mass[tid] : 0;
+      S.mass[tid] = 0;
+      const double mine = tid < h ? e(logit_of(static_cast<uint32_t>(y >> 32))) : 0.0;
+      const double sum = block_scan_d(S.d, mine, warp, lane);
+      // The least of the ends that lie among the candidates; an end that does not is not less.
+      int end = greedy ? 1 : 0x7fffffff;
+      if (limit && R.top_k <= h) end = min(end, R.top_k);
+      if (!limit && whole && h == m_list) end = min(end, h);
+      if (by_m) {
+        const int passing = max(__syncthreads_count(tid < h && mine >= static_cast<double>(R.min_p)), 1);
+        if (passing < h || (head <= m_key && m_key >= low_key)) end = min(end, passing);
+      }
+      if (by_p) {
+        const int n = limit ? R.top_k : h;                     // top-p's share is of these, or more
+        if (n > h) {
           sure = false;
         } else {
-          const unsigned long long need = t_lo > 1.0 ? __double2ull_ru(t_lo) : 1ull;
-          const Found f = find_on_list<true>(S, m_list, by_count.key, max_key, need, by_key, fixed);
-          if (!f.there) {
-            sure = known && !limit && !whole && border.key >= low_key;    // below the list: another border is on it
-          } else {
-            const unsigned long long each = max(fixed(f.key), 1ull);
-            const unsigned long long ties = (need - f.above + each - 1) / each;
-            const Border by_sum{f.key, static_cast<int>(min(ties, 0x7ffffffeull))};
-            const bool clear = static_cast<double>(f.above + ties * each) >= t_hi;
-            if (clear) take(by_sum);
-            else if (!known || !less(border, by_sum)) sure = false;
-          }
+          if (tid == n - 1) S.z = sum;
+          __syncthreads();
+          if (limit || (whole && h == m_list)) { total = S.z; error = 0.0; }
+          const double target = static_cast<double>(R.top_p) * total;
+          const int least = 1 + __syncthreads_count(tid < n && sum < target * (1.0 - error));
+          const int most = 1 + __syncthreads_count(tid < n && sum < target * (1.0 + error));
+          if (!(target > 0.0)) sure = false;                   // (a NaN)
+          else if (least == most && least <= n) end = min(end, least);
+          else if (least <= n) sure = end <= least;            // too close to tell, unless something else ends before
         }
       }
-    }
-    if (!known) {
-      if (whole) take(Border{low_key, 0x7fffffff});
-      else sure = false;
+      if (sure && end <= h) {                                  // the kept ones by index, and their running sums
+        kept = end;
+        const uint32_t v = ~static_cast<uint32_t>(y);
+        if (tid < kept) S.token[tid] = v;
+        __syncthreads();
+        int place = 0;
+        if (tid < kept)
+          for (int j = 0; j < kept; ++j) place += S.token[j] < v ? 1 : 0;
+        __syncthreads();
+        if (tid < kept) {
+          S.token[place] = v;
+          sums[place] = mine;
+        }
+        __syncthreads();
+        const double running = block_scan_d(S.d, tid < kept ? sums[tid] : 0.0, warp, lane);
+        if (tid < kept) sums[tid] = running;
+        __syncthreads();
+      }
     }
   }
-  if (!sure || !fits) {
-    if (greedy && !fits) sure = false;
+  if (!sure) {
     if (tid == 0) A.marks[s] = 1;
     return;
   }
-
-  // ---- the kept ones: to the front of the list, lowest indices first among those with the border's key
-  uint32_t cut = 0xffffffffu;
-  {
-    const Found f = border.ties == 0x7fffffff
-                        ? Found{false, 0, 0, 0}
-                        : find_on_list<false>(S, m_list, 0, 0xffffffffu, static_cast<unsigned long long>(border.ties),
-                                              [&](int i, uint32_t& k) {
-                                                k = ~static_cast<uint32_t>(S.list[i]);
-                                                return static_cast<uint32_t>(S.list[i] >> 32) == border.key;
-                                              }, one);
-    if (f.there) cut = ~f.key;
+  if (kept == 0) kept = wide_list(S, R, e, m_list, low_key, max_key, limit, greedy, whole, add_up, total_quick);
+  if (kept == 0) {
+    if (tid == 0) A.marks[s] = 1;
+    return;
   }
-  __syncthreads();
-  if (tid == 0) S.moved = 0;
-  __syncthreads();
-  for (int i0 = 0; i0 < m_list; i0 += kListThreads) {
-    const int i = i0 + tid;
-    const unsigned long long x = i < m_list ? S.list[i] : 0;
-    const uint32_t k = static_cast<uint32_t>(x >> 32), v = static_cast<uint32_t>(x);
-    const bool keep = i < m_list && (k > border.key || (k == border.key && v <= cut));
-    __syncthreads();
-    const unsigned who = __ballot_sync(0xffffffffu, keep);
-    unsigned at = 0;
-    if (lane == 0 && who) at = atomicAdd(&S.moved, static_cast<unsigned>(__popc(who)));
-    at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
-    if (keep) S.list[at] = (static_cast<unsigned long long>(v) << 32) | k;      // (at <= i0: read by all already)
-    __syncthreads();
-  }
-  const int kept = static_cast<int>(S.moved);
   if (tid == 0) {
     if (A.kept_out) A.kept_out[s] = kept;
     A.marks[s] = 0;
   }
-  if (d1 <= d0) return;
-  int n2 = 1;
-  while (n2 < kept) n2 *= 2;
-  for (int i = kept + tid; i < n2; i += kListThreads) S.list[i] = ~0ull;
-  for (int size = 2; size <= n2; size *= 2) {
-    for (int stride = size / 2; stride > 0; stride /= 2) {
-      __syncthreads();
-      for (int x = tid; x < n2 / 2; x += kListThreads) {
-        const int i = 2 * x - (x & (stride - 1)), j = i + stride;
-        const unsigned long long a = S.list[i], b = S.list[j];
-        if ((a > b) == ((i & size) == 0)) { S.list[i] = b; S.list[j] = a; }
-      }
-    }
-  }
-  __syncthreads();
-  // ---- running sums, a stretch per thread
-  const int stretch = (kept + kListThreads - 1) / kListThreads, i0 = min(tid * stretch, kept), i1 = min(i0 + stretch, kept);
-  double mine = 0.0;
-  for (int i = i0; i < i1; ++i) mine += e(logit_of(static_cast<uint32_t>(S.list[i])));
-  const double incl = warp_scan_d(mine, lane);
-  if (lane == 31) S.d[warp] = incl;
-  __syncthreads();
-  double run = incl - mine;
-  for (int w = 0; w < warp; ++w) run += S.d[w];
-  double* sums = reinterpret_cast<double*>(S.list);
-  for (int i = i0; i < i1; ++i) {
-    const unsigned long long x = S.list[i];
-    run += e(logit_of(static_cast<uint32_t>(x)));
-    S.token[i] = static_cast<uint32_t>(x >> 32);
-    sums[i] = run;
-  }
-  __syncthreads();
   const double total = sums[kept - 1];
   for (int64_t d = d0 + tid; d < d1; d += kListThreads) {
     const float u = __ldg(A.uniforms + d);
@@ -896,6 +1074,8 @@ template <bool HALF, int CL>
 __device__ __forceinline__ void list_rows(const Args& A) {
   extern __shared__ __align__(16) unsigned char list_smem[];
   ListShared& S = *reinterpret_cast<ListShared*>(list_smem);
+  S.count[threadIdx.x] = 0;
+  S.mass[threadIdx.x] = 0;
   const int clusters = gridDim.x / CL;
   for (int s = A.row0 + blockIdx.x / CL; s < A.n_seq; s += clusters) {
     list_row<HALF, CL>(A, S, s);
