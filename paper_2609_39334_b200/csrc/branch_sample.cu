@@ -38,7 +38,6 @@
 #include <stdlib.h>
 
 #include "common.cuh"
-#include "quick_exp2.cuh"
 #include "umma.cuh"
 
 namespace ss {
@@ -275,19 +274,41 @@ __device__ __forceinline__ double warp_sums_4(const double (&v)[4], int lane) {
 
 // A lane's sum of a segment in fp32, two logits at a time, relative to a power of two 2^e0 that the lane moves when a logit exceeds
 // it by 2^60.
-// A term is within 1.21e-7 (quick_exp2.cuh).  Eight terms are added pairwise (three
+// l * c = n + f with |f| <= 1/2: n from a sum whose low bits are the integer, f exactly by an FMA with the high part of c (one
+// rounding to 2^-26) and one with the low part; 2^f by a polynomial of degree 6 (minimax of the relative error on |f| <=
+// 0.5002, coefficients rounded: 1.6e-8); n into the exponent by an integer addition.  A term is within 1.21e-7: 1.6e-8, 2.1e-8
+// from f, 2.4e-8 from the polynomial's inner roundings and 6e-8 from its last one.  Eight terms are added pairwise (three
 // roundings, 1.79e-7) and go to fp64 from there: a sum of any of them is within kQuickError of the exact one.  Terms below
 // 2^(e0 - 124) count as that, 2^-124 of the lane's largest and less.
 struct QuickState {
   float mx, e0, low, shift;
 };
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 both(float a) { return pack2(a, a); }
 __device__ __forceinline__ void quick_base(QuickState& q, const Args& A, float e0) {
   q.e0 = e0;
   q.low = (e0 - 124.f) * A.inv_c;
   q.shift = 12582912.f - e0;                                   // 1.5 * 2^23
 }
 __device__ __forceinline__ f32x2 quick_terms(float l0, float l1, const QuickState& q, const Args& A) {
-  return quick_pair(l0, l1, QuickBase{q.low, q.shift}, A.c_hi, A.c_lo);
+  const f32x2 l = pack2(fmaxf(l0, q.low), fmaxf(l1, q.low)), c_hi = both(A.c_hi);
+  const f32x2 nb = fma2(l, c_hi, both(q.shift));               // bits: 0x4b400000 + (n - e0)
+  f32x2 f = fma2(l, c_hi, fma2(nb, both(-1.f), both(q.shift)));
+  f = fma2(l, both(A.c_lo), f);
+  f32x2 p = fma2(f, both(0.00015353319759014994f), both(0.0013398926239460707f));
+  p = fma2(p, f, both(0.009618437848985195f));
+  p = fma2(p, f, both(0.055503323674201965f));
+  p = fma2(p, f, both(0.24022647738456726f));
+  p = fma2(p, f, both(0.6931471824645996f));
+  p = fma2(p, f, both(1.f));
+  float p0, p1, n0, n1;
+  unpack2(p, p0, p1);
+  unpack2(nb, n0, n1);
+  return pack2(__int_as_float(__float_as_int(p0) + (__float_as_int(n0) << 23)), __int_as_float(__float_as_int(p1) + (__float_as_int(n1) << 23)));
 }
 __device__ __forceinline__ double quick_sums(const float (&l)[16], const Args& A, QuickState& q) {
   float top = l[0];

@@ -9,7 +9,6 @@
 #include <math.h>
 
 #include "common.cuh"
-#include "quick_exp2.cuh"
 
 namespace ss {
 namespace filtered {
@@ -426,16 +425,20 @@ template <bool HALF>
 __global__ void __launch_bounds__(kThreads) whole_rows_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
   __shared__ WholeShared S;
-  for (int s = blockIdx.x; s < A.n_seq; s += gridDim.x) {
-    if (A.marks[s] == 0) continue;
-    whole_row<HALF>(A, S, s);
-    __syncthreads();
+  // the marks of 32 rows of this block at a time
+  for (int64_t s0 = blockIdx.x; s0 < A.n_seq; s0 += static_cast<int64_t>(gridDim.x) * 32) {
+    const int64_t mine = s0 + static_cast<int64_t>(threadIdx.x & 31) * gridDim.x;
+    unsigned marked = __ballot_sync(0xffffffffu, mine < A.n_seq && A.marks[mine] != 0);
+    for (; marked; marked &= marked - 1) {
+      whole_row<HALF>(A, S, static_cast<int>(s0 + static_cast<int64_t>(__ffs(marked) - 1) * gridDim.x));
+      __syncthreads();
+    }
   }
 }
 
 // ---- most rows: one pass over the row, the rest on a short list --------------------------------------------------------------------
 // What is kept is nearly always among the few largest logits, so one pass collects those above a THRESHOLD in shared memory (the
-// list) and, where top-p is over the whole row, adds up all terms in fp32 with a proven bound (quick_exp2.cuh).  The threshold comes from a
+// list) and, where top-p is over the whole row, adds up all terms in fp32 with a bound (quick_pair).  The threshold comes from a
 // sample spread over the row: of the maxima of 64 groups of n sampled tokens a share e^(-n f) lies below the value that a share f of
 // the row exceeds.  Nothing rests on it: a border found on the list is the row's if it does not lie below the threshold, and where
 // the list is too short or too long, or a sum comes too close to top-p's target to tell, the row is marked and made again by the
@@ -449,7 +452,7 @@ constexpr int kBins = 512;
 constexpr int kGroups = 64;                                    // of sampled tokens: 8 lanes each
 constexpr double kFix = 1125899906842624.0;                    // 2^50: kCap terms of at most 1 stay below 2^63
 constexpr double kFixError = 1e-11;                            // kCap * 2^-51 of the largest term, and the sums' own roundings
-constexpr double kSumError = 4e-7;                             // of the quick sum of a row, kQuickError and what is added to it
+constexpr double kSumError = 5e-7;                             // of the quick sum of a row, see quick_pair
 constexpr float kLowest = -3.4028235e38f;
 
 struct ListShared {
@@ -536,6 +539,53 @@ __device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo,
   }
 }
 
+// 2^(l c - e0) of two logits in fp32 (e0 a whole number): l * c = n + f with |f| <= 1/2, n from a sum whose low bits are the integer,
+// f exactly by an FMA with the high part of c (one rounding to 2^-26) and one with the low part, 2^f by the special-function unit
+// (documented: relative error 2^-22), n into the exponent by an integer addition.  A term is within 2.6e-7; eight terms that are
+// added pairwise (three roundings, 1.8e-7) and go to fp64 from there are within 4.4e-7 of the exact sum.  l c - e0 has to lie in
+// [-124, 100]: smaller ones are raised to `low`.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 both(float a) { return pack2(a, a); }
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+struct Quick {
+  float c_hi, c_lo, shift, low;
+};
+__device__ __forceinline__ f32x2 quick_pair(float l0, float l1, const Quick& q) {
+  const f32x2 l = pack2(l0, l1), c = both(q.c_hi), shift = both(q.shift);
+  const f32x2 nb = fma2(l, c, shift);                          // bits: 0x4b400000 + (n - e0)
+  f32x2 f = fma2(l, c, fma2(nb, both(-1.f), shift));
+  f = fma2(l, both(q.c_lo), f);
+  float f0, f1, n0, n1;
+  unpack2(f, f0, f1);
+  unpack2(nb, n0, n1);
+  return pack2(__int_as_float(__float_as_int(ex2(f0)) + (__float_as_int(n0) << 23)), __int_as_float(__float_as_int(ex2(f1)) + (__float_as_int(n1) << 23)));
+}
+
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// x[i], i from 0 to 15
+__device__ __forceinline__ float pick16(const float (&x)[16], int i) {
+  float a[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) a[j] = i & 8 ? x[j + 8] : x[j];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) a[j] = i & 4 ? a[j + 4] : a[j];
+  a[0] = i & 2 ? a[2] : a[0];
+  a[1] = i & 2 ? a[3] : a[1];
+  return i & 1 ? a[1] : a[0];
+}
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -744,8 +794,9 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
   }
   __syncthreads();
   if (!whole && warp == 0) {
-    // (a list for the cluster's first block has to take them all)
-    const float want = fmaxf(2048.f, fminf(4096.f, 2.f * static_cast<float>(by_k ? R.top_k : 0))) / CL;
+    // Candidates wanted: top-k says how many it needs, min-p needs few, top-p of the whole row may need many.  (A list for the
+    // cluster's first block has to take them all.)
+    const float want = (by_k ? fminf(fmaxf(512.f, 2.f * static_cast<float>(R.top_k)), 4096.f) : R.min_p > 0.f ? 1024.f : 4096.f) / CL;
     const float share = fminf(want / static_cast<float>(max(here, 1)), 1.f);
     const int at = min(static_cast<int>(kGroups * __expf(-8.f * kVec * share)), kGroups - 1);
 #pragma unroll
@@ -761,17 +812,19 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
   }
   __syncthreads();
   const float low = S.low;
-  float base = 0.f, c_hi = 0.f, c_lo = 0.f;
+  float base = 0.f;
   double c = 0.0;
+  Quick quick{0.f, 0.f, 0.f, 0.f};
   if (add_up) {
     c = 1.4426950408889634 / static_cast<double>(R.temperature);
-    c_hi = static_cast<float>(c);
-    c_lo = static_cast<float>(c - static_cast<double>(c_hi));
+    quick.c_hi = static_cast<float>(c);
+    quick.c_lo = static_cast<float>(c - static_cast<double>(quick.c_hi));
     float top = S.group[lane];
     top = warp_max(fmaxf(top, S.group[lane + 32]));
-    base = rintf(fminf(fmaxf(top * c_hi, -1e6f), 1e6f));       // (the same in all lanes)
+    base = rintf(fminf(fmaxf(top * quick.c_hi, -1e6f), 1e6f)); // (the same in all lanes)
+    quick.shift = 12582912.f - base;                           // 1.5 * 2^23
+    quick.low = (base - 124.f) / quick.c_hi;
   }
-  const QuickBase quick = quick_base(base, c_hi);
 
   // ---- the pass
   float mx = -INFINITY;
@@ -785,7 +838,7 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
     }
     if (add_up) {
       float a, b;
-      unpack2(quick_pair(x, -INFINITY, quick, c_hi, c_lo), a, b);
+      unpack2(quick_pair(fmaxf(x, quick.low), quick.low, quick), a, b);
       z += static_cast<double>(a);
     }
   };
@@ -805,26 +858,30 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
     for (int j = 0; j < kVecs; ++j) unpack<HALF>(u[j], x + j * kVec);
     float top = x[0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = max_nan(top, x[i]);
-    mx = max_nan(mx, top);
+    for (int i = 1; i < 15; i += 2) top = max3_nan(top, x[i], x[i + 1]);
+    mx = max3_nan(mx, top, x[15]);
     unsigned hits = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) hits += x[i] >= low ? 1 : 0;
+    for (int i = 0; i < 16; ++i) hits |= x[i] >= low ? 1u << i : 0u;
     if (hits) {
-      unsigned at = atomicAdd(&S.n, hits);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (x[i] >= low) {
-          if (at < kCap) S.list[at] = entry_of(x[i], lead + (v0 + (i / kVec) * 32 + lane) * kVec + i % kVec);
-          ++at;
-        }
+      unsigned at = atomicAdd(&S.n, static_cast<unsigned>(__popc(hits)));
+      for (; hits; hits &= hits - 1, ++at) {
+        const int i = __ffs(hits) - 1;
+        if (at < kCap) S.list[at] = entry_of(pick16(x, i), lead + (v0 + (i / kVec) * 32 + lane) * kVec + i % kVec);
       }
     }
     if (add_up) {
+      float least = x[0];
+#pragma unroll
+      for (int i = 1; i < 15; i += 2) least = min3(least, x[i], x[i + 1]);
+      if (!(fminf(least, x[15]) >= quick.low)) {               // masked tokens, or past the end
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = fmaxf(x[i], quick.low);
+      }
 #pragma unroll
       for (int h = 0; h < 16; h += 8) {
-        const f32x2 t = add2(add2(quick_pair(x[h], x[h + 1], quick, c_hi, c_lo), quick_pair(x[h + 2], x[h + 3], quick, c_hi, c_lo)),
-                             add2(quick_pair(x[h + 4], x[h + 5], quick, c_hi, c_lo), quick_pair(x[h + 6], x[h + 7], quick, c_hi, c_lo)));
+        const f32x2 t = add2(add2(quick_pair(x[h], x[h + 1], quick), quick_pair(x[h + 2], x[h + 3], quick)),
+                             add2(quick_pair(x[h + 4], x[h + 5], quick), quick_pair(x[h + 6], x[h + 7], quick)));
         float a, b;
         unpack2(t, a, b);
         z += static_cast<double>(a + b);
@@ -840,7 +897,7 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
   z = S.d[0];
 #pragma unroll
   for (int w = 1; w < kListWarps; ++w) { mx = max_nan(mx, S.f[w]); z += S.d[w]; }
-  if (add_up && !(mx * c_hi <= base + 100.f)) z = NAN;         // (terms out of range: the sample was far off)
+  if (add_up && !(mx * quick.c_hi <= base + 100.f)) z = NAN;         // (terms out of range: the sample was far off)
   unsigned n = S.n;
   bool fits = n <= kCap;
   uint32_t low_key = whole ? kNegInf + 1 : key_of(low);
@@ -1122,13 +1179,39 @@ static int32_t launch_clusters(const Args& A, int rows, cudaStream_t st) {
   SS_LAUNCH((list_cluster_kernel<HALF, CL>), rows * CL, kListThreads, sizeof(ListShared), st, A);
   return SS_OK;
 }
+// Clusters that fit the device at once.
+template <bool HALF, int CL>
+static int resident_clusters() {
+  static int cached[kDeviceSlots] = {0};
+  const int slot = current_device_slot();
+  if (slot >= 0 && cached[slot] > 0) return cached[slot];
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CL;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(CL);
+  cfg.blockDim = dim3(kListThreads);
+  cfg.dynamicSmemBytes = sizeof(ListShared);
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  static bool done[kDeviceSlots] = {false};
+  int n = 0;
+  if (prepare(list_cluster_kernel<HALF, CL>, done) != SS_OK ||
+      cudaOccupancyMaxActiveClusters(&n, list_cluster_kernel<HALF, CL>, &cfg) != cudaSuccess || n < 1) {
+    (void)cudaGetLastError();
+    n = sm_count_of_current_device() / CL;
+  }
+  if (slot >= 0) cached[slot] = n;
+  return n;
+}
 // Whole rounds of a row per block, what is left over on clusters that fill the machine, then the marked rows.
 template <bool HALF>
 static int32_t launch(Args A, cudaStream_t st) {
   const int blocks = 2 * sm_count_of_current_device();
   const int whole = A.n_seq / blocks * blocks, n_seq = A.n_seq;
   int rest = n_seq - whole;
-  int size = rest * 8 <= blocks ? 8 : rest * 4 <= blocks ? 4 : rest * 2 <= blocks ? 2 : 1;
+  int size = rest <= resident_clusters<HALF, 8>() ? 8 : rest <= resident_clusters<HALF, 4>() ? 4 : rest <= resident_clusters<HALF, 2>() ? 2 : 1;
   while (size > 1 && A.vocab < 4096 * size) size /= 2;         // (a slice of a short row is not worth a block)
   const int first = size == 1 ? n_seq : whole;                 // rows of one block each
   int32_t rc = SS_OK;
