@@ -753,28 +753,71 @@ __device__ __noinline__ int wide_list(ListShared& S, const RowParams R, const Te
   return kept;
 }
 
+// A block's slice of a row, from 16-byte boundary to 16-byte boundary but for the row's ends.
 template <bool HALF, int CL>
-__device__ void list_row(const Args& A, ListShared& S, int s) {
-  constexpr int kVec = HALF ? 8 : 4;                           // tokens of a vector
+struct Slice {
+  static constexpr int kVec = HALF ? 8 : 4;                    // tokens of a vector
+  const void* row;
+  const uint4* vecs;
+  int lead, n_vec, vec0, vec1;                                 // tokens in front of the first whole vector; vectors; this block's
+};
+template <bool HALF, int CL>
+__device__ __forceinline__ Slice<HALF, CL> slice_of(const Args& A, int s, int rank) {
+  using T = Slice<HALF, CL>;
+  T t;
+  t.row = row_of<HALF>(A, s);
+  const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(t.row) % 16) / (HALF ? 2 : 4);
+  t.lead = skew ? min(T::kVec - skew, A.vocab) : 0;
+  t.n_vec = (A.vocab - t.lead) / T::kVec;
+  const int per = (t.n_vec + CL - 1) / CL;
+  t.vec0 = min(rank * per, t.n_vec);
+  t.vec1 = min(t.vec0 + per, t.n_vec);
+  t.vecs = reinterpret_cast<const uint4*>(static_cast<const char*>(t.row) + t.lead * (HALF ? 2 : 4));
+  return t;
+}
+// What a row begins with, fetched while the row before it is on its list: parameters, and a vector a thread of the sample (a warp's
+// 512 bytes in a row, the warps spread over the slice).
+struct RowHead {
+  int64_t d0, d1;
+  RowParams R;
+  uint4 sample;
+};
+template <bool HALF, int CL>
+__device__ __forceinline__ RowHead row_head(const Args& A, int s, int rank) {
+  RowHead h;
+  h.d0 = __ldg(A.draw_offsets + s);
+  h.d1 = __ldg(A.draw_offsets + s + 1);
+  h.R = row_params(A, s);
+  h.sample = make_uint4(0, 0, 0, 0);
+  if (A.vocab > kCap) {
+    const Slice<HALF, CL> t = slice_of<HALF, CL>(A, s, rank);
+    const int n = t.vec1 - t.vec0, at = (threadIdx.x >> 5) * (n / kListWarps) + (threadIdx.x & 31);
+    if (n > 0) h.sample = __ldg(t.vecs + t.vec0 + min(at, n - 1));
+  }
+  return h;
+}
+
+// Row s, whose head is `H`; `next`: the row behind it (its head is left in H), or -1.
+template <bool HALF, int CL>
+__device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& H, int s, int next) {
+  constexpr int kVec = Slice<HALF, CL>::kVec;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = A.vocab;
   cg::cluster_group cl = cg::this_cluster();
   const int rank = CL > 1 ? static_cast<int>(cl.block_rank()) : 0;
-  const int64_t d0 = __ldg(A.draw_offsets + s), d1 = __ldg(A.draw_offsets + s + 1);
+  const int64_t d0 = H.d0, d1 = H.d1;
+  const RowParams R = H.R;
   if (d1 <= d0 && !A.kept_out) {
     if (tid == 0 && rank == 0) A.marks[s] = 0;
+    if (next >= 0) H = row_head<HALF, CL>(A, next, rank);
     return;
   }
-  const void* row = row_of<HALF>(A, s);
-  const RowParams R = row_params(A, s);
+  const Slice<HALF, CL> L = slice_of<HALF, CL>(A, s, rank);
+  const void* row = L.row;
+  const uint4* vecs = L.vecs;
+  const int lead = L.lead, n_vec = L.n_vec, vec0 = L.vec0, vec1 = L.vec1;
   const bool fine = R.temperature >= 0.f && R.temperature < INFINITY;
   const bool greedy = R.temperature == 0.f || R.top_k == 1 || R.top_p <= 0.f;
   const bool by_k = R.top_k > 0 && R.top_k < V;
-  // this block's slice, from 16-byte boundary to 16-byte boundary but for the row's ends
-  const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16) / (HALF ? 2 : 4);
-  const int lead = skew ? min(kVec - skew, V) : 0;             // tokens in front of the first whole vector
-  const int n_vec = (V - lead) / kVec, per = (n_vec + CL - 1) / CL;
-  const int vec0 = min(rank * per, n_vec), vec1 = min(vec0 + per, n_vec);
-  const uint4* vecs = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + lead * (HALF ? 2 : 4));
   const int here = (vec1 - vec0) * kVec;
   const bool whole = V <= kCap;                                // every finite logit goes on the list
   const bool add_up = fine && !greedy && !whole && !by_k && R.top_p < 1.f;
@@ -784,7 +827,7 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
     float m = -INFINITY;
     if (here > 0) {
       float x[kVec];
-      unpack<HALF>(__ldg(vecs + vec0 + static_cast<int>(static_cast<int64_t>(tid) * (vec1 - vec0) / kListThreads)), x);
+      unpack<HALF>(H.sample, x);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) m = fmaxf(m, x[i]);
     }
@@ -893,6 +936,7 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
   z = warp_sum_d(z);
   if (lane == 0) { S.f[warp] = mx; S.d[warp] = z; }
   __syncthreads();
+  if (next >= 0) H = row_head<HALF, CL>(A, next, rank);
   mx = S.f[0];
   z = S.d[0];
 #pragma unroll
@@ -986,7 +1030,7 @@ __device__ void list_row(const Args& A, ListShared& S, int s) {
       if (y > -3.4e38) m_key = min(key_of(static_cast<float>(y)), max_key);
       head = max(head, m_key);
     }
-    if ((limit || by_p) && m_list > kListThreads) {            // one histogram: the bin that top-k or top-p ends in
+    if ((limit || by_p) && m_list > (whole && !limit ? kListThreads : 128)) {   // one histogram: the bin that top-k or top-p ends in
       const uint32_t range = max_key - low_key;
       const int shift = range < kBins ? 0 : 32 - __clz(range) - 9;
       for (int i = tid; i < m_list; i += kListThreads) {
@@ -1133,9 +1177,12 @@ __device__ __forceinline__ void list_rows(const Args& A) {
   ListShared& S = *reinterpret_cast<ListShared*>(list_smem);
   S.count[threadIdx.x] = 0;
   S.mass[threadIdx.x] = 0;
-  const int clusters = gridDim.x / CL;
-  for (int s = A.row0 + blockIdx.x / CL; s < A.n_seq; s += clusters) {
-    list_row<HALF, CL>(A, S, s);
+  const int clusters = gridDim.x / CL, rank = CL > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
+  int s = A.row0 + blockIdx.x / CL;
+  if (s >= A.n_seq) return;                                    // (the whole cluster)
+  RowHead H = row_head<HALF, CL>(A, s, rank);
+  for (; s < A.n_seq; s += clusters) {
+    list_row<HALF, CL>(A, S, H, s, s + clusters < A.n_seq ? s + clusters : -1);
     __syncthreads();
     if (CL > 1) cg::this_cluster().sync();
   }
