@@ -29,7 +29,7 @@ using namespace umma;
 
 constexpr int kSoftmaxWarps = 8;
 constexpr int kThreads = (kSoftmaxWarps + 4) * 32;
-constexpr int kStageBytes = kTile * 256;       // one K or V step: [2 halves of 64 dims][128 rows][128 B]
+constexpr int kStageBytes = kTile * 256;       // one K or V step: [16 groups of 8 keys][2 halves of 64 dims][8 rows][128 B]
 constexpr int kStagesK = 3, kStagesV = 2;
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
 constexpr int kOffQ = 0, kOffK = 65536, kOffV = kOffK + kStagesK * kStageBytes;
@@ -139,6 +139,8 @@ __device__ __noinline__ void unit_rows_exact(const Params& P, const Unit& U, int
   }
 }
 
+// BLOCKS: a page's rows of one head start on 8-row boundaries of the pool and come as one copy, else as four.
+template <bool BLOCKS>
 __global__ void __launch_bounds__(kThreads, 1)
 draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                   const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ Params P) {
@@ -440,8 +442,12 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             for (int pg = 0; pg < kTilePages; ++pg) {
               if (pg < n_pages) {
                 const int y = coord[t * 8 + pg];
-                tma_load_2d(dst + pg * 2048, tm, 0, y, bar);
-                tma_load_2d(dst + 16384 + pg * 2048, tm, 64, y, bar);
+                if (BLOCKS) {
+                  tma_load_4d(dst + pg * 4096, tm, 0, 0, 0, y >> 3, bar);
+                } else {
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) tma_load_2d(dst + pg * 4096 + x * 1024, tm, (x & 1) * 64, y + (x >> 1) * 8, bar);
+                }
               }
             }
           }
@@ -460,7 +466,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
               }
               if (!there) {
 #pragma unroll
-                for (int x = 0; x < 16; ++x) *reinterpret_cast<uint4*>(dst + (x >> 3) * 16384 + r * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+                for (int x = 0; x < 16; ++x) *reinterpret_cast<uint4*>(dst + (r >> 3) * 2048 + (x >> 3) * 1024 + (r & 7) * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
               }
             }
             fence_proxy_async_smem();
@@ -478,8 +484,8 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       if (steps[s] > 0 && elect_one()) {
         constexpr uint32_t idesc_qk = instr_desc_bf16(128, kTile, false), idesc_pv = instr_desc_bf16(128, kDim, true);
         const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + kOffQ + (dual ? s : 0) * 32768), 0, 1024);
-        const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem + kOffK), 0, 1024);
-        const uint64_t v_desc0 = smem_desc_sw128(smem_u32(smem + kOffV), 16384, 1024);
+        const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem + kOffK), 0, 2048);
+        const uint64_t v_desc0 = smem_desc_sw128(smem_u32(smem + kOffV), 1024, 2048);
         const uint32_t t_s = tmem + kColS + s * 128, t_o = tmem + kColO + s * 128;
         bool ok = mbar_wait(&C.q_full, seq & 1, abort_flag);
         for (int k = 0; k < steps[s] && ok; ++k) {
@@ -492,7 +498,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)
             mma_bf16_ss(t_s, smem_desc_advance(q_desc, (kk >> 2) * 16384 + (kk & 3) * 32),
-                        smem_desc_advance(k_desc, (kk >> 2) * 16384 + (kk & 3) * 32), idesc_qk, kk > 0 ? 1u : 0u);
+                        smem_desc_advance(k_desc, (kk >> 2) * 1024 + (kk & 3) * 32), idesc_qk, kk > 0 ? 1u : 0u);
           mma_commit(&C.s_full[s]);
           mma_commit(&C.k_empty[sk]);
           if (!dual) mma_commit(&C.k_empty[sk]);
@@ -502,7 +508,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           const uint64_t v_desc = smem_desc_advance(v_desc0, static_cast<uint32_t>(sv) * kStageBytes);
 #pragma unroll
           for (int kk = 0; kk < kTile / 16; ++kk)                // P of keys 0..63 at columns 0..31, of keys 64..127 at 64..95
-            mma_bf16_ts(t_o, t_s + (kk >> 2) * 64 + (kk & 3) * 8, smem_desc_advance(v_desc, kk * 2048), idesc_pv,
+            mma_bf16_ts(t_o, t_s + (kk >> 2) * 64 + (kk & 3) * 8, smem_desc_advance(v_desc, kk * 4096), idesc_pv,
                         (k > 0 || kk > 0) ? 1u : 0u);
           mma_commit(&C.v_empty[sv]);
           if (!dual) mma_commit(&C.v_empty[sv]);
@@ -537,26 +543,35 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   if (warp == kSoftmaxWarps) tmem_dealloc(tmem, kTmemCols);
 }
 
-int32_t launch_tiles(const Params& P, cudaStream_t st, int blocks) {
+template <bool BLOCKS>
+static int32_t launch(const Params& P, cudaStream_t st, int blocks, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq) {
   static bool configured[kDeviceSlots] = {false};
   const int dev_slot = current_device_slot();
   if (dev_slot < 0 || !configured[dev_slot]) {
-    if (cudaFuncSetAttribute(draft_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
+    if (cudaFuncSetAttribute(draft_umma_kernel<BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
       (void)cudaGetLastError();
       return SS_ERR_CUDA;
     }
     if (dev_slot >= 0) configured[dev_slot] = true;
   }
+  SS_LAUNCH(draft_umma_kernel<BLOCKS>, blocks, kThreads, kSmem, st, tk, tv, tq, P);
+  return SS_OK;
+}
+
+int32_t launch_tiles(const Params& P, cudaStream_t st, int blocks) {
   const int64_t rows = ((P.num_pages > 0 ? P.num_pages - 1 : 0) * P.page_stride + (P.Hkv - 1) * P.head_stride) / 128 + kPage;
   if (rows >= 0x7fffffffLL) return SS_ERR_UNSUPPORTED;
   CUtensorMap tk, tv, tq;
-  if (!tmap::encode_2d_bf16(&tk, P.k_pool, kDim, static_cast<uint64_t>(rows), kDim * 2, kPage) ||
-      !tmap::encode_2d_bf16(&tv, P.v_pool, kDim, static_cast<uint64_t>(rows), kDim * 2, kPage) ||
+  const bool whole = P.page_stride % 1024 == 0 && P.head_stride % 1024 == 0;
+  auto encode = [&](CUtensorMap* map, const void* pool) {
+    return whole ? tmap::encode_kv_block_bf16(map, pool, static_cast<uint64_t>(rows))
+                 : tmap::encode_2d_bf16(map, pool, kDim, static_cast<uint64_t>(rows), kDim * 2, 8);
+  };
+  if (!encode(&tk, P.k_pool) || !encode(&tv, P.v_pool) ||
       !tmap::encode_q_bf16(&tq, P.q, static_cast<uint64_t>(P.Hq), static_cast<uint64_t>(P.q_rows > 0 ? P.q_rows : 1),
                            static_cast<uint32_t>(P.G), static_cast<uint32_t>(P.tok_per_tile)))
     return SS_ERR_CUDA;
-  SS_LAUNCH(draft_umma_kernel, blocks, kThreads, kSmem, st, tk, tv, tq, P);
-  return SS_OK;
+  return whole ? launch<true>(P, st, blocks, tk, tv, tq) : launch<false>(P, st, blocks, tk, tv, tq);
 }
 
 }  // namespace draft
