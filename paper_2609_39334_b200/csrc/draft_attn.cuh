@@ -31,6 +31,15 @@ struct alignas(16) CutUnit {
   int64_t dst;
 };
 
+// The chain of a path as segments of whole pages, in key order.
+struct Chain {
+  int n;
+  int first[SS_MAX_DEPTH + 1];               // first page of a segment in the chain's pages
+  int len[SS_MAX_DEPTH];                     // its tokens
+  int start[SS_MAX_DEPTH];                   // index of its first token in the path's sequence
+  int page0[SS_MAX_DEPTH];                   // its first entry in node_pages
+};
+
 struct Params {
   int Hq, Hkv, G;
   int tok_per_tile;
@@ -51,18 +60,10 @@ struct Params {
   // workspace
   Header* hdr;
   PathInfo* paths;
+  Chain* chains;
   uint4* seen;                               // by row of out: the drafts that its token sees, one bit each
   CutUnit* cuts;                             // one per block of the grid
   float *part_o, *part_lse;                  // 2 slots per block of the grid: [slot][2 * kRows][kDim], [slot][2 * kRows]
-};
-
-// The chain of a path as segments of whole pages, in key order.
-struct Chain {
-  int n;
-  int first[SS_MAX_DEPTH + 1];               // first page of a segment in the chain's pages
-  int len[SS_MAX_DEPTH];                     // its tokens
-  int start[SS_MAX_DEPTH];                   // index of its first token in the path's sequence
-  int64_t page0[SS_MAX_DEPTH];               // its first entry in node_pages
 };
 
 #ifdef __CUDACC__
@@ -76,7 +77,7 @@ __device__ __forceinline__ void chain_of(Chain& C, const Params& P, int leaf) {
     C.first[n] = pages;
     C.len[n] = len;
     C.start[n] = tokens;
-    C.page0[n] = P.node_page_offsets[node[c]];
+    C.page0[n] = static_cast<int>(P.node_page_offsets[node[c]]);
     pages += (len + kPage - 1) / kPage;
     tokens += len;
     ++n;
@@ -91,7 +92,7 @@ __device__ __forceinline__ int segment_of(const Chain& C, int vp) {
   return s;
 }
 __device__ __forceinline__ int64_t physical_page(const Chain& C, const Params& P, int s, int vp) {
-  const int64_t entry = C.page0[s] + (vp - C.first[s]);
+  const int64_t entry = static_cast<int64_t>(C.page0[s]) + (vp - C.first[s]);
   int64_t page = entry >= 0 && entry < P.total_node_pages ? static_cast<int64_t>(P.node_pages[entry]) : -1;
   if (page < 0 || page >= P.num_pages) {
     set_status(&P.hdr->status, SS_ERR_BAD_INPUT);

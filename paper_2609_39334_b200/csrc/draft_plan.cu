@@ -53,6 +53,7 @@ __global__ void __launch_bounds__(kPlanThreads) draft_plan_kernel(const __grid_c
         I.L = static_cast<int>(tokens);
         I.tiles = pages > kTilePages ? static_cast<int>((pages + kTilePages - 1) / kTilePages) : 1;
         if (bad != SS_OK) I.T = 0;
+        else chain_of(P.chains[p], P, I.leaf);
         I.status = bad;
         I.blocks = (I.T + 2 * P.tok_per_tile - 1) / (2 * P.tok_per_tile);
         if (I.blocks < 1) I.blocks = 1;
@@ -92,8 +93,7 @@ __global__ void __launch_bounds__(kPlainWarps * 32) draft_plain_kernel(const __g
     const PathInfo I = P.paths[p];
     if (I.status != SS_OK && threadIdx.x == 0) set_status(&P.hdr->status, I.status);
     if (I.T == 0) continue;
-    Chain C;
-    chain_of(C, P, I.leaf);
+    const Chain& C = P.chains[p];
     for (int x = part * kPlainWarps + (threadIdx.x >> 5); x < I.T * P.Hq; x += kPlainBlocks * kPlainWarps) {
       const int t = x / P.Hq, h = x - t * P.Hq;
       Row r;
@@ -162,6 +162,7 @@ static size_t carve(const ss_attn_desc_t* d, void* base, Params* P) {
   const size_t blocks = static_cast<size_t>(sm_count_of_current_device());
   P->hdr = c.take<Header>(1);
   P->paths = c.take<PathInfo>(static_cast<size_t>(d->num_paths) + 1);
+  P->chains = c.take<Chain>(static_cast<size_t>(d->num_paths) + 1);
   P->seen = c.take<uint4>(static_cast<size_t>(d->total_q) + 1);
   P->cuts = c.take<CutUnit>(blocks);
   P->part_lse = c.take<float>(blocks * 2 * 2 * kRows);

@@ -6,19 +6,23 @@
 // shared with its neighbours.  What a block has of a shared unit goes out as a partial result (normalised, with its log-sum),
 // merged by the kernel behind this one; everything else is written once, final.
 //
-// Two softmax STREAMS of four warps, a thread per row, each with its own scores (128 TMEM columns) and accumulator (128):
-//   a unit of two tiles: stream s has tile s, both go over every step (a key is read once for up to 256 rows);
-//   a unit of one tile:  stream s has every other step, and the two accumulators are joined at the end.
-// So while one stream is in its softmax, the tensor cores work for the other.  S = Q K^T and O += P V of a stream are issued by one
-// lane in this order, and tcgen05 instructions of one thread run in order: a step's scores may overwrite the probabilities
-// before them, and when scores are there, the product before them is in the accumulator.
-// Softmax of a step: the row's exact maximum (the reference moves when it is exceeded by 2^8 only: exponentials stay below 2^8 and
-// the accumulator is hardly ever rescaled), exponentials, their fp32 sum, probabilities in bf16 over the scores they come from.
+// Two softmax STREAMS of four warps, a thread per row, each with its own scores (2 x 64 TMEM columns) and accumulator (128), go
+// over a step's keys in halves of 64:
+//   a unit of two tiles: stream s has tile s and both halves (a key is read once for up to 256 rows);
+//   a unit of one tile:  stream s has half s, and the two accumulators are joined at the end.
+// A stream's products are issued by one lane: S(q) = Q K^T of half step q goes out before O += P(q-1) V, so that the next scores are
+// there when the softmax is through with the last ones.  tcgen05 instructions of one thread run in order: S(q) may overwrite P(q-2),
+// and when S(q) is there, the products up to P(q-2) V are in the accumulator.
+// (With scores of 128 keys and one buffer a stream waited for P V and Q K^T after every softmax: 4150 clocks a step of two tiles
+// against 2500 for the softmax.)
+// Softmax of a half step: the row's exact maximum (the reference moves when it is exceeded by 2^8 only: exponentials stay below 2^8
+// and the accumulator is hardly ever rescaled), exponentials, their fp32 sum, probabilities in bf16 over the scores they come from.
 // Masks: from 128 bits per row (which drafts it sees) and the page's place in the chain, in steps that reach the drafts only.
 // Keys that nobody may read (behind a node's end) have their V rows cleared in shared memory; a draft that holds NaN or an infinity
 // and is hidden from some rows reaches them as 0 * NaN: a row that is not finite is computed again, key by key, without it.
 // Roles: warps 0-3, 4-7 streams; 8 K and Q through TMA and the next unit's description; 9 V through TMA; 10, 11 issue the streams'
-// products.  Every wait is bounded (see umma.cuh).
+// products.  They go from unit to unit on their own (descriptions in two slots): while the streams write a unit's rows out, the
+// next one's first keys and its queries are on their way and multiplied.  Every wait is bounded (see umma.cuh).
 #include "draft_attn.cuh"
 #include "umma.cuh"
 
@@ -47,14 +51,17 @@ struct Unit {
   Chain C;
 };
 struct Ctrl {
-  uint64_t q_full, k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV], v_land, s_full[2], p_full[2], o_final[2];
+  uint64_t unit_ready[2], unit_free[2], q_free;
+  uint64_t q_full, k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV], v_land, s_full[2][2], p_full[2][2], o_before[2], o_final[2];
   uint32_t tmem_slot;
   int abort_flag;
   int redo[2];                                 // by unit slot: some row is to be computed again
+  int stop;                                    // a softmax thread has given up
   alignas(16) int coord[2][32];                // pool rows of the pages of four steps, by producer warp
   long long warp_total[kThreads / 32];
   long long pos, end, quota, off;              // this block's place in the line; off: in the steps of path `path`
   int path;
+  float exchange[2][128];                      // between the streams of a row
   Unit unit[2];
 };
 static_assert(sizeof(Ctrl) + kSmem <= 232448, "shared memory of a block");
@@ -79,48 +86,88 @@ __device__ __forceinline__ void store_32B(void* p, const uint32_t (&w)[8]) {
                "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 
+// 128 bytes of every lane to its own line (null: nowhere): four lanes' quarters are exchanged, so that a store instruction writes eight
+// whole lines and not a sector of 32.
+__device__ __forceinline__ void store_lines(void* line, uint32_t (&w)[32], int lane) {
+#pragma unroll
+  for (int m = 1; m <= 2; m *= 2) {
+    const bool upper = (lane & m) != 0;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      if (p & m) continue;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        uint32_t &a = w[8 * p + x], &b = w[8 * (p | m) + x];
+        const uint32_t v = __shfl_xor_sync(0xffffffffu, upper ? a : b, m);
+        if (upper) a = v; else b = v;
+      }
+    }
+  }
+  // quarter `lane & 3` of the lines of lanes 4 g .. 4 g + 3
+  const unsigned long long mine = reinterpret_cast<unsigned long long>(line);
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const unsigned long long to = __shfl_sync(0xffffffffu, mine, (lane & ~3) | p);
+    const uint32_t q[8] = {w[8 * p], w[8 * p + 1], w[8 * p + 2], w[8 * p + 3], w[8 * p + 4], w[8 * p + 5], w[8 * p + 6], w[8 * p + 7]};
+    if (to) store_32B(reinterpret_cast<char*>(to) + 32 * (lane & 3), q);
+  }
+}
+
 __device__ __forceinline__ long long path_cost(const PathInfo& I, int Hkv) {
   return I.T > 0 ? static_cast<long long>(I.tiles) * I.blocks * Hkv : 0;
 }
 
-// The next unit of this block's line into slot `dst` (one thread).
-__device__ __noinline__ void fetch_unit(Ctrl& C, const Params& P, int dst) {
+// The next unit of this block's line into slot `dst` (whole warp).
+__device__ __noinline__ void fetch_unit(Ctrl& C, const Params& P, int dst, int lane) {
   Unit& U = C.unit[dst];
-  U.valid = 0;
-  if (C.pos >= C.end || C.abort_flag) return;
-  PathInfo I = P.paths[C.path];
-  while (C.off >= path_cost(I, P.Hkv)) {       // (ends: steps are left)
-    C.off -= path_cost(I, P.Hkv);
-    I = P.paths[++C.path];
+  const long long pos = C.pos, end = C.end, quota = C.quota;
+  if (pos >= end || *const_cast<volatile int*>(&C.abort_flag)) {
+    __syncwarp();
+    if (lane == 0) U.valid = 0;
+    return;
   }
-  const int u = static_cast<int>(C.off / I.tiles);
-  U.tile0 = static_cast<int>(C.off - static_cast<long long>(u) * I.tiles);
-  U.n_tiles = static_cast<int>(min(static_cast<long long>(I.tiles - U.tile0), C.end - C.pos));
-  U.g = u / I.blocks;
-  const int tok0 = (u - U.g * I.blocks) * I.per_block;
-  U.n_tok = min(I.per_block, I.T - tok0);
-  U.dual = U.n_tok > P.tok_per_tile;
-  U.drafts0 = I.L - I.T;
-  U.holes = I.holes;
-  U.clear_last = I.L % kTile != 0 || I.L == 0;
-  U.src = I.src + tok0;
-  U.dst = I.dst + tok0;
-  chain_of(U.C, P, I.leaf);
-  const bool first = C.pos == C.quota * blockIdx.x, whole = U.n_tiles == I.tiles;
-  U.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (first ? 0 : 1);
-  if (!whole && U.tile0 == 0) {                // it starts here and ends with block `last`: the merge begins at this block
-    const int last = static_cast<int>((C.pos + I.tiles - 1) / C.quota);
-    P.cuts[blockIdx.x] = CutUnit{last - static_cast<int>(blockIdx.x) + 1, U.slot, U.g, U.n_tok, U.dst};
+  int path = C.path;
+  long long off = C.off;
+  PathInfo I = P.paths[path];
+  while (off >= path_cost(I, P.Hkv)) {         // (ends: steps are left)
+    off -= path_cost(I, P.Hkv);
+    I = P.paths[++path];
   }
-  C.pos += U.n_tiles;
-  C.off += U.n_tiles;
-  U.valid = 1;
+  const uint32_t* from = reinterpret_cast<const uint32_t*>(P.chains + path);
+  uint32_t* to = reinterpret_cast<uint32_t*>(&U.C);
+  for (int i = lane; i < static_cast<int>(sizeof(Chain) / 4); i += 32) to[i] = from[i];
+  const int u = static_cast<int>(off / I.tiles), tile0 = static_cast<int>(off - static_cast<long long>(u) * I.tiles);
+  const int n_tiles = static_cast<int>(min(static_cast<long long>(I.tiles - tile0), end - pos));
+  __syncwarp();
+  if (lane == 0) {
+    U.tile0 = tile0;
+    U.n_tiles = n_tiles;
+    U.g = u / I.blocks;
+    const int tok0 = (u - U.g * I.blocks) * I.per_block;
+    U.n_tok = min(I.per_block, I.T - tok0);
+    U.dual = U.n_tok > P.tok_per_tile;
+    U.drafts0 = I.L - I.T;
+    U.holes = I.holes;
+    U.clear_last = I.L % kTile != 0 || I.L == 0;
+    U.src = I.src + tok0;
+    U.dst = I.dst + tok0;
+    const bool first = pos == quota * blockIdx.x, whole = n_tiles == I.tiles;
+    U.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (first ? 0 : 1);
+    if (!whole && tile0 == 0) {                // it starts here and ends with block `last`: the merge begins at this block
+      const int last = static_cast<int>((pos + I.tiles - 1) / quota);
+      P.cuts[blockIdx.x] = CutUnit{last - static_cast<int>(blockIdx.x) + 1, U.slot, U.g, U.n_tok, U.dst};
+    }
+    C.pos = pos + n_tiles;
+    C.off = off + n_tiles;
+    C.path = path;
+    U.valid = 1;
+  }
 }
 
 // The rows of a unit's part once more, a warp per row, key by key: what a row does not see is not touched.
 __device__ __noinline__ void unit_rows_exact(const Params& P, const Unit& U, int warp, int lane) {
   const int rows = U.n_tok * P.G;
-  for (int x = warp; x < rows; x += kThreads / 32) {
+  for (int x = warp; x < rows; x += kSoftmaxWarps) {
     const int t = x / P.G, h = U.g * P.G + x - t * P.G;
     Row r;
     row_start(r, P.q + ((U.src + t) * P.Hq + h) * kDim, lane);
@@ -152,12 +199,18 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 
   if (tid == 0) {
     C.abort_flag = (smem_u32(smem) & 1023u) ? 1 : 0;
-    C.redo[0] = C.redo[1] = 0;
+    C.redo[0] = C.redo[1] = C.stop = 0;
+    for (int s = 0; s < 2; ++s) { mbar_init(&C.unit_ready[s], 1); mbar_init(&C.unit_free[s], kSoftmaxWarps + 3); }
     mbar_init(&C.q_full, 1);
+    mbar_init(&C.q_free, 2);
     for (int s = 0; s < kStagesK; ++s) { mbar_init(&C.k_full[s], 1); mbar_init(&C.k_empty[s], 2); }
     for (int s = 0; s < kStagesV; ++s) { mbar_init(&C.v_full[s], 1); mbar_init(&C.v_empty[s], 2); }
     mbar_init(&C.v_land, 1);
-    for (int s = 0; s < 2; ++s) { mbar_init(&C.s_full[s], 1); mbar_init(&C.p_full[s], 128); mbar_init(&C.o_final[s], 1); }
+    for (int s = 0; s < 2; ++s) {
+      for (int b = 0; b < 2; ++b) { mbar_init(&C.s_full[s][b], 1); mbar_init(&C.p_full[s][b], 128); }
+      mbar_init(&C.o_before[s], 1);
+      mbar_init(&C.o_final[s], 1);
+    }
     fence_barrier_init();
     prefetch_tensormap(&tmap_k);
     prefetch_tensormap(&tmap_v);
@@ -201,76 +254,77 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     C.off = start - (incl - mine);
   }
   __syncthreads();
-  if (tid == kSoftmaxWarps * 32) fetch_unit(C, P, 0);
-  __syncthreads();
-
   const uint32_t tmem = C.tmem_slot;
   const int G = P.G, tpt = P.tok_per_tile;
   uint32_t g_tile = 0;                         // steps behind this block (the same in every role)
-  uint32_t n_s[2] = {0, 0}, n_o[2] = {0, 0};   // steps, and units with a step, behind each stream
+  uint32_t n_half = 0;                         // half steps behind each stream
+  uint32_t n_before = 0;                       // units with more than one half step behind
   uint32_t n_land = 0;                         // V producer: cleared steps so far
   uint32_t seq = 0;
 
+  // The next unit, when its description is there; false: none, or a wait has run out.
+  auto unit_there = [&]() -> bool { return mbar_wait(&C.unit_ready[seq & 1], (seq >> 1) & 1, abort_flag); };
+  auto unit_done = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&C.unit_free[seq & 1]);
+  };
+  if (warp == kSoftmaxWarps) {
+    fetch_unit(C, P, 0, lane);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&C.unit_ready[0]);
+  }
+
   for (;; ++seq) {
     const Unit& U = C.unit[seq & 1];
-    if (!U.valid) break;
+    bool there = unit_there();
+    if (warp < kSoftmaxWarps) {                                  // (they meet at barriers: all of them go on, or none)
+      if (!there) C.stop = 1;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      there = *const_cast<volatile int*>(&C.stop) == 0;
+    } else {
+      there = __all_sync(0xffffffffu, there);
+    }
+    if (!there || !U.valid) break;
     const int n_tiles = U.n_tiles, dual = U.dual;
-    const int steps[2] = {dual ? n_tiles : (n_tiles + 1) / 2, dual ? n_tiles : n_tiles / 2};
+    const int halves = dual ? 2 * n_tiles : n_tiles;             // of each stream
 
     if (warp < kSoftmaxWarps) {
       // =================================================== softmax + epilogue ==================================
-      const int s = warp >> 2, row = tid & 127, mine_steps = steps[s];
+      const int s = warp >> 2, row = tid & 127;
       const int tok_base = dual && s ? tpt : 0, tok_here = dual ? (s ? U.n_tok - tpt : tpt) : U.n_tok;
       const int i = row / G, hl = row - i * G;
       const bool row_valid = i < tok_here;
-      const uint4 seen = row_valid ? P.seen[U.dst + tok_base + i] : make_uint4(0, 0, 0, 0);
       const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-      const uint32_t t_s = tmem + lanes + kColS + s * 128, t_o = tmem + lanes + kColO + s * 128;
+      const uint32_t t_o = tmem + lanes + kColO + s * 128;
       const float cl2 = P.scale_log2, lazy_raw = kLazyLog2 / cl2;
-      const int pages = U.C.first[U.C.n];
       float m = -INFINITY, l = 0.f;
       bool ok = true;
-      for (int k = 0; k < mine_steps; ++k) {
-        const int jt = U.tile0 + (dual ? k : 2 * k + s);
-        uint32_t mask[4];
-        const bool masked = U.holes || (jt + 1) * kTile > U.drafts0;             // (block-uniform)
-        if (masked) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            mask[w] = 0;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int vp = jt * kTilePages + 2 * w + x;
-              if (vp < pages) mask[w] |= page_mask(U.C, segment_of(U.C, vp), vp, U.drafts0, seen) << (16 * x);
-            }
-          }
-        }
-        if (!mbar_wait(&C.s_full[s], (n_s[s] + k) & 1, abort_flag)) ok = false;
+      for (int q = 0; q < halves; ++q) {
+        const uint32_t gq = n_half + q;
+        const int jt = U.tile0 + (dual ? q >> 1 : q), hf = dual ? q & 1 : s;      // step of the chain, half of it
+        const uint32_t t_s = tmem + lanes + kColS + s * 128 + (gq & 1) * 64;
+        if (!mbar_wait(&C.s_full[s][gq & 1], (gq >> 1) & 1, abort_flag)) ok = false;
         tc_fence_after();
         uint32_t sr[64];
-        auto load64 = [&](int c0) {
-          tmem_ld32(t_s + c0, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
-          tmem_ld32(t_s + c0 + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
-          tmem_wait_ld();
-          if (masked) {
-            const uint32_t w0 = c0 ? mask[2] : mask[0], w1 = c0 ? mask[3] : mask[1];
+        tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
+        tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
+        tmem_wait_ld();
+        if (U.holes || jt * kTile + hf * 64 + 64 > U.drafts0) {                   // (block-uniform) not everything is seen
+          const uint4 seen = row_valid ? P.seen[U.dst + tok_base + i] : make_uint4(0, 0, 0, 0);
+          const int pages = U.C.first[U.C.n];
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              if (!((w0 >> c) & 1u)) sr[c] = 0xff800000u;                        // -inf
-              if (!((w1 >> c) & 1u)) sr[32 + c] = 0xff800000u;
-            }
+          for (int w = 0; w < 4; ++w) {
+            const int vp = jt * kTilePages + hf * 4 + w;
+            const uint32_t mask = vp < pages ? page_mask(U.C, segment_of(U.C, vp), vp, U.drafts0, seen) : 0u;
+#pragma unroll
+            for (int c = 0; c < 16; ++c)
+              if (!((mask >> c) & 1u)) sr[16 * w + c] = 0xff800000u;             // -inf
           }
-        };
-        auto max64 = [&]() {
-          float e[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        }
+        float e[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < 64; c += 2) e[(c >> 1) & 3] = max3(e[(c >> 1) & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
-          return fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
-        };
-        load64(0);
-        float mx = max64();
-        load64(64);
-        mx = fmaxf(mx, max64());
+        for (int c = 0; c < 64; c += 2) e[(c >> 1) & 3] = max3(e[(c >> 1) & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
+        const float mx = fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
         float alpha = 1.f;
         const bool move = mx > m + lazy_raw;                                     // (also for a row's first visible key)
         if (move) {
@@ -282,29 +336,29 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         const f32x2 cl2_2 = pack2(cl2, cl2), nmc2 = pack2(-mc, -mc);
         f32x2 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
         uint32_t pr[32];
-        auto exp64 = [&]() {
 #pragma unroll
-          for (int c = 0; c < 64; c += 2) {
-            float x0, x1;
-            unpack2(fma2(pack2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), cl2_2, nmc2), x0, x1);
-            const float e0 = ex2(x0), e1 = ex2(x1);
-            sum2[(c >> 1) & 1] = add2(sum2[(c >> 1) & 1], pack2(e0, e1));
-            pr[c >> 1] = pack_bf16(e0, e1);
-          }
-        };
-        exp64();                                                                 // keys 64 .. 127: over the columns they are in
-        tmem_st32(t_s + 64, pr);
-        load64(0);
-        exp64();
-        tmem_st32(t_s, pr);
+        for (int c = 0; c < 64; c += 2) {
+          float x0, x1;
+          unpack2(fma2(pack2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), cl2_2, nmc2), x0, x1);
+          const float e0 = ex2(x0), e1 = ex2(x1);
+          sum2[(c >> 1) & 1] = add2(sum2[(c >> 1) & 1], pack2(e0, e1));
+          pr[c >> 1] = pack_bf16(e0, e1);
+        }
+        tmem_st32(t_s, pr);                                                      // over the scores they come from
         float a0, a1, a2, a3;
         unpack2(sum2[0], a0, a1);
         unpack2(sum2[1], a2, a3);
         l += (a0 + a1) + (a2 + a3);
-        if (__any_sync(0xffffffffu, move && k > 0)) {                            // rescale O (warp-collective)
+        if (__any_sync(0xffffffffu, move && q > 0)) {                            // rescale O (warp-collective), once P(q-1) V is in it:
+          // the scores of the half step after this one were asked for behind that product
+          const uint32_t gn = gq + 1;
+          ok = (q + 1 < halves ? mbar_wait(&C.s_full[s][gn & 1], (gn >> 1) & 1, abort_flag)
+                               : mbar_wait(&C.o_before[s], n_before & 1, abort_flag)) && ok;
+          tc_fence_after();
 #pragma unroll 1
           for (int c0 = 0; c0 < kDim; c0 += 32) {
             uint32_t o[32];
+            __syncwarp();
             tmem_ld32(t_o + c0, o);
             tmem_wait_ld();
 #pragma unroll
@@ -314,76 +368,75 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         }
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(&C.p_full[s]);
+        mbar_arrive(&C.p_full[s][gq & 1]);
       }
       // ---- epilogue
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        if (steps[x] > 0 && (x == s || !dual)) ok = mbar_wait(&C.o_final[x], n_o[x] & 1, abort_flag) && ok;
+        if (x == s || !dual) ok = mbar_wait(&C.o_final[x], seq & 1, abort_flag) && ok;
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       float w_own = 1.f, w_oth = 0.f;
       if (!dual) {                                                               // the two streams of a row become one
-        float* xm = reinterpret_cast<float*>(smem + kOffQ + 32768);              // (the second tile's rows of Q: not in use)
-        xm[s * 128 + row] = m;
-        xm[256 + s * 128 + row] = l;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        const float m2 = xm[(s ^ 1) * 128 + row], l2 = xm[256 + (s ^ 1) * 128 + row];
+        auto other = [&](float mine) {
+          C.exchange[s][row] = mine;
+          asm volatile("bar.sync 1, 256;" ::: "memory");
+          const float got = C.exchange[s ^ 1][row];
+          asm volatile("bar.sync 1, 256;" ::: "memory");
+          return got;
+        };
+        const float m2 = other(m), l2 = other(l);
         const float top = fmaxf(m, m2);
         w_own = m == -INFINITY ? 0.f : ex2((m - top) * cl2);
         w_oth = m2 == -INFINITY ? 0.f : ex2((m2 - top) * cl2);
         l = s == 0 ? l * w_own + l2 * w_oth : l2 * w_oth + l * w_own;
         m = top;
-        fence_proxy_async_smem();                                                // (TMA writes here again, for a unit of two tiles)
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const float lse = l == 0.f ? -INFINITY : m * P.scale + __logf(l);
       w_own *= inv;
       w_oth *= inv;
-      const int c_begin = dual ? 0 : s * 64, c_end = dual ? kDim : s * 64 + 64;
       const uint32_t t_oth = tmem + lanes + kColO + (s ^ 1) * 128;
-      const bool has_own = steps[s] > 0, has_oth = !dual && steps[s ^ 1] > 0;
       bool finite = lse < INFINITY;                                              // (not for a NaN)
+      // 32 columns of the row's result from c0 on
+      auto result32 = [&](int c0, uint32_t (&o)[32]) {
+        __syncwarp();
+        tmem_ld32(t_o + c0, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * w_own);
+        if (!dual) {
+          uint32_t o2[32];
+          tmem_ld32(t_oth + c0, o2);
+          tmem_wait_ld();
+#pragma unroll
+          for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(fmaf(__uint_as_float(o2[x]), w_oth, __uint_as_float(o[x])));
+        }
+#pragma unroll
+        for (int x = 0; x < 32; ++x) finite = finite && fabsf(__uint_as_float(o[x])) < INFINITY;
+      };
       if (ok) {
+        const int c_begin = dual ? 0 : s * 64, c_end = dual ? kDim : s * 64 + 64;
+        if (U.slot < 0) {
+          __nv_bfloat16* dst = P.out + ((U.dst + tok_base + i) * P.Hq + U.g * G + hl) * kDim;
 #pragma unroll 1
-        for (int c0 = c_begin; c0 < c_end; c0 += 32) {
-          uint32_t o[32];
-          __syncwarp();
-          if (has_own) {
-            tmem_ld32(t_o + c0, o);
-            tmem_wait_ld();
+          for (int c0 = c_begin; c0 < c_end; c0 += 64) {
+            uint32_t o[32], w[32];
 #pragma unroll
-            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * w_own);
-          } else {
+            for (int y = 0; y < 2; ++y) {
+              result32(c0 + 32 * y, o);
 #pragma unroll
-            for (int x = 0; x < 32; ++x) o[x] = 0u;
-          }
-          if (has_oth) {
-            uint32_t o2[32];
-            tmem_ld32(t_oth + c0, o2);
-            tmem_wait_ld();
-#pragma unroll
-            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(fmaf(__uint_as_float(o2[x]), w_oth, __uint_as_float(o[x])));
-          }
-#pragma unroll
-          for (int x = 0; x < 32; ++x) finite = finite && fabsf(__uint_as_float(o[x])) < INFINITY;
-          if (!row_valid) continue;
-          if (U.slot < 0) {
-            __nv_bfloat16* dst = P.out + ((U.dst + tok_base + i) * P.Hq + U.g * G + hl) * kDim + c0;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              uint32_t w[8];
-#pragma unroll
-              for (int y = 0; y < 8; ++y) w[y] = pack_bf16(__uint_as_float(o[16 * x + 2 * y]), __uint_as_float(o[16 * x + 2 * y + 1]));
-              store_32B(dst + 16 * x, w);
+              for (int x = 0; x < 16; ++x) w[16 * y + x] = pack_bf16(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]));
             }
-          } else {
-            float* dst = P.part_o + (static_cast<int64_t>(U.slot) * (2 * kRows) + (dual && s ? kRows : 0) + row) * kDim + c0;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const uint32_t w[8] = {o[8 * x], o[8 * x + 1], o[8 * x + 2], o[8 * x + 3], o[8 * x + 4], o[8 * x + 5], o[8 * x + 6], o[8 * x + 7]};
-              store_32B(dst + 8 * x, w);
-            }
+            store_lines(row_valid ? dst + c0 : nullptr, w, lane);
+          }
+        } else {
+          float* dst = P.part_o + (static_cast<int64_t>(U.slot) * (2 * kRows) + (dual && s ? kRows : 0) + row) * kDim;
+#pragma unroll 1
+          for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+            uint32_t o[32];
+            result32(c0, o);
+            store_lines(row_valid ? dst + c0 : nullptr, o, lane);
           }
         }
         if (row_valid && !finite) C.redo[seq & 1] = 1;
@@ -392,6 +445,14 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           else if (P.lse) P.lse[(U.dst + tok_base + i) * P.Hq + U.g * G + hl] = lse;
         }
       }
+      tc_fence_before();
+      asm volatile("bar.sync 1, 256;" ::: "memory");             // (each stream has read the other's accumulator, too)
+      if (C.redo[seq & 1]) {
+        unit_rows_exact(P, U, warp, lane);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (tid == 0) C.redo[seq & 1] = 0;                       // (set again two units on)
+      }
+      unit_done();
     } else if (warp < kSoftmaxWarps + 2) {
       // =================================================== producers ==============================================
       const int which = warp - kSoftmaxWarps;                    // 0: K (and Q), 1: V
@@ -402,16 +463,21 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       uint8_t* ring = smem + (which ? kOffV : kOffK);
       const int pages = U.C.first[U.C.n];
       bool ok = true;
-      if (which == 0 && elect_one()) {
-        mbar_arrive_expect_tx(&C.q_full, static_cast<uint32_t>((dual ? 2 : 1) * 2 * 128 * G * tpt));
-        for (int x = 0; x < 1 + dual; ++x) {
-          uint8_t* dst = smem + kOffQ + x * 32768;
-          const int src = static_cast<int>(U.src) + x * tpt;
-          tma_load_3d(dst, &tmap_q, 0, U.g * G, src, &C.q_full);
-          tma_load_3d(dst + 16384, &tmap_q, 64, U.g * G, src, &C.q_full);
+      // Q rows, once the products of the unit before have read theirs (behind the first steps' keys, which need not wait for that)
+      auto load_q = [&]() {
+        if (seq > 0) ok = mbar_wait(&C.q_free, (seq - 1) & 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok && elect_one()) {
+          mbar_arrive_expect_tx(&C.q_full, static_cast<uint32_t>((dual ? 2 : 1) * 2 * 128 * G * tpt));
+          for (int x = 0; x < 1 + dual; ++x) {
+            uint8_t* dst = smem + kOffQ + x * 32768;
+            const int src = static_cast<int>(U.src) + x * tpt;
+            tma_load_3d(dst, &tmap_q, 0, U.g * G, src, &C.q_full);
+            tma_load_3d(dst + 16384, &tmap_q, 64, U.g * G, src, &C.q_full);
+          }
         }
-      }
-      __syncwarp();
+        __syncwarp();
+      };
       // The pages of four steps at a time, one a lane, a block ahead of their use; one elected lane issues the copies.
       auto pool_row = [&](int j, int pg) -> int {
         const int vp = (U.tile0 + j) * kTilePages + pg;
@@ -473,64 +539,67 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive(&full[st]);
           }
+          if (which == 0 && j0 + t == min(1, n_tiles - 1)) load_q();
         }
         __syncwarp();
         cur = nxt;
       }
-      if (which == 0 && lane == 0) fetch_unit(C, P, (seq & 1) ^ 1);
+      if (which == 0) {
+        const int next = (seq & 1) ^ 1;
+        if (seq > 0) ok = mbar_wait(&C.unit_free[next], ((seq - 1) >> 1) & 1, abort_flag) && ok;
+        __syncwarp();
+        fetch_unit(C, P, next, lane);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&C.unit_ready[next]);
+      } else {
+        unit_done();
+      }
     } else {
       // =================================================== products of stream s =================================
       const int s = warp - (kSoftmaxWarps + 2);
-      if (steps[s] > 0 && elect_one()) {
-        constexpr uint32_t idesc_qk = instr_desc_bf16(128, kTile, false), idesc_pv = instr_desc_bf16(128, kDim, true);
+      if (elect_one()) {
+        constexpr uint32_t idesc_qk = instr_desc_bf16(128, 64, false), idesc_pv = instr_desc_bf16(128, kDim, true);
         const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + kOffQ + (dual ? s : 0) * 32768), 0, 1024);
         const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem + kOffK), 0, 2048);
         const uint64_t v_desc0 = smem_desc_sw128(smem_u32(smem + kOffV), 1024, 2048);
         const uint32_t t_s = tmem + kColS + s * 128, t_o = tmem + kColO + s * 128;
-        bool ok = mbar_wait(&C.q_full, seq & 1, abort_flag);
-        for (int k = 0; k < steps[s] && ok; ++k) {
-          const uint32_t gj = g_tile + (dual ? k : 2 * k + s);
-          const int sk = gj % kStagesK, sv = gj % kStagesV;
-          ok = mbar_wait(&C.k_full[sk], (gj / kStagesK) & 1, abort_flag);
-          if (!ok) break;
+        auto issue_qk = [&](int q) -> bool {
+          const uint32_t gq = n_half + q, gj = g_tile + (dual ? q >> 1 : q);
+          const int sk = gj % kStagesK, hf = dual ? q & 1 : s;
+          if (!mbar_wait(&C.k_full[sk], (gj / kStagesK) & 1, abort_flag)) return false;
           tc_fence_after();
-          const uint64_t k_desc = smem_desc_advance(k_desc0, static_cast<uint32_t>(sk) * kStageBytes);
+          const uint64_t k_desc = smem_desc_advance(k_desc0, static_cast<uint32_t>(sk) * kStageBytes + hf * 16384u);
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)
-            mma_bf16_ss(t_s, smem_desc_advance(q_desc, (kk >> 2) * 16384 + (kk & 3) * 32),
+            mma_bf16_ss(t_s + (gq & 1) * 64, smem_desc_advance(q_desc, (kk >> 2) * 16384 + (kk & 3) * 32),
                         smem_desc_advance(k_desc, (kk >> 2) * 1024 + (kk & 3) * 32), idesc_qk, kk > 0 ? 1u : 0u);
-          mma_commit(&C.s_full[s]);
-          mma_commit(&C.k_empty[sk]);
-          if (!dual) mma_commit(&C.k_empty[sk]);
-          ok = mbar_wait(&C.v_full[sv], (gj / kStagesV) & 1, abort_flag) && mbar_wait(&C.p_full[s], (n_s[s] + k) & 1, abort_flag);
+          mma_commit(&C.s_full[s][gq & 1]);
+          if (!dual || hf) mma_commit(&C.k_empty[sk]);
+          if (q + 1 == halves) mma_commit(&C.q_free);
+          return true;
+        };
+        bool ok = mbar_wait(&C.q_full, seq & 1, abort_flag) && issue_qk(0);
+        for (int q = 0; q < halves && ok; ++q) {
+          if (q + 1 < halves) ok = issue_qk(q + 1);
+          const uint32_t gq = n_half + q, gj = g_tile + (dual ? q >> 1 : q);
+          const int sv = gj % kStagesV, hf = dual ? q & 1 : s;
+          ok = ok && mbar_wait(&C.v_full[sv], (gj / kStagesV) & 1, abort_flag) && mbar_wait(&C.p_full[s][gq & 1], (gq >> 1) & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
-          const uint64_t v_desc = smem_desc_advance(v_desc0, static_cast<uint32_t>(sv) * kStageBytes);
+          const uint64_t v_desc = smem_desc_advance(v_desc0, static_cast<uint32_t>(sv) * kStageBytes + hf * 16384u);
 #pragma unroll
-          for (int kk = 0; kk < kTile / 16; ++kk)                // P of keys 0..63 at columns 0..31, of keys 64..127 at 64..95
-            mma_bf16_ts(t_o, t_s + (kk >> 2) * 64 + (kk & 3) * 8, smem_desc_advance(v_desc, kk * 4096), idesc_pv,
-                        (k > 0 || kk > 0) ? 1u : 0u);
-          mma_commit(&C.v_empty[sv]);
-          if (!dual) mma_commit(&C.v_empty[sv]);
-          if (k + 1 == steps[s]) mma_commit(&C.o_final[s]);
+          for (int kk = 0; kk < 4; ++kk)
+            mma_bf16_ts(t_o, t_s + (gq & 1) * 64 + kk * 8, smem_desc_advance(v_desc, kk * 4096), idesc_pv, (q > 0 || kk > 0) ? 1u : 0u);
+          if (!dual || hf) mma_commit(&C.v_empty[sv]);
+          if (q + 2 == halves) mma_commit(&C.o_before[s]);
+          if (q + 1 == halves) mma_commit(&C.o_final[s]);
         }
       }
-    }
-    // ---- the unit's end: every role meets here, the pipeline is empty
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    if (C.redo[seq & 1]) {
-      unit_rows_exact(P, U, warp, lane);
-      __syncthreads();
-      if (tid == 0) C.redo[seq & 1] = 0;
+      unit_done();
     }
     g_tile += n_tiles;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      n_s[x] += steps[x];
-      n_o[x] += steps[x] > 0 ? 1 : 0;
-    }
+    n_half += halves;
+    n_before += halves > 1 ? 1 : 0;
   }
 
   __syncthreads();
