@@ -294,6 +294,8 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       const int tok_base = dual && s ? tpt : 0, tok_here = dual ? (s ? U.n_tok - tpt : tpt) : U.n_tok;
       const int i = row / G, hl = row - i * G;
       const bool row_valid = i < tok_here;
+      const bool any_row = __any_sync(0xffffffffu, row_valid);
+      const uint4 seen = row_valid ? P.seen[U.dst + tok_base + i] : make_uint4(0, 0, 0, 0);
       const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
       const uint32_t t_o = tmem + lanes + kColO + s * 128;
       const float cl2 = P.scale_log2, lazy_raw = kLazyLog2 / cl2;
@@ -304,13 +306,16 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         const int jt = U.tile0 + (dual ? q >> 1 : q), hf = dual ? q & 1 : s;      // step of the chain, half of it
         const uint32_t t_s = tmem + lanes + kColS + s * 128 + (gq & 1) * 64;
         if (!mbar_wait(&C.s_full[s][gq & 1], (gq >> 1) & 1, abort_flag)) ok = false;
+        if (!any_row) {                        // (products of rows that nobody asked for come out in rows that nobody reads)
+          mbar_arrive(&C.p_full[s][gq & 1]);
+          continue;
+        }
         tc_fence_after();
         uint32_t sr[64];
         tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
         tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
         tmem_wait_ld();
         if (U.holes || jt * kTile + hf * 64 + 64 > U.drafts0) {                   // (block-uniform) not everything is seen
-          const uint4 seen = row_valid ? P.seen[U.dst + tok_base + i] : make_uint4(0, 0, 0, 0);
           const int pages = U.C.first[U.C.n];
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
@@ -478,6 +483,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         }
         __syncwarp();
       };
+      if (which == 0 && seq == 0) load_q();
       // The pages of four steps at a time, one a lane, a block ahead of their use; one elected lane issues the copies.
       auto pool_row = [&](int j, int pg) -> int {
         const int vp = (U.tile0 + j) * kTilePages + pg;
@@ -539,7 +545,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive(&full[st]);
           }
-          if (which == 0 && j0 + t == min(1, n_tiles - 1)) load_q();
+          if (which == 0 && seq > 0 && j0 + t == min(1, n_tiles - 1)) load_q();
         }
         __syncwarp();
         cur = nxt;
