@@ -5,7 +5,6 @@
 // counting, top-p one by adding up probabilities, min-p one by a bound on the logit; the least of the three holds.  A draw then
 // goes by the running sum over the kept tokens in index order.  Logits are compared as order-preserving integers (bf16 ones are
 // widened: exact); probabilities are fp64 relative to the row's maximum.
-#include <cooperative_groups.h>
 #include <math.h>
 
 #include "common.cuh"
@@ -13,10 +12,8 @@
 namespace ss {
 namespace filtered {
 
-namespace cg = cooperative_groups;
-
 constexpr int kMaxVocab = 2097152;
-constexpr int kThreads = 1024, kWarps = kThreads / 32;         // of a block that goes through whole rows
+constexpr int kThreads = 512, kWarps = kThreads / 32;          // of a block that goes through whole rows
 constexpr int kSeg = 512;                                      // tokens of a segment (a sum each, for the draws)
 constexpr uint32_t kNegInf = 0x007fffffu;                      // key of -inf; those of NaN are below it or above kPosInf
 constexpr uint32_t kPosInf = 0xff800000u;
@@ -33,8 +30,10 @@ struct Args {
   float temperature_all, top_p_all, min_p_all;
   int top_k_all;
   int n_seq, vocab;
-  int row0;                                    // first row of this launch
   int32_t* marks;                              // [n_seq]: rows that the list is not enough for
+  int whole_rows;                              // rows of one block each; the others are split into
+  int parts;                                   // so many parts
+  struct Part* part;                           // [blocks]
 };
 struct RowParams {
   float temperature, top_p, min_p;
@@ -421,21 +420,6 @@ __device__ void whole_row(const Args& A, WholeShared& S, int s) {
   __syncthreads();
 }
 
-template <bool HALF>
-__global__ void __launch_bounds__(kThreads) whole_rows_kernel(const __grid_constant__ Args A) {
-  ss::grid_dependency_enter();
-  __shared__ WholeShared S;
-  // the marks of 32 rows of this block at a time
-  for (int64_t s0 = blockIdx.x; s0 < A.n_seq; s0 += static_cast<int64_t>(gridDim.x) * 32) {
-    const int64_t mine = s0 + static_cast<int64_t>(threadIdx.x & 31) * gridDim.x;
-    unsigned marked = __ballot_sync(0xffffffffu, mine < A.n_seq && A.marks[mine] != 0);
-    for (; marked; marked &= marked - 1) {
-      whole_row<HALF>(A, S, static_cast<int>(s0 + static_cast<int64_t>(__ffs(marked) - 1) * gridDim.x));
-      __syncthreads();
-    }
-  }
-}
-
 // ---- most rows: one pass over the row, the rest on a short list --------------------------------------------------------------------
 // What is kept is nearly always among the few largest logits, so one pass collects those above a THRESHOLD in shared memory (the
 // list) and, where top-p is over the whole row, adds up all terms in fp32 with a bound (quick_pair).  The threshold comes from a
@@ -443,9 +427,13 @@ __global__ void __launch_bounds__(kThreads) whole_rows_kernel(const __grid_const
 // the row exceeds.  Nothing rests on it: a border found on the list is the row's if it does not lie below the threshold, and where
 // the list is too short or too long, or a sum comes too close to top-p's target to tell, the row is marked and made again by the
 // kernel behind this one.  (Short rows are on the list as a whole.)
-// On the list: borders by histograms of 512 bins over the range of keys that is left, counts or terms in 64-bit fixed point (any
-// order, the same sums), three rounds for a range of 2^24 keys; the kept ones sorted by index; their running sum in fp64; a thread per draw.
-// Two blocks an SM, so that one is in its pass while the other is on its list.
+// On the list: one histogram to the at most 512 candidates for what is kept, those in order, a thread each, and every filter's end by
+// a running sum (fp64).  Where more are kept: borders by find_on_list, the kept ones sorted by index.  A draw is a thread's.
+// Two blocks an SM, so that one is in its pass while the other is on its list.  In the pass every lane has the next four vectors on
+// their way to shared memory while it works on the last four: 16 warps then ask for as much as an SM's share of the bandwidth takes
+// (straight into registers, with room for four vectors, a block got 11.8 bytes a clock, alone or beside the other one).  Rows that are
+// left over behind whole rounds, one a block, are split over the blocks: each hands its part's list over in the workspace, the next
+// kernel puts them together.
 constexpr int kListThreads = 512, kListWarps = kListThreads / 32;
 constexpr int kCap = 8192;                                     // entries of a list
 constexpr int kBins = 512;
@@ -455,24 +443,46 @@ constexpr double kFixError = 1e-11;                            // kCap * 2^-51 o
 constexpr double kSumError = 5e-7;                             // of the quick sum of a row, see quick_pair
 constexpr float kLowest = -3.4028235e38f;
 
-struct ListShared {
+struct RowBuffer {                                             // a row between the pass and its list
   unsigned long long list[kCap];                               // key, token; then token, key; then running sums
-  uint32_t token[kCap];
+  unsigned n;                                                  // entries offered to the list
+  float low, base;                                             // threshold; the quick sum is relative to 2^base
+  bool skip;                                                   // nothing to do
+  int64_t d0, d1;
+  RowParams R;
+  float max[kListWarps];
+  double sum[kListWarps];
+};
+struct ListShared {
+  union {
+    uint32_t token[kCap];
+    uint4 ring[kListWarps][4][32];                             // in the pass
+  };
   unsigned long long mass[kBins];
   unsigned count[kBins];
   double d[kListWarps];
-  float f[kListWarps];
   float group[kGroups];
-  float low;                                                   // threshold
-  unsigned n;                                                  // entries offered to the list
   unsigned bin, moved;
   uint32_t min_key;                                            // of the list
   unsigned long long above, in_bin, all;
   unsigned long long u[kListWarps];
-  // for the cluster's first block
   double z;
-  float max, base;
 };
+constexpr int kPartCap = 2048;                                 // entries of a part's list
+struct Part {                                                  // of a row, in the workspace
+  unsigned n;
+  float low, base, max;
+  double sum;
+  unsigned long long list[kPartCap];
+};
+
+// The kListThreads threads that work on a list.
+__device__ __forceinline__ void list_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kListThreads) : "memory"); }
+__device__ __forceinline__ int list_count(bool p) {
+  int n;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.popc.u32 %0, 1, %2, p;\n\t}" : "=r"(n) : "r"(static_cast<int>(p)), "n"(kListThreads) : "memory");
+  return n;
+}
 
 // Sum of the first `warp` of kListWarps values.
 template <typename T>
@@ -486,7 +496,7 @@ __device__ __forceinline__ T warps_before(const T* per_warp, int warp, int lane)
 __device__ __forceinline__ double block_scan_d(double* per_warp, double v, int warp, int lane) {
   const double incl = warp_scan_d(v, lane);
   if (lane == 31) per_warp[warp] = incl;
-  __syncthreads();
+  list_sync();
   return incl + warps_before(per_warp, warp, lane);
 }
 
@@ -500,7 +510,7 @@ struct Found {                                                 // where a runnin
 template <bool MASS, typename Entry, typename Weight>
 __device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo, uint32_t hi, unsigned long long target, Entry entry, Weight weight) {
   static_assert(kBins == kListThreads, "a bin per thread");
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x % kListThreads, lane = tid & 31, warp = tid >> 5;
   unsigned long long above = 0;
   for (;;) {
     const uint32_t range = hi - lo;
@@ -513,7 +523,7 @@ __device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo,
         else atomicAdd(&S.count[b], 1u);
       }
     }
-    __syncthreads();
+    list_sync();
     const int bin = kBins - 1 - tid;                           // from the top
     const unsigned long long here = MASS ? S.mass[bin] : static_cast<unsigned long long>(S.count[bin]);
     if (MASS) S.mass[bin] = 0; else S.count[bin] = 0;
@@ -525,11 +535,11 @@ __device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo,
     }
     if (lane == 31) S.u[warp] = incl;
     if (tid == 0) S.bin = kBins;
-    __syncthreads();
+    list_sync();
     incl += warps_before(S.u, warp, lane) + above;
     if (incl >= target && incl - here < target) { S.bin = bin; S.above = incl - here; S.in_bin = here; }
     if (tid == kListThreads - 1) S.all = incl;
-    __syncthreads();
+    list_sync();
     const uint32_t at = S.bin;
     if (at == kBins) return Found{false, lo, S.all, 0};
     above = S.above;
@@ -609,18 +619,18 @@ __device__ __forceinline__ void unpack(const uint4& u, float* x) {
 
 // Many candidates, or an end that is none of a few: borders by find_on_list, the kept ones sorted by index, running sums in their
 // places.  Returns how many are kept; 0: the list cannot tell.
-__device__ __noinline__ int wide_list(ListShared& S, const RowParams R, const Term e, int m_list, uint32_t low_key, uint32_t max_key, bool limit,
-                                      bool greedy, bool whole, bool add_up, double total_quick) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+__device__ __noinline__ int wide_list(ListShared& S, unsigned long long* list, const RowParams R, const Term e, int m_list, uint32_t low_key, uint32_t max_key, bool limit,
+                                      bool greedy, bool whole, bool add_up, double total_quick, double error_quick) {
+  const int tid = threadIdx.x % kListThreads, lane = tid & 31, warp = tid >> 5;
   bool sure = true;
-  __syncthreads();
+  list_sync();
   Border border{kNegInf, 0};
   bool known = false;
   auto take = [&](const Border& b) {
     if (!known || less(b, border)) border = b;
     known = true;
   };
-  auto by_key = [&](int i, uint32_t& k) { k = static_cast<uint32_t>(S.list[i] >> 32); return true; };
+  auto by_key = [&](int i, uint32_t& k) { k = static_cast<uint32_t>(list[i] >> 32); return true; };
   auto fixed = [&](uint32_t k) { return __double2ull_rn(e(logit_of(k)) * kFix); };
   auto one = [](uint32_t) { return 1ull; };
   if (greedy) {
@@ -653,12 +663,12 @@ __device__ __noinline__ int wide_list(ListShared& S, const RowParams R, const Te
             const unsigned long long each = fixed(by_count.key);
             // (the list holds all that have the border's key: take those off that are not kept)
             unsigned long long same = 0;
-            for (int i = tid; i < m_list; i += kListThreads) same += static_cast<uint32_t>(S.list[i] >> 32) == by_count.key ? 1 : 0;
+            for (int i = tid; i < m_list; i += kListThreads) same += static_cast<uint32_t>(list[i] >> 32) == by_count.key ? 1 : 0;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) same += __shfl_xor_sync(0xffffffffu, same, o);
-            __syncthreads();
+            list_sync();
             if (lane == 0) S.d[warp] = static_cast<double>(same);
-            __syncthreads();
+            list_sync();
             double all = 0.0;
 #pragma unroll
             for (int w = 0; w < kListWarps; ++w) all += S.d[w];
@@ -667,7 +677,7 @@ __device__ __noinline__ int wide_list(ListShared& S, const RowParams R, const Te
           total = sum / kFix;
         } else {
           total = total_quick;
-          error = kSumError;
+          error = error_quick;
         }
         const double target = static_cast<double>(R.top_p) * total;
         const double t_lo = target * (1.0 - error) * kFix, t_hi = target * (1.0 + error) * kFix;
@@ -703,181 +713,202 @@ __device__ __noinline__ int wide_list(ListShared& S, const RowParams R, const Te
                         ? Found{false, 0, 0, 0}
                         : find_on_list<false>(S, m_list, 0, 0xffffffffu, static_cast<unsigned long long>(border.ties),
                                               [&](int i, uint32_t& k) {
-                                                k = ~static_cast<uint32_t>(S.list[i]);
-                                                return static_cast<uint32_t>(S.list[i] >> 32) == border.key;
+                                                k = ~static_cast<uint32_t>(list[i]);
+                                                return static_cast<uint32_t>(list[i] >> 32) == border.key;
                                               }, one);
     if (f.there) cut = ~f.key;
   }
   if (tid == 0) S.moved = 0;
-  __syncthreads();
+  list_sync();
   auto keeps = [&](unsigned long long x) {
     const uint32_t k = static_cast<uint32_t>(x >> 32), v = static_cast<uint32_t>(x);
     return k > border.key || (k == border.key && v <= cut);
   };
   auto turned = [](unsigned long long x) { return (x << 32) | (x >> 32); };
   for (int i0 = 0; i0 < m_list; i0 += kListThreads) {
-    const unsigned long long x = i0 + tid < m_list ? S.list[i0 + tid] : 0;
+    const unsigned long long x = i0 + tid < m_list ? list[i0 + tid] : 0;
     const bool keep = i0 + tid < m_list && keeps(x);
-    __syncthreads();
-    if (keep) S.list[atomicAdd(&S.moved, 1u)] = turned(x);     // (not behind i0 + kListThreads: read by all already)
-    __syncthreads();
+    list_sync();
+    if (keep) list[atomicAdd(&S.moved, 1u)] = turned(x);     // (not behind i0 + kListThreads: read by all already)
+    list_sync();
   }
   const int kept = static_cast<int>(S.moved);
   int n2 = 1;
   while (n2 < kept) n2 *= 2;
-  for (int i = kept + tid; i < n2; i += kListThreads) S.list[i] = ~0ull;
+  for (int i = kept + tid; i < n2; i += kListThreads) list[i] = ~0ull;
   for (int size = 2; size <= n2; size *= 2) {
     for (int stride = size / 2; stride > 0; stride /= 2) {
-      __syncthreads();
+      list_sync();
       for (int x = tid; x < n2 / 2; x += kListThreads) {
         const int i = 2 * x - (x & (stride - 1)), j = i + stride;
-        const unsigned long long a = S.list[i], b = S.list[j];
-        if ((a > b) == ((i & size) == 0)) { S.list[i] = b; S.list[j] = a; }
+        const unsigned long long a = list[i], b = list[j];
+        if ((a > b) == ((i & size) == 0)) { list[i] = b; list[j] = a; }
       }
     }
   }
-  __syncthreads();
+  list_sync();
   // ---- running sums, a stretch per thread
   const int stretch = (kept + kListThreads - 1) / kListThreads, i0 = min(tid * stretch, kept), i1 = min(i0 + stretch, kept);
   double mine = 0.0;
-  for (int i = i0; i < i1; ++i) mine += e(logit_of(static_cast<uint32_t>(S.list[i])));
+  for (int i = i0; i < i1; ++i) mine += e(logit_of(static_cast<uint32_t>(list[i])));
   double run = block_scan_d(S.d, mine, warp, lane) - mine;
-  double* sums = reinterpret_cast<double*>(S.list);
+  double* sums = reinterpret_cast<double*>(list);
   for (int i = i0; i < i1; ++i) {
-    const unsigned long long x = S.list[i];
+    const unsigned long long x = list[i];
     run += e(logit_of(static_cast<uint32_t>(x)));
     S.token[i] = static_cast<uint32_t>(x >> 32);
     sums[i] = run;
   }
-  __syncthreads();
+  list_sync();
   return kept;
 }
 
-// A block's slice of a row, from 16-byte boundary to 16-byte boundary but for the row's ends.
-template <bool HALF, int CL>
+// A part of a row, from 16-byte boundary to 16-byte boundary but for the row's ends.
+template <bool HALF>
 struct Slice {
   static constexpr int kVec = HALF ? 8 : 4;                    // tokens of a vector
   const void* row;
   const uint4* vecs;
-  int lead, n_vec, vec0, vec1;                                 // tokens in front of the first whole vector; vectors; this block's
+  int lead, n_vec, vec0, vec1;                                 // tokens in front of the first whole vector; vectors; the part's
 };
-template <bool HALF, int CL>
-__device__ __forceinline__ Slice<HALF, CL> slice_of(const Args& A, int s, int rank) {
-  using T = Slice<HALF, CL>;
+template <bool HALF>
+__device__ __forceinline__ Slice<HALF> slice_of(const Args& A, int s, int part, int parts) {
+  using T = Slice<HALF>;
   T t;
   t.row = row_of<HALF>(A, s);
   const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(t.row) % 16) / (HALF ? 2 : 4);
   t.lead = skew ? min(T::kVec - skew, A.vocab) : 0;
   t.n_vec = (A.vocab - t.lead) / T::kVec;
-  const int per = (t.n_vec + CL - 1) / CL;
-  t.vec0 = min(rank * per, t.n_vec);
+  const int per = (t.n_vec + parts - 1) / parts;
+  t.vec0 = min(part * per, t.n_vec);
   t.vec1 = min(t.vec0 + per, t.n_vec);
   t.vecs = reinterpret_cast<const uint4*>(static_cast<const char*>(t.row) + t.lead * (HALF ? 2 : 4));
   return t;
 }
-// What a row begins with, fetched while the row before it is on its list: parameters, and a vector a thread of the sample (a warp's
-// 512 bytes in a row, the warps spread over the slice).
+// What a row's parameters make of it.
+struct RowKind {
+  bool fine, greedy, by_k, whole, add_up;
+  bool rough;                                                  // the sum without quick_pair's reduction, see rough_error
+};
+__device__ __forceinline__ RowKind kind_of(const RowParams& R, int V) {
+  RowKind k;
+  k.fine = R.temperature >= 0.f && R.temperature < INFINITY;
+  k.greedy = R.temperature == 0.f || R.top_k == 1 || R.top_p <= 0.f;
+  k.by_k = R.top_k > 0 && R.top_k < V;
+  k.whole = V <= kCap;                                         // every finite logit goes on the list
+  k.add_up = k.fine && !k.greedy && !k.whole && !k.by_k && R.top_p < 1.f;
+  k.rough = R.min_p > 0.f;                                     // (min-p is nearly always what ends such a row then: any bound will do)
+  return k;
+}
+// Relative error of a sum of 2^(fma(l, c_hi, -base)): an exponent x is off by 2^-24 |x| (its rounding) and 2^-25 |l c| (that of c), and |x|
+// is at most `far` beside the largest term's and log2 V on average over the terms (the entropy of the row); the rest as for quick_pair.
+__device__ __forceinline__ double rough_error(double base, double far, int V) {
+  const double x = 33 - __clz(V) + far;
+  return 0.6932 * (0x1p-24 * x + 0x1p-25 * (x + fabs(base))) + kSumError;
+}
+__device__ __forceinline__ Quick quick_of(const RowParams& R, float base, double& c) {
+  Quick q;
+  c = 1.4426950408889634 / static_cast<double>(R.temperature);
+  q.c_hi = static_cast<float>(c);
+  q.c_lo = static_cast<float>(c - static_cast<double>(q.c_hi));
+  q.shift = 12582912.f - base;                                 // 1.5 * 2^23
+  q.low = (base - 124.f) / q.c_hi;
+  return q;
+}
+struct Job {                                                   // of a block: a row or a part of one
+  int s, part, parts;
+};
+// What a job begins with: parameters, and a vector a thread of the sample (a warp's 512 bytes in a row, the warps spread over the part).
 struct RowHead {
   int64_t d0, d1;
   RowParams R;
   uint4 sample;
 };
-template <bool HALF, int CL>
-__device__ __forceinline__ RowHead row_head(const Args& A, int s, int rank) {
+template <bool HALF>
+__device__ __forceinline__ RowHead row_head(const Args& A, const Job& job) {
+  const int tid = threadIdx.x % kListThreads;
   RowHead h;
-  h.d0 = __ldg(A.draw_offsets + s);
-  h.d1 = __ldg(A.draw_offsets + s + 1);
-  h.R = row_params(A, s);
+  h.d0 = __ldg(A.draw_offsets + job.s);
+  h.d1 = __ldg(A.draw_offsets + job.s + 1);
+  h.R = row_params(A, job.s);
   h.sample = make_uint4(0, 0, 0, 0);
   if (A.vocab > kCap) {
-    const Slice<HALF, CL> t = slice_of<HALF, CL>(A, s, rank);
-    const int n = t.vec1 - t.vec0, at = (threadIdx.x >> 5) * (n / kListWarps) + (threadIdx.x & 31);
+    const Slice<HALF> t = slice_of<HALF>(A, job.s, job.part, job.parts);
+    const int n = t.vec1 - t.vec0, at = (tid >> 5) * (n / kListWarps) + (tid & 31);
     if (n > 0) h.sample = __ldg(t.vecs + t.vec0 + min(at, n - 1));
   }
   return h;
 }
-
-// Row s, whose head is `H`; `next`: the row behind it (its head is left in H), or -1.
-template <bool HALF, int CL>
-__device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& H, int s, int next) {
-  constexpr int kVec = Slice<HALF, CL>::kVec;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = A.vocab;
-  cg::cluster_group cl = cg::this_cluster();
-  const int rank = CL > 1 ? static_cast<int>(cl.block_rank()) : 0;
-  const int64_t d0 = H.d0, d1 = H.d1;
-  const RowParams R = H.R;
-  if (d1 <= d0 && !A.kept_out) {
-    if (tid == 0 && rank == 0) A.marks[s] = 0;
-    if (next >= 0) H = row_head<HALF, CL>(A, next, rank);
-    return;
-  }
-  const Slice<HALF, CL> L = slice_of<HALF, CL>(A, s, rank);
-  const void* row = L.row;
-  const uint4* vecs = L.vecs;
-  const int lead = L.lead, n_vec = L.n_vec, vec0 = L.vec0, vec1 = L.vec1;
-  const bool fine = R.temperature >= 0.f && R.temperature < INFINITY;
-  const bool greedy = R.temperature == 0.f || R.top_k == 1 || R.top_p <= 0.f;
-  const bool by_k = R.top_k > 0 && R.top_k < V;
-  const int here = (vec1 - vec0) * kVec;
-  const bool whole = V <= kCap;                                // every finite logit goes on the list
-  const bool add_up = fine && !greedy && !whole && !by_k && R.top_p < 1.f;
-  // ---- threshold
-  if (tid == 0) { S.n = 0; S.low = kLowest; }
-  if (!whole) {
-    float m = -INFINITY;
-    if (here > 0) {
-      float x[kVec];
-      unpack<HALF>(H.sample, x);
+// The buffer for a job's pass: its threshold (the threads of lists).
+template <bool HALF>
+__device__ __forceinline__ void begin_row(const Args& A, ListShared& S, RowBuffer& B, const Job& job, const RowHead& H) {
+  constexpr int kVec = Slice<HALF>::kVec;
+  const int tid = threadIdx.x % kListThreads, lane = tid & 31;
+  const RowKind K = kind_of(H.R, A.vocab);
+  list_sync();
+  if (!K.whole) {
+    float x[kVec], m = -INFINITY;
+    unpack<HALF>(H.sample, x);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) m = fmaxf(m, x[i]);
-    }
+    for (int i = 0; i < kVec; ++i) m = fmaxf(m, x[i]);
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     if ((lane & 7) == 0) S.group[tid >> 3] = m;
+    list_sync();
   }
-  __syncthreads();
-  if (!whole && warp == 0) {
-    // Candidates wanted: top-k says how many it needs, min-p needs few, top-p of the whole row may need many.  (A list for the
-    // cluster's first block has to take them all.)
-    const float want = (by_k ? fminf(fmaxf(512.f, 2.f * static_cast<float>(R.top_k)), 4096.f) : R.min_p > 0.f ? 1024.f : 4096.f) / CL;
-    const float share = fminf(want / static_cast<float>(max(here, 1)), 1.f);
+  if (tid >= 32) return;
+  float low = kLowest, base = 0.f;
+  if (!K.whole) {
+    const Slice<HALF> t = slice_of<HALF>(A, job.s, job.part, job.parts);
+    // Candidates wanted: top-k says how many it needs, min-p needs few, top-p of the whole row may need many.
+    const float want = (K.by_k ? fminf(fmaxf(512.f, 2.f * static_cast<float>(H.R.top_k)), 4096.f) : H.R.min_p > 0.f ? 512.f : 4096.f) / job.parts;
+    const float share = fminf(want / static_cast<float>(max((t.vec1 - t.vec0) * kVec, 1)), 1.f);
     const int at = min(static_cast<int>(kGroups * __expf(-8.f * kVec * share)), kGroups - 1);
-#pragma unroll
-    for (int x = 0; x < kGroups; x += 32) {
-      const float m = S.group[lane + x];
-      int below = 0;
-      for (int i = 0; i < kGroups; ++i) {
-        const float o = S.group[i];
-        below += o < m || (o == m && i < lane + x) ? 1 : 0;
-      }
-      if (below == at && m > kLowest) S.low = m;
+    const float m0 = S.group[lane], m1 = S.group[lane + 32];
+    int below0 = 0, below1 = 0;
+    for (int i = 0; i < kGroups; ++i) {
+      const float o = S.group[i];
+      below0 += o < m0 || (o == m0 && i < lane) ? 1 : 0;
+      below1 += o < m1 || (o == m1 && i < lane + 32) ? 1 : 0;
+    }
+    const float mine = below0 == at ? m0 : below1 == at ? m1 : -INFINITY;
+    low = fmaxf(warp_max(mine), kLowest);                      // (one lane has it)
+    if (K.add_up) {
+      double c;
+      base = rintf(fminf(fmaxf(warp_max(fmaxf(m0, m1)) * quick_of(H.R, 0.f, c).c_hi, -1e6f), 1e6f));
     }
   }
-  __syncthreads();
-  const float low = S.low;
-  float base = 0.f;
-  double c = 0.0;
-  Quick quick{0.f, 0.f, 0.f, 0.f};
-  if (add_up) {
-    c = 1.4426950408889634 / static_cast<double>(R.temperature);
-    quick.c_hi = static_cast<float>(c);
-    quick.c_lo = static_cast<float>(c - static_cast<double>(quick.c_hi));
-    float top = S.group[lane];
-    top = warp_max(fmaxf(top, S.group[lane + 32]));
-    base = rintf(fminf(fmaxf(top * quick.c_hi, -1e6f), 1e6f)); // (the same in all lanes)
-    quick.shift = 12582912.f - base;                           // 1.5 * 2^23
-    quick.low = (base - 124.f) / quick.c_hi;
+  if (lane == 0) {
+    B.n = 0;
+    B.low = low;
+    B.base = base;
+    B.skip = H.d1 <= H.d0 && !A.kept_out;
+    B.d0 = H.d0;
+    B.d1 = H.d1;
+    B.R = H.R;
   }
+}
 
-  // ---- the pass
+// One pass over a job's logits (the first kListThreads threads).
+template <bool HALF>
+__device__ __forceinline__ void pass_row(const Args& A, uint4 (&ring)[4][32], RowBuffer& B, const Job& job) {
+  constexpr int kVec = Slice<HALF>::kVec;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = A.vocab;
+  if (B.skip) return;
+  const Slice<HALF> L = slice_of<HALF>(A, job.s, job.part, job.parts);
+  const RowParams R = B.R;
+  const float low = B.low, base = B.base;
+  const bool add_up = kind_of(R, V).add_up, rough = kind_of(R, V).rough;
+  double c;
+  const Quick quick = add_up ? quick_of(R, base, c) : Quick{0.f, 0.f, 0.f, 0.f};
   float mx = -INFINITY;
   double z = 0.0;
   auto single = [&](int v) {
-    const float x = load_logit<HALF>(row, v);
+    const float x = load_logit<HALF>(L.row, v);
     mx = max_nan(mx, x);
     if (x >= low) {                                            // (a NaN is not taken)
-      const unsigned at = atomicAdd(&S.n, 1u);
-      if (at < kCap) S.list[at] = entry_of(x, v);
+      const unsigned at = atomicAdd(&B.n, 1u);
+      if (at < kCap) B.list[at] = entry_of(x, v);
     }
     if (add_up) {
       float a, b;
@@ -885,20 +916,42 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
       z += static_cast<double>(a);
     }
   };
-  if (rank == 0 && tid < lead) single(tid);
-  if (rank == CL - 1 && tid < V - lead - n_vec * kVec) single(lead + n_vec * kVec + tid);
-  constexpr int kVecs = HALF ? 2 : 4;                          // vectors of a lane at a time: 16 tokens
-  for (int v0 = vec0 + warp * (32 * kVecs); v0 < vec1; v0 += kListWarps * 32 * kVecs) {
-    uint4 u[kVecs];
+  if (job.part == 0 && tid < L.lead) single(tid);
+  if (job.part == job.parts - 1 && tid < V - L.lead - L.n_vec * kVec) single(L.lead + L.n_vec * kVec + tid);
+  const uint4 nothing = HALF ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
+                             : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);   // -inf
+  const uint32_t slot = static_cast<uint32_t>(__cvta_generic_to_shared(&ring[0][lane]));
+  auto fetch = [&](int v0) {
+    const uint4* from = L.vecs + v0 + lane;
+    const bool full = v0 + 128 <= L.vec1;                      // (warp-uniform)
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      const int at = v0 + j * 32 + lane;
-      u[j] = at < vec1 ? __ldg(vecs + at) : HALF ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
-                                                 : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+    for (int j = 0; j < 4; ++j)
+      if (full || v0 + j * 32 + lane < L.vec1)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot + j * 512), "l"(from + j * 32) : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  constexpr int kStep = kListWarps * 128;
+  int v0 = L.vec0 + warp * 128;
+  if (v0 < L.vec1) fetch(v0);
+  for (; v0 < L.vec1; v0 += kStep) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    uint4 u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = ring[j][lane];
+    if (v0 + 128 > L.vec1) {                                   // past the end: nothing
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (v0 + j * 32 + lane >= L.vec1) u[j] = nothing;
     }
+    __syncwarp();
+    if (v0 + kStep < L.vec1) fetch(v0 + kStep);
+    // 16 tokens at a time
+#pragma unroll
+    for (int g = 0; g < (HALF ? 2 : 1); ++g) {
+    constexpr int kVecs = HALF ? 2 : 4;                        // vectors of them
     float x[16];
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) unpack<HALF>(u[j], x + j * kVec);
+    for (int j = 0; j < kVecs; ++j) unpack<HALF>(u[g * kVecs + j], x + j * kVec);
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < 15; i += 2) top = max3_nan(top, x[i], x[i + 1]);
@@ -907,13 +960,29 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
 #pragma unroll
     for (int i = 0; i < 16; ++i) hits |= x[i] >= low ? 1u << i : 0u;
     if (hits) {
-      unsigned at = atomicAdd(&S.n, static_cast<unsigned>(__popc(hits)));
+      unsigned at = atomicAdd(&B.n, static_cast<unsigned>(__popc(hits)));
       for (; hits; hits &= hits - 1, ++at) {
         const int i = __ffs(hits) - 1;
-        if (at < kCap) S.list[at] = entry_of(pick16(x, i), lead + (v0 + (i / kVec) * 32 + lane) * kVec + i % kVec);
+        if (at < kCap) B.list[at] = entry_of(pick16(x, i), L.lead + (v0 + (g * kVecs + i / kVec) * 32 + lane) * kVec + i % kVec);
       }
     }
-    if (add_up) {
+    if (add_up && rough) {
+      const f32x2 c_hi = both(quick.c_hi), shift = both(-base);
+#pragma unroll
+      for (int h = 0; h < 16; h += 8) {
+        float e[8];
+#pragma unroll
+        for (int y = 0; y < 8; y += 2) {
+          float x0, x1;
+          unpack2(fma2(pack2(x[h + y], x[h + y + 1]), c_hi, shift), x0, x1);
+          e[y] = ex2(x0);
+          e[y + 1] = ex2(x1);
+        }
+        float a, b;
+        unpack2(add2(add2(pack2(e[0], e[1]), pack2(e[2], e[3])), add2(pack2(e[4], e[5]), pack2(e[6], e[7]))), a, b);
+        z += static_cast<double>(a + b);
+      }
+    } else if (add_up) {
       float least = x[0];
 #pragma unroll
       for (int i = 1; i < 15; i += 2) least = min3(least, x[i], x[i + 1]);
@@ -930,97 +999,69 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
         z += static_cast<double>(a + b);
       }
     }
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   z = warp_sum_d(z);
-  if (lane == 0) { S.f[warp] = mx; S.d[warp] = z; }
-  __syncthreads();
-  if (next >= 0) H = row_head<HALF, CL>(A, next, rank);
-  mx = S.f[0];
-  z = S.d[0];
+  // (terms out of range: the sample was far off)
+  if (lane == 0) { B.max[warp] = mx; B.sum[warp] = !add_up || mx * quick.c_hi <= base + 100.f ? z : static_cast<double>(NAN); }
+}
+__device__ __forceinline__ void passed(const RowBuffer& B, float& mx, double& z) {
+  mx = B.max[0];
+  z = B.sum[0];
 #pragma unroll
-  for (int w = 1; w < kListWarps; ++w) { mx = max_nan(mx, S.f[w]); z += S.d[w]; }
-  if (add_up && !(mx * quick.c_hi <= base + 100.f)) z = NAN;         // (terms out of range: the sample was far off)
-  unsigned n = S.n;
-  bool fits = n <= kCap;
-  uint32_t low_key = whole ? kNegInf + 1 : key_of(low);
-  if (CL > 1) {                                                // to the first block, in the order of the blocks
-    if (tid == 0) { S.z = z; S.max = mx; S.base = base; }
-    cl.sync();
-    if (rank == 0) {
-      unsigned first[CL + 1];                                  // of every block's entries
-      first[0] = 0;
-      first[1] = n;
-#pragma unroll
-      for (int b = 1; b < CL; ++b) {
-        const ListShared* o = cl.map_shared_rank(&S, b);
-        const unsigned m = o->n;
-        if (add_up) z += o->z * exp2(static_cast<double>(o->base) - static_cast<double>(base));
-        mx = max_nan(mx, o->max);
-        if (!whole) low_key = max(low_key, key_of(o->low));
-        fits = fits && m <= kCap;
-        first[b + 1] = first[b] + m;
-      }
-      n = first[CL];
-      fits = fits && n <= kCap;
-      if (fits) {
-        for (unsigned i = first[1] + tid; i < n; i += kListThreads) {
-          int b = 1;
-#pragma unroll
-          for (int x = 2; x < CL; ++x) b += i >= first[x] ? 1 : 0;
-          unsigned from = first[1];
-#pragma unroll
-          for (int x = 2; x < CL; ++x) from = b == x ? first[x] : from;
-          S.list[i] = cl.map_shared_rank(&S, b)->list[i - from];
-        }
-      }
-    }
-    cl.sync();
-    if (rank) return;
-    __syncthreads();
-  }
+  for (int w = 1; w < kListWarps; ++w) { mx = max_nan(mx, B.max[w]); z += B.sum[w]; }
+}
 
+// Row s from its list (all of it): false, and nothing given, where the list cannot tell.
+__device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned long long* list, int s, int64_t d0, int64_t d1, const RowParams& R,
+                                         int m_list, bool fits, float low, float mx, double z, float base) {
+  const int tid = threadIdx.x % kListThreads, lane = tid & 31, warp = tid >> 5;
+  const RowKind K = kind_of(R, A.vocab);
+  const bool fine = K.fine, greedy = K.greedy, by_k = K.by_k, whole = K.whole, add_up = K.add_up;
+  uint32_t low_key = whole ? kNegInf + 1 : key_of(low);
   // ---- the border
   auto give_all = [&](int token, int kept) {
     for (int64_t d = d0 + tid; d < d1; d += kListThreads) {
       A.tokens_out[d] = token;
       if (A.seq_out) A.seq_out[d] = s;
     }
-    if (tid == 0) {
-      if (A.kept_out) A.kept_out[s] = kept;
-      A.marks[s] = 0;
-    }
+    if (tid == 0 && A.kept_out) A.kept_out[s] = kept;
   };
   if (!fine || !(mx < INFINITY) || mx == -INFINITY) {          // (a NaN is not less)
     give_all(-1, 0);
-    return;
+    return true;
   }
   const uint32_t max_key = key_of(mx);
-  const int m_list = static_cast<int>(n);
   Term e;
   e.max = static_cast<double>(mx);
   e.inv_t = greedy ? 1.0 : 1.0 / static_cast<double>(R.temperature);
   auto fixed = [&](uint32_t k) { return __double2ull_rn(e(logit_of(k)) * kFix); };
   const bool limit = !greedy && by_k && !(whole && R.top_k >= m_list);            // top-k leaves something out
   const bool by_p = !greedy && R.top_p < 1.f, by_m = !greedy && R.min_p > 0.f;
-  const double total_quick = add_up ? z * exp2(static_cast<double>(base) - e.max * c) : 0.0;
-  double* sums = reinterpret_cast<double*>(S.list);            // (behind the borders: running sums of the kept ones, beside S.token)
+  const double total_quick = add_up ? z * exp2(static_cast<double>(base) - e.max * (1.4426950408889634 / static_cast<double>(R.temperature))) : 0.0;
+  double* sums = reinterpret_cast<double*>(list);            // (behind the borders: running sums of the kept ones, beside S.token)
   int kept = 0;
 
   // ---- few candidates (what no filter can keep left out): in order, a thread each
+  double error_quick = 0.0;
+  if (add_up) {
+    const double c = 1.4426950408889634 / static_cast<double>(R.temperature);
+    error_quick = K.rough ? rough_error(base, fabs(e.max * c - base), A.vocab) : kSumError;
+  }
   bool sure = fits && (!by_p || limit || whole || add_up);
   if (sure) {
     uint32_t head = greedy ? max_key : low_key, m_key = 0;     // they have at least the key `head`
-    double total = total_quick, error = by_p && !limit ? kSumError : 0.0;
+    double total = total_quick, error = error_quick;
     if (whole) {
       if (tid == 0) S.min_key = max_key;
-      __syncthreads();
+      list_sync();
       uint32_t lowest = max_key;
-      for (int i = tid; i < m_list; i += kListThreads) lowest = min(lowest, static_cast<uint32_t>(S.list[i] >> 32));
+      for (int i = tid; i < m_list; i += kListThreads) lowest = min(lowest, static_cast<uint32_t>(list[i] >> 32));
       lowest = __reduce_min_sync(0xffffffffu, lowest);
       if (lane == 0) atomicMin(&S.min_key, lowest);
-      __syncthreads();
+      list_sync();
       low_key = S.min_key;
       if (!greedy) head = low_key;
     }
@@ -1034,14 +1075,14 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
       const uint32_t range = max_key - low_key;
       const int shift = range < kBins ? 0 : 32 - __clz(range) - 9;
       for (int i = tid; i < m_list; i += kListThreads) {
-        const uint32_t k = static_cast<uint32_t>(S.list[i] >> 32);
+        const uint32_t k = static_cast<uint32_t>(list[i] >> 32);
         if (k < low_key) continue;
         const uint32_t b = (k - low_key) >> shift;
         if (limit) atomicAdd(&S.count[b], 1u);
         else atomicAdd(&S.mass[b], fixed(k));
       }
       if (tid == 0) S.bin = 0;
-      __syncthreads();
+      list_sync();
       const int bin = kBins - 1 - tid;
       const unsigned long long here = limit ? static_cast<unsigned long long>(S.count[bin]) : S.mass[bin];
       S.count[bin] = 0;
@@ -1053,18 +1094,18 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
         if (lane >= o) incl += up;
       }
       if (lane == 31) S.u[warp] = incl;
-      __syncthreads();
+      list_sync();
       incl += warps_before(S.u, warp, lane);
       if (whole && !limit) {                                   // (the list is all there is)
         if (tid == kListThreads - 1) S.all = incl;
-        __syncthreads();
+        list_sync();
         total = static_cast<double>(S.all) / kFix;
         error = kFixError;
       }
       const double far = static_cast<double>(R.top_p) * total * (1.0 + 2.0 * error) * kFix;
       const unsigned long long target = limit ? static_cast<unsigned long long>(R.top_k) : far < 1.8e19 ? __double2ull_ru(far) : ~0ull;
       if (incl >= target && incl - here < target) S.bin = bin;
-      __syncthreads();
+      list_sync();
       // (top-p's share is of all that top-k keeps: min-p must not shorten those then)
       const uint32_t to = low_key + (S.bin << shift);
       head = limit && by_p ? to : max(head, to);
@@ -1072,26 +1113,26 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
       head = low_key;                                          // (all of a short list)
     }
     if (tid == 0) S.moved = 0;
-    __syncthreads();
+    list_sync();
     for (int i = tid; i < m_list; i += kListThreads) {
-      if (static_cast<uint32_t>(S.list[i] >> 32) >= head) {
+      if (static_cast<uint32_t>(list[i] >> 32) >= head) {
         const unsigned at = atomicAdd(&S.moved, 1u);
         if (at < kListThreads) S.token[at] = static_cast<uint32_t>(i);
       }
     }
-    __syncthreads();
+    list_sync();
     const int h = static_cast<int>(S.moved);
     if (h <= kListThreads) {
       // in order: largest logit first, equal ones by index
-      unsigned long long y = tid < h ? S.list[S.token[tid]] ^ 0xffffffffull : 0;
+      unsigned long long y = tid < h ? list[S.token[tid]] ^ 0xffffffffull : 0;
       if (tid < h) S.mass[tid] = y;
-      __syncthreads();
+      list_sync();
       int at = 0;
       if (tid < h)
         for (int j = 0; j < h; ++j) at += S.mass[j] > y ? 1 : 0;
-      __syncthreads();
+      list_sync();
       if (tid < h) S.mass[at] = y;
-      __syncthreads();
+      list_sync();
       y = tid < h ? S.mass[tid] : 0;
       S.mass[tid] = 0;
       const double mine = tid < h ? e(logit_of(static_cast<uint32_t>(y >> 32))) : 0.0;
@@ -1101,7 +1142,7 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
       if (limit && R.top_k <= h) end = min(end, R.top_k);
       if (!limit && whole && h == m_list) end = min(end, h);
       if (by_m) {
-        const int passing = max(__syncthreads_count(tid < h && mine >= static_cast<double>(R.min_p)), 1);
+        const int passing = max(list_count(tid < h && mine >= static_cast<double>(R.min_p)), 1);
         if (passing < h || (head <= m_key && m_key >= low_key)) end = min(end, passing);
       }
       if (by_p) {
@@ -1110,11 +1151,11 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
           sure = false;
         } else {
           if (tid == n - 1) S.z = sum;
-          __syncthreads();
+          list_sync();
           if (limit || (whole && h == m_list)) { total = S.z; error = 0.0; }
           const double target = static_cast<double>(R.top_p) * total;
-          const int least = 1 + __syncthreads_count(tid < n && sum < target * (1.0 - error));
-          const int most = 1 + __syncthreads_count(tid < n && sum < target * (1.0 + error));
+          const int least = 1 + list_count(tid < n && sum < target * (1.0 - error));
+          const int most = 1 + list_count(tid < n && sum < target * (1.0 + error));
           if (!(target > 0.0)) sure = false;                   // (a NaN)
           else if (least == most && least <= n) end = min(end, least);
           else if (least <= n) sure = end <= least;            // too close to tell, unless something else ends before
@@ -1124,35 +1165,26 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
         kept = end;
         const uint32_t v = ~static_cast<uint32_t>(y);
         if (tid < kept) S.token[tid] = v;
-        __syncthreads();
+        list_sync();
         int place = 0;
         if (tid < kept)
           for (int j = 0; j < kept; ++j) place += S.token[j] < v ? 1 : 0;
-        __syncthreads();
+        list_sync();
         if (tid < kept) {
           S.token[place] = v;
           sums[place] = mine;
         }
-        __syncthreads();
+        list_sync();
         const double running = block_scan_d(S.d, tid < kept ? sums[tid] : 0.0, warp, lane);
         if (tid < kept) sums[tid] = running;
-        __syncthreads();
+        list_sync();
       }
     }
   }
-  if (!sure) {
-    if (tid == 0) A.marks[s] = 1;
-    return;
-  }
-  if (kept == 0) kept = wide_list(S, R, e, m_list, low_key, max_key, limit, greedy, whole, add_up, total_quick);
-  if (kept == 0) {
-    if (tid == 0) A.marks[s] = 1;
-    return;
-  }
-  if (tid == 0) {
-    if (A.kept_out) A.kept_out[s] = kept;
-    A.marks[s] = 0;
-  }
+  if (!sure) return false;
+  if (kept == 0) kept = wide_list(S, list, R, e, m_list, low_key, max_key, limit, greedy, whole, add_up, total_quick, error_quick);
+  if (kept == 0) return false;
+  if (tid == 0 && A.kept_out) A.kept_out[s] = kept;
   const double total = sums[kept - 1];
   for (int64_t d = d0 + tid; d < d1; d += kListThreads) {
     const float u = __ldg(A.uniforms + d);
@@ -1169,33 +1201,121 @@ __device__ __forceinline__ void list_row(const Args& A, ListShared& S, RowHead& 
     A.tokens_out[d] = static_cast<int32_t>(S.token[a]);
     if (A.seq_out) A.seq_out[d] = s;
   }
+  return true;
 }
 
-template <bool HALF, int CL>
-__device__ __forceinline__ void list_rows(const Args& A) {
-  extern __shared__ __align__(16) unsigned char list_smem[];
-  ListShared& S = *reinterpret_cast<ListShared*>(list_smem);
-  S.count[threadIdx.x] = 0;
-  S.mass[threadIdx.x] = 0;
-  const int clusters = gridDim.x / CL, rank = CL > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
-  int s = A.row0 + blockIdx.x / CL;
-  if (s >= A.n_seq) return;                                    // (the whole cluster)
-  RowHead H = row_head<HALF, CL>(A, s, rank);
-  for (; s < A.n_seq; s += clusters) {
-    list_row<HALF, CL>(A, S, H, s, s + clusters < A.n_seq ? s + clusters : -1);
-    __syncthreads();
-    if (CL > 1) cg::this_cluster().sync();
-  }
-}
+struct RowsShared {
+  RowBuffer B;
+  ListShared S;
+};
 template <bool HALF>
 __global__ void __launch_bounds__(kListThreads, 2) list_rows_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
-  list_rows<HALF, 1>(A);
+  extern __shared__ __align__(16) unsigned char smem[];
+  RowsShared& M = *reinterpret_cast<RowsShared*>(smem);
+  RowBuffer& B = M.B;
+  const int tid = threadIdx.x, block = blockIdx.x;
+  const int mine = block < A.whole_rows ? (A.whole_rows - block + gridDim.x - 1) / gridDim.x : 0;
+  const bool part = A.parts > 1 && block < (A.n_seq - A.whole_rows) * A.parts;
+  const int jobs = mine + (part ? 1 : 0);
+  if (jobs == 0) return;
+  auto job_of = [&](int j) {
+    return j < mine ? Job{block + j * static_cast<int>(gridDim.x), 0, 1} : Job{A.whole_rows + block / A.parts, block % A.parts, A.parts};
+  };
+  M.S.count[tid] = 0;
+  M.S.mass[tid] = 0;
+  RowHead H = row_head<HALF>(A, job_of(0));
+  for (int j = 0; j < jobs; ++j) {
+    const Job job = job_of(j);
+    begin_row<HALF>(A, M.S, B, job, H);
+    list_sync();
+    pass_row<HALF>(A, M.S.ring[tid >> 5], B, job);
+    list_sync();
+    if (j + 1 < jobs) H = row_head<HALF>(A, job_of(j + 1));
+    if (!B.skip) {
+      float mx;
+      double z;
+      passed(B, mx, z);
+      if (job.parts == 1) {
+        const bool done = list_row(A, M.S, B.list, job.s, B.d0, B.d1, B.R, static_cast<int>(min(B.n, static_cast<unsigned>(kCap))), B.n <= kCap,
+                                   B.low, mx, z, B.base);
+        if (tid == 0) A.marks[job.s] = done ? 0 : 1;
+      } else {
+        Part& P = A.part[block];
+        for (unsigned i = tid; i < min(B.n, static_cast<unsigned>(kPartCap)); i += kListThreads) P.list[i] = B.list[i];
+        if (tid == 0) { P.n = B.n; P.low = B.low; P.base = B.base; P.max = mx; P.sum = z; }
+      }
+    } else if (tid == 0 && job.parts == 1) {
+      A.marks[job.s] = 0;
+    }
+  }
 }
-template <bool HALF, int CL>
-__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(kListThreads, 2) list_cluster_kernel(const __grid_constant__ Args A) {
+
+// The rows that were split, from the lists of their parts, and all that a list was not enough for.
+struct FinishShared {
+  union {
+    unsigned long long list[kCap];
+    WholeShared whole;
+  };
+  ListShared S;
+};
+template <bool HALF>
+__global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
-  list_rows<HALF, CL>(A);
+  static_assert(kThreads == kListThreads, "the threads of a list go through whole rows");
+  extern __shared__ __align__(16) unsigned char smem[];
+  FinishShared& M = *reinterpret_cast<FinishShared*>(smem);
+  const int tid = threadIdx.x;
+  M.S.count[tid] = 0;
+  M.S.mass[tid] = 0;
+  __syncthreads();
+  for (int s = A.whole_rows + blockIdx.x; s < A.n_seq; s += gridDim.x) {
+    const int64_t d0 = __ldg(A.draw_offsets + s), d1 = __ldg(A.draw_offsets + s + 1);
+    if (d1 <= d0 && !A.kept_out) continue;
+    const RowParams R = row_params(A, s);
+    const Part* parts = A.part + static_cast<int64_t>(s - A.whole_rows) * A.parts;
+    const bool add_up = kind_of(R, A.vocab).add_up;
+    // a lane a part (every warp for itself): counts, sums, in the order of the parts
+    const int lane = tid & 31, warp = tid >> 5;
+    const bool has = lane < A.parts;
+    const unsigned m = has ? parts[lane].n : 0;
+    unsigned first = m;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned up = __shfl_up_sync(0xffffffffu, first, o);
+      if (lane >= o) first += up;
+    }
+    const unsigned n = __shfl_sync(0xffffffffu, first, 31);
+    first -= m;
+    const bool fits = __all_sync(0xffffffffu, m <= kPartCap) && n <= kCap;
+    float mx = has ? parts[lane].max : -INFINITY;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float low = warp_max(has ? parts[lane].low : kLowest), base = parts[0].base;
+    const double z = warp_sum_d(has && add_up ? parts[lane].sum * exp2(static_cast<double>(parts[lane].base) - static_cast<double>(base)) : 0.0);
+    if (fits) {
+      for (int p = warp; p < A.parts; p += kListWarps) {
+        const unsigned count = __shfl_sync(0xffffffffu, m, p), to = __shfl_sync(0xffffffffu, first, p);
+        for (unsigned i = lane; i < count; i += 32) M.list[to + i] = parts[p].list[i];
+      }
+    }
+    __syncthreads();
+    const bool done = list_row(A, M.S, M.list, s, d0, d1, R, fits ? static_cast<int>(n) : 0, fits, low, mx, z, base);
+    __syncthreads();
+    if (!done) {
+      whole_row<HALF>(A, M.whole, s);
+      __syncthreads();
+    }
+  }
+  // the marks of 32 rows of this block at a time
+  for (int64_t s0 = blockIdx.x; s0 < A.whole_rows; s0 += static_cast<int64_t>(gridDim.x) * 32) {
+    const int64_t mine = s0 + static_cast<int64_t>(tid & 31) * gridDim.x;
+    unsigned marked = __ballot_sync(0xffffffffu, mine < A.whole_rows && A.marks[mine] != 0);
+    for (; marked; marked &= marked - 1) {
+      whole_row<HALF>(A, M.whole, static_cast<int>(s0 + static_cast<int64_t>(__ffs(marked) - 1) * gridDim.x));
+      __syncthreads();
+    }
+  }
 }
 
 static int32_t check(const ss_sample_desc_t* d) {
@@ -1205,82 +1325,46 @@ static int32_t check(const ss_sample_desc_t* d) {
   if (d->vocab > kMaxVocab) return SS_ERR_UNSUPPORTED;
   return SS_OK;
 }
-static size_t workspace_bytes_of(const ss_sample_desc_t* d) { return align_up(sizeof(int32_t) * (static_cast<size_t>(d->n_seq) + 64)); }
-
+static size_t carve(const ss_sample_desc_t* d, void* base, Args* A) {
+  Carver c(base);
+  A->marks = c.take<int32_t>(static_cast<size_t>(d->n_seq) + 1);
+  A->part = c.take<Part>(2 * static_cast<size_t>(sm_count_of_current_device()));
+  return c.off;
+}
 template <typename Kernel>
-static int32_t prepare(Kernel kernel, bool (&done)[kDeviceSlots]) {
+static int32_t prepare(Kernel kernel, size_t smem, bool (&done)[kDeviceSlots]) {
   const int slot = current_device_slot();
   if (slot >= 0 && done[slot]) return SS_OK;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(ListShared))) != cudaSuccess) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) {
     (void)cudaGetLastError();
     return SS_ERR_CUDA;
   }
   if (slot >= 0) done[slot] = true;
   return SS_OK;
 }
-template <bool HALF, int CL>
-static int32_t launch_clusters(const Args& A, int rows, cudaStream_t st) {
-  static bool done[kDeviceSlots] = {false};
-  const int32_t rc = prepare(list_cluster_kernel<HALF, CL>, done);
-  if (rc != SS_OK) return rc;
-  SS_LAUNCH((list_cluster_kernel<HALF, CL>), rows * CL, kListThreads, sizeof(ListShared), st, A);
-  return SS_OK;
-}
-// Clusters that fit the device at once.
-template <bool HALF, int CL>
-static int resident_clusters() {
-  static int cached[kDeviceSlots] = {0};
-  const int slot = current_device_slot();
-  if (slot >= 0 && cached[slot] > 0) return cached[slot];
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = CL;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(CL);
-  cfg.blockDim = dim3(kListThreads);
-  cfg.dynamicSmemBytes = sizeof(ListShared);
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  static bool done[kDeviceSlots] = {false};
-  int n = 0;
-  if (prepare(list_cluster_kernel<HALF, CL>, done) != SS_OK ||
-      cudaOccupancyMaxActiveClusters(&n, list_cluster_kernel<HALF, CL>, &cfg) != cudaSuccess || n < 1) {
-    (void)cudaGetLastError();
-    n = sm_count_of_current_device() / CL;
-  }
-  if (slot >= 0) cached[slot] = n;
-  return n;
-}
-// Whole rounds of a row per block, what is left over on clusters that fill the machine, then the marked rows.
+// Whole rounds of a row per block, what is left over in parts (of 4096 tokens at least; none where they would be only one), then the
+// kernel that finishes what these leave.
 template <bool HALF>
 static int32_t launch(Args A, cudaStream_t st) {
+  static bool done_rows[kDeviceSlots] = {false}, done_finish[kDeviceSlots] = {false};
+  int32_t rc = prepare(list_rows_kernel<HALF>, sizeof(RowsShared), done_rows);
+  if (rc == SS_OK) rc = prepare(finish_rows_kernel<HALF>, sizeof(FinishShared), done_finish);
+  if (rc != SS_OK) return rc;
   const int blocks = 2 * sm_count_of_current_device();
-  const int whole = A.n_seq / blocks * blocks, n_seq = A.n_seq;
-  int rest = n_seq - whole;
-  int size = rest <= resident_clusters<HALF, 8>() ? 8 : rest <= resident_clusters<HALF, 4>() ? 4 : rest <= resident_clusters<HALF, 2>() ? 2 : 1;
-  while (size > 1 && A.vocab < 4096 * size) size /= 2;         // (a slice of a short row is not worth a block)
-  const int first = size == 1 ? n_seq : whole;                 // rows of one block each
-  int32_t rc = SS_OK;
-  if (first > 0) {
-    static bool done[kDeviceSlots] = {false};
-    rc = prepare(list_rows_kernel<HALF>, done);
-    if (rc != SS_OK) return rc;
-    A.row0 = 0;
-    A.n_seq = first;
-    SS_LAUNCH(list_rows_kernel<HALF>, first < blocks ? first : blocks, kListThreads, sizeof(ListShared), st, A);
+  A.whole_rows = A.n_seq / blocks * blocks;
+  int rest = A.n_seq - A.whole_rows;
+  A.parts = rest > 0 && A.vocab > kCap ? blocks / rest : 1;
+  if (A.parts > A.vocab / 4096) A.parts = A.vocab / 4096;
+  if (A.parts > 32) A.parts = 32;                              // (a lane each)
+  if (A.parts < 2) {
+    A.parts = 1;
+    A.whole_rows = A.n_seq;
+    rest = 0;
   }
-  rest = n_seq - first;
-  if (rest > 0) {
-    A.row0 = first;
-    A.n_seq = n_seq;
-    rc = size == 8 ? launch_clusters<HALF, 8>(A, rest, st) : size == 4 ? launch_clusters<HALF, 4>(A, rest, st) : launch_clusters<HALF, 2>(A, rest, st);
-    if (rc != SS_OK) return rc;
-  }
-  A.row0 = 0;
-  A.n_seq = n_seq;
-  const int most = sm_count_of_current_device();
-  SS_LAUNCH(whole_rows_kernel<HALF>, n_seq < most ? n_seq : most, kThreads, 0, st, A);
+  const int grid = A.whole_rows >= blocks ? blocks : A.whole_rows > rest * A.parts ? A.whole_rows : rest * A.parts;
+  SS_LAUNCH(list_rows_kernel<HALF>, grid, kListThreads, sizeof(RowsShared), st, A);
+  const int finish = A.n_seq < blocks ? A.n_seq : blocks;
+  SS_LAUNCH(finish_rows_kernel<HALF>, finish, kListThreads, sizeof(FinishShared), st, A);
   return SS_OK;
 }
 
@@ -1292,7 +1376,8 @@ extern "C" int32_t ss_filtered_sample_workspace_bytes(const ss_sample_desc_t* de
   if (!out_bytes) return SS_ERR_INVALID_ARG;
   const int32_t rc = check(desc);
   if (rc != SS_OK) return rc;
-  *out_bytes = workspace_bytes_of(desc);
+  Args A = {};
+  *out_bytes = carve(desc, nullptr, &A);
   return SS_OK;
 }
 
@@ -1301,11 +1386,11 @@ extern "C" int32_t ss_filtered_sample(const ss_sample_desc_t* d, void* workspace
   const int32_t rc = check(d);
   if (rc != SS_OK) return rc;
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % ss::kAlign) return SS_ERR_INVALID_ARG;
-  if (workspace_bytes < workspace_bytes_of(d)) return SS_ERR_WORKSPACE_TOO_SMALL;
+  Args A = {};
+  if (workspace_bytes < carve(d, workspace, &A)) return SS_ERR_WORKSPACE_TOO_SMALL;
   if (d->n_seq == 0) return SS_OK;
   if (!d->logits || !d->draw_offsets) return SS_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(d->logits) % (d->logits_type == SS_LOGITS_BF16 ? 2 : 4)) return SS_ERR_UNSUPPORTED;
-  Args A = {};
   A.logits = d->logits;
   A.draw_offsets = d->draw_offsets;
   A.uniforms = d->uniforms;
@@ -1323,6 +1408,5 @@ extern "C" int32_t ss_filtered_sample(const ss_sample_desc_t* d, void* workspace
   A.top_k_all = d->top_k_all;
   A.n_seq = d->n_seq;
   A.vocab = d->vocab;
-  A.marks = static_cast<int32_t*>(workspace);
   return d->logits_type == SS_LOGITS_BF16 ? launch<true>(A, ss::as_stream(stream)) : launch<false>(A, ss::as_stream(stream));
 }
