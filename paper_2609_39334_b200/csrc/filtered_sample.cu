@@ -76,10 +76,36 @@ struct Border {
 };
 __device__ __forceinline__ bool less(const Border& a, const Border& b) { return a.key > b.key || (a.key == b.key && a.ties < b.ties); }
 
-struct Term {                                  // e_v of a row
-  double max, inv_t;
-  __device__ __forceinline__ double operator()(float x) const { return exp((static_cast<double>(x) - max) * inv_t); }
+// e_v of a row: K = the integer nearest to 128 x for x = (logit - max) log2(e) / T, r = 128 x - K, 2^(K / 128) from a table of 128
+// entries and an integer addition to the exponent, 2^(r / 128) by a polynomial of degree 4 (as the branch sampler's; after Tang,
+// "Table-driven implementation of the exponential function in IEEE floating-point arithmetic", ACM TOMS 15, 1989): 2e-16 of itself, in
+// a sixth of the instructions of exp.  Terms below 2^-1000 count as that.
+constexpr int kTable = 128;
+struct Term {
+  double max, c, lowest;                       // c: 128 log2(e) / T
+  const double* table;                         // shared memory
+  __device__ __forceinline__ double operator()(float x) const {
+    constexpr double a1 = 0.005415212348124257, a2 = 1.466226238764014e-05, a3 = 2.6466431340771855e-08, a4 = 3.5830331985890313e-11;
+    constexpr double kRound = 6755399441055744.0;              // 1.5 * 2^52
+    const double d = fmax(static_cast<double>(x) - max, lowest);
+    const double k = fma(d, c, kRound), r = fma(d, c, kRound - k);
+    const int bits = __double2loint(k);
+    const double t0 = table[bits & (kTable - 1)];
+    const double t = __hiloint2double(__double2hiint(t0) + ((bits >> 7) << 20), __double2loint(t0));
+    return fma(t * r, fma(fma(fma(a4, r, a3), r, a2), r, a1), t);
+  }
 };
+__device__ __forceinline__ Term term_of(float max, float temperature, const double* table) {
+  Term e;
+  e.max = static_cast<double>(max);
+  e.c = kTable * 1.4426950408889634 / static_cast<double>(temperature);
+  e.lowest = -1000.0 * kTable / e.c;
+  e.table = table;
+  return e;
+}
+__device__ __forceinline__ void make_table(double* table) {    // (whole block; a barrier has to follow)
+  if (threadIdx.x < kTable) table[threadIdx.x] = exp2(threadIdx.x * (1.0 / kTable));
+}
 // The smallest key whose token passes min-p (e does not fall with the logit): from the logarithm, then by the definition itself, in
 // doubling steps and by halves - a step is enough but where a rounded e^x is the same for many logits.
 __device__ __noinline__ uint32_t min_p_key(const Term& e, float temperature, float min_p, uint32_t max_key) {
@@ -172,7 +198,7 @@ __device__ __forceinline__ unsigned long long block_max_u(WholeShared& S, unsign
 }
 
 template <bool HALF>
-__device__ void whole_row(const Args& A, WholeShared& S, int s) {
+__device__ void whole_row(const Args& A, WholeShared& S, const double* table, int s) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = A.vocab;
   const int64_t d0 = A.draw_offsets[s], d1 = A.draw_offsets[s + 1];
   if (d1 <= d0 && !A.kept_out) return;
@@ -203,9 +229,7 @@ __device__ void whole_row(const Args& A, WholeShared& S, int s) {
     give_all(static_cast<int>(~static_cast<uint32_t>(best)), 1);
     return;
   }
-  Term e;
-  e.max = static_cast<double>(logit_of(max_key));
-  e.inv_t = 1.0 / static_cast<double>(R.temperature);
+  const Term e = term_of(logit_of(max_key), R.temperature, table);
   // ---- top-k: the k-th largest key, eight bits at a time
   Border border{kNegInf + 1, 0x7fffffff};
   if (R.top_k > 0 && static_cast<unsigned long long>(R.top_k) < finite) {
@@ -422,7 +446,7 @@ __device__ void whole_row(const Args& A, WholeShared& S, int s) {
 
 // ---- most rows: one pass over the row, the rest on a short list --------------------------------------------------------------------
 // What is kept is nearly always among the few largest logits, so one pass collects those above a THRESHOLD in shared memory (the
-// list) and, where top-p is over the whole row, adds up all terms in fp32 with a bound (quick_pair).  The threshold comes from a
+// list) and, where top-p is over the whole row, adds up all terms in fp32 (with a bound: quick_error).  The threshold comes from a
 // sample spread over the row: of the maxima of 64 groups of n sampled tokens a share e^(-n f) lies below the value that a share f of
 // the row exceeds.  Nothing rests on it: a border found on the list is the row's if it does not lie below the threshold, and where
 // the list is too short or too long, or a sum comes too close to top-p's target to tell, the row is marked and made again by the
@@ -440,7 +464,6 @@ constexpr int kBins = 512;
 constexpr int kGroups = 64;                                    // of sampled tokens: 8 lanes each
 constexpr double kFix = 1125899906842624.0;                    // 2^50: kCap terms of at most 1 stay below 2^63
 constexpr double kFixError = 1e-11;                            // kCap * 2^-51 of the largest term, and the sums' own roundings
-constexpr double kSumError = 5e-7;                             // of the quick sum of a row, see quick_pair
 constexpr float kLowest = -3.4028235e38f;
 
 struct RowBuffer {                                             // a row between the pass and its list
@@ -454,6 +477,7 @@ struct RowBuffer {                                             // a row between 
   double sum[kListWarps];
 };
 struct ListShared {
+  double table[kTable];
   union {
     uint32_t token[kCap];
     uint4 ring[kListWarps][4][32];                             // in the pass
@@ -549,11 +573,6 @@ __device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo,
   }
 }
 
-// 2^(l c - e0) of two logits in fp32 (e0 a whole number): l * c = n + f with |f| <= 1/2, n from a sum whose low bits are the integer,
-// f exactly by an FMA with the high part of c (one rounding to 2^-26) and one with the low part, 2^f by the special-function unit
-// (documented: relative error 2^-22), n into the exponent by an integer addition.  A term is within 2.6e-7; eight terms that are
-// added pairwise (three roundings, 1.8e-7) and go to fp64 from there are within 4.4e-7 of the exact sum.  l c - e0 has to lie in
-// [-124, 100]: smaller ones are raised to `low`.
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pack2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
@@ -561,28 +580,9 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm(
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ f32x2 both(float a) { return pack2(a, a); }
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-struct Quick {
-  float c_hi, c_lo, shift, low;
-};
-__device__ __forceinline__ f32x2 quick_pair(float l0, float l1, const Quick& q) {
-  const f32x2 l = pack2(l0, l1), c = both(q.c_hi), shift = both(q.shift);
-  const f32x2 nb = fma2(l, c, shift);                          // bits: 0x4b400000 + (n - e0)
-  f32x2 f = fma2(l, c, fma2(nb, both(-1.f), shift));
-  f = fma2(l, both(q.c_lo), f);
-  float f0, f1, n0, n1;
-  unpack2(f, f0, f1);
-  unpack2(nb, n0, n1);
-  return pack2(__int_as_float(__float_as_int(ex2(f0)) + (__float_as_int(n0) << 23)), __int_as_float(__float_as_int(ex2(f1)) + (__float_as_int(n1) << 23)));
-}
-
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ float min3(float a, float b, float c) {
-  float r;
-  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 // x[i], i from 0 to 15
@@ -788,7 +788,6 @@ __device__ __forceinline__ Slice<HALF> slice_of(const Args& A, int s, int part, 
 // What a row's parameters make of it.
 struct RowKind {
   bool fine, greedy, by_k, whole, add_up;
-  bool rough;                                                  // the sum without quick_pair's reduction, see rough_error
 };
 __device__ __forceinline__ RowKind kind_of(const RowParams& R, int V) {
   RowKind k;
@@ -797,23 +796,33 @@ __device__ __forceinline__ RowKind kind_of(const RowParams& R, int V) {
   k.by_k = R.top_k > 0 && R.top_k < V;
   k.whole = V <= kCap;                                         // every finite logit goes on the list
   k.add_up = k.fine && !k.greedy && !k.whole && !k.by_k && R.top_p < 1.f;
-  k.rough = R.min_p > 0.f;                                     // (min-p is nearly always what ends such a row then: any bound will do)
   return k;
 }
-// Relative error of a sum of 2^(fma(l, c_hi, -base)): an exponent x is off by 2^-24 |x| (its rounding) and 2^-25 |l c| (that of c), and |x|
-// is at most `far` beside the largest term's and log2 V on average over the terms (the entropy of the row); the rest as for quick_pair.
-__device__ __forceinline__ double rough_error(double base, double far, int V) {
+// Relative error of a quick sum: terms 2^(fma(l, c', -base)) by the special-function unit (documented: 2^-22), c' = log2(e) / T in fp32,
+// eight added pairwise (three roundings of 2^-24), from there in fp64.  An exponent x is off by 2^-24 |x| (its rounding) and 2^-25 |l c|
+// (that of c'); |x| is at most `far` for the largest term and log2 V further on average over the terms (the entropy of the row).  About
+// 3e-6: where a row's end by top-p lies closer to a token's than that, its sum is made again in fp64 (exact_total).
+__device__ __forceinline__ double quick_error(double base, double far, int V) {
   const double x = 33 - __clz(V) + far;
-  return 0.6932 * (0x1p-24 * x + 0x1p-25 * (x + fabs(base))) + kSumError;
+  return 0.6932 * (0x1p-24 * x + 0x1p-25 * (x + fabs(base))) + 0x1p-22 + 4 * 0x1p-24;
 }
-__device__ __forceinline__ Quick quick_of(const RowParams& R, float base, double& c) {
-  Quick q;
-  c = 1.4426950408889634 / static_cast<double>(R.temperature);
-  q.c_hi = static_cast<float>(c);
-  q.c_lo = static_cast<float>(c - static_cast<double>(q.c_hi));
-  q.shift = 12582912.f - base;                                 // 1.5 * 2^23
-  q.low = (base - 124.f) / q.c_hi;
-  return q;
+__device__ __forceinline__ float quick_c(const RowParams& R) { return static_cast<float>(1.4426950408889634 / static_cast<double>(R.temperature)); }
+// The sum of all of a row's terms (the threads of a list).
+template <bool HALF>
+__device__ __noinline__ double exact_total(ListShared& S, const void* row, int V, const Term e) {
+  const int tid = threadIdx.x % kListThreads;
+  double sum = 0.0;
+#pragma unroll 8
+  for (int v = tid; v < V; v += kListThreads) sum += e(load_logit<HALF>(row, v));
+  sum = warp_sum_d(sum);
+  list_sync();
+  if ((tid & 31) == 0) S.d[tid >> 5] = sum;
+  list_sync();
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kListWarps; ++w) sum += S.d[w];
+  list_sync();
+  return sum;
 }
 struct Job {                                                   // of a block: a row or a part of one
   int s, part, parts;
@@ -874,8 +883,7 @@ __device__ __forceinline__ void begin_row(const Args& A, ListShared& S, RowBuffe
     const float mine = below0 == at ? m0 : below1 == at ? m1 : -INFINITY;
     low = fmaxf(warp_max(mine), kLowest);                      // (one lane has it)
     if (K.add_up) {
-      double c;
-      base = rintf(fminf(fmaxf(warp_max(fmaxf(m0, m1)) * quick_of(H.R, 0.f, c).c_hi, -1e6f), 1e6f));
+      base = rintf(fminf(fmaxf(warp_max(fmaxf(m0, m1)) * quick_c(H.R), -1e6f), 1e6f));
     }
   }
   if (lane == 0) {
@@ -898,9 +906,8 @@ __device__ __forceinline__ void pass_row(const Args& A, uint4 (&ring)[4][32], Ro
   const Slice<HALF> L = slice_of<HALF>(A, job.s, job.part, job.parts);
   const RowParams R = B.R;
   const float low = B.low, base = B.base;
-  const bool add_up = kind_of(R, V).add_up, rough = kind_of(R, V).rough;
-  double c;
-  const Quick quick = add_up ? quick_of(R, base, c) : Quick{0.f, 0.f, 0.f, 0.f};
+  const bool add_up = kind_of(R, V).add_up;
+  const float c = add_up ? quick_c(R) : 0.f;
   float mx = -INFINITY;
   double z = 0.0;
   auto single = [&](int v) {
@@ -910,11 +917,7 @@ __device__ __forceinline__ void pass_row(const Args& A, uint4 (&ring)[4][32], Ro
       const unsigned at = atomicAdd(&B.n, 1u);
       if (at < kCap) B.list[at] = entry_of(x, v);
     }
-    if (add_up) {
-      float a, b;
-      unpack2(quick_pair(fmaxf(x, quick.low), quick.low, quick), a, b);
-      z += static_cast<double>(a);
-    }
+    if (add_up) z += static_cast<double>(ex2(fmaf(x, c, -base)));
   };
   if (job.part == 0 && tid < L.lead) single(tid);
   if (job.part == job.parts - 1 && tid < V - L.lead - L.n_vec * kVec) single(L.lead + L.n_vec * kVec + tid);
@@ -966,36 +969,20 @@ __device__ __forceinline__ void pass_row(const Args& A, uint4 (&ring)[4][32], Ro
         if (at < kCap) B.list[at] = entry_of(pick16(x, i), L.lead + (v0 + (g * kVecs + i / kVec) * 32 + lane) * kVec + i % kVec);
       }
     }
-    if (add_up && rough) {
-      const f32x2 c_hi = both(quick.c_hi), shift = both(-base);
+    if (add_up) {
+      const f32x2 c2 = both(c), shift = both(-base);
 #pragma unroll
       for (int h = 0; h < 16; h += 8) {
         float e[8];
 #pragma unroll
         for (int y = 0; y < 8; y += 2) {
           float x0, x1;
-          unpack2(fma2(pack2(x[h + y], x[h + y + 1]), c_hi, shift), x0, x1);
+          unpack2(fma2(pack2(x[h + y], x[h + y + 1]), c2, shift), x0, x1);
           e[y] = ex2(x0);
           e[y + 1] = ex2(x1);
         }
         float a, b;
         unpack2(add2(add2(pack2(e[0], e[1]), pack2(e[2], e[3])), add2(pack2(e[4], e[5]), pack2(e[6], e[7]))), a, b);
-        z += static_cast<double>(a + b);
-      }
-    } else if (add_up) {
-      float least = x[0];
-#pragma unroll
-      for (int i = 1; i < 15; i += 2) least = min3(least, x[i], x[i + 1]);
-      if (!(fminf(least, x[15]) >= quick.low)) {               // masked tokens, or past the end
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = fmaxf(x[i], quick.low);
-      }
-#pragma unroll
-      for (int h = 0; h < 16; h += 8) {
-        const f32x2 t = add2(add2(quick_pair(x[h], x[h + 1], quick), quick_pair(x[h + 2], x[h + 3], quick)),
-                             add2(quick_pair(x[h + 4], x[h + 5], quick), quick_pair(x[h + 6], x[h + 7], quick)));
-        float a, b;
-        unpack2(t, a, b);
         z += static_cast<double>(a + b);
       }
     }
@@ -1005,7 +992,7 @@ __device__ __forceinline__ void pass_row(const Args& A, uint4 (&ring)[4][32], Ro
   for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   z = warp_sum_d(z);
   // (terms out of range: the sample was far off)
-  if (lane == 0) { B.max[warp] = mx; B.sum[warp] = !add_up || mx * quick.c_hi <= base + 100.f ? z : static_cast<double>(NAN); }
+  if (lane == 0) { B.max[warp] = mx; B.sum[warp] = !add_up || mx * c <= base + 100.f ? z : static_cast<double>(NAN); }
 }
 __device__ __forceinline__ void passed(const RowBuffer& B, float& mx, double& z) {
   mx = B.max[0];
@@ -1015,6 +1002,7 @@ __device__ __forceinline__ void passed(const RowBuffer& B, float& mx, double& z)
 }
 
 // Row s from its list (all of it): false, and nothing given, where the list cannot tell.
+template <bool HALF>
 __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned long long* list, int s, int64_t d0, int64_t d1, const RowParams& R,
                                          int m_list, bool fits, float low, float mx, double z, float base) {
   const int tid = threadIdx.x % kListThreads, lane = tid & 31, warp = tid >> 5;
@@ -1034,22 +1022,25 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
     return true;
   }
   const uint32_t max_key = key_of(mx);
-  Term e;
-  e.max = static_cast<double>(mx);
-  e.inv_t = greedy ? 1.0 : 1.0 / static_cast<double>(R.temperature);
+  const Term e = term_of(mx, greedy ? 1.f : R.temperature, S.table);
   auto fixed = [&](uint32_t k) { return __double2ull_rn(e(logit_of(k)) * kFix); };
   const bool limit = !greedy && by_k && !(whole && R.top_k >= m_list);            // top-k leaves something out
   const bool by_p = !greedy && R.top_p < 1.f, by_m = !greedy && R.min_p > 0.f;
-  const double total_quick = add_up ? z * exp2(static_cast<double>(base) - e.max * (1.4426950408889634 / static_cast<double>(R.temperature))) : 0.0;
+  double total_quick = 0.0, error_quick = 0.0;
+  if (add_up) {
+    const double top = e.max * static_cast<double>(quick_c(R));
+    total_quick = z * exp2(static_cast<double>(base) - top);
+    error_quick = quick_error(base, fabs(top - base), A.vocab);
+  }
+  // (once it is needed)
+  auto make_exact = [&]() {
+    total_quick = exact_total<HALF>(S, row_of<HALF>(A, s), A.vocab, e);
+    error_quick = kFixError;
+  };
   double* sums = reinterpret_cast<double*>(list);            // (behind the borders: running sums of the kept ones, beside S.token)
   int kept = 0;
 
   // ---- few candidates (what no filter can keep left out): in order, a thread each
-  double error_quick = 0.0;
-  if (add_up) {
-    const double c = 1.4426950408889634 / static_cast<double>(R.temperature);
-    error_quick = K.rough ? rough_error(base, fabs(e.max * c - base), A.vocab) : kSumError;
-  }
   bool sure = fits && (!by_p || limit || whole || add_up);
   if (sure) {
     uint32_t head = greedy ? max_key : low_key, m_key = 0;     // they have at least the key `head`
@@ -1153,10 +1144,19 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
           if (tid == n - 1) S.z = sum;
           list_sync();
           if (limit || (whole && h == m_list)) { total = S.z; error = 0.0; }
-          const double target = static_cast<double>(R.top_p) * total;
-          const int least = 1 + list_count(tid < n && sum < target * (1.0 - error));
-          const int most = 1 + list_count(tid < n && sum < target * (1.0 + error));
-          if (!(target > 0.0)) sure = false;                   // (a NaN)
+          int least, most;
+          double target;
+          for (int round = 0;; ++round) {
+            target = static_cast<double>(R.top_p) * total;
+            least = 1 + list_count(tid < n && sum < target * (1.0 - error));
+            most = 1 + list_count(tid < n && sum < target * (1.0 + error));
+            // (too close to tell, and nothing else ends before: by the exact sum, whose own error no longer counts)
+            if (!add_up || round == 1 || !((least < most && least <= n && end > least) || !(target > 0.0))) break;
+            make_exact();
+            total = total_quick;
+            error = 0.0;
+          }
+          if (!(target > 0.0)) sure = false;
           else if (least == most && least <= n) end = min(end, least);
           else if (least <= n) sure = end <= least;            // too close to tell, unless something else ends before
         }
@@ -1182,6 +1182,7 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
     }
   }
   if (!sure) return false;
+  if (kept == 0 && add_up && error_quick > kFixError) make_exact();
   if (kept == 0) kept = wide_list(S, list, R, e, m_list, low_key, max_key, limit, greedy, whole, add_up, total_quick, error_quick);
   if (kept == 0) return false;
   if (tid == 0 && A.kept_out) A.kept_out[s] = kept;
@@ -1219,11 +1220,17 @@ __global__ void __launch_bounds__(kListThreads, 2) list_rows_kernel(const __grid
   const bool part = A.parts > 1 && block < (A.n_seq - A.whole_rows) * A.parts;
   const int jobs = mine + (part ? 1 : 0);
   if (jobs == 0) return;
+  // The second half of the blocks (an SM's second, as blocks are dealt out) has its part first, the first half last: the two blocks
+  // of an SM then are not on their lists at the same time.
+  const int lead = part && 2 * block >= static_cast<int>(gridDim.x) ? 1 : 0;
   auto job_of = [&](int j) {
-    return j < mine ? Job{block + j * static_cast<int>(gridDim.x), 0, 1} : Job{A.whole_rows + block / A.parts, block % A.parts, A.parts};
+    const int row = j - lead;
+    return row >= 0 && row < mine ? Job{block + row * static_cast<int>(gridDim.x), 0, 1}
+                                  : Job{A.whole_rows + block / A.parts, block % A.parts, A.parts};
   };
   M.S.count[tid] = 0;
   M.S.mass[tid] = 0;
+  make_table(M.S.table);
   RowHead H = row_head<HALF>(A, job_of(0));
   for (int j = 0; j < jobs; ++j) {
     const Job job = job_of(j);
@@ -1237,7 +1244,7 @@ __global__ void __launch_bounds__(kListThreads, 2) list_rows_kernel(const __grid
       double z;
       passed(B, mx, z);
       if (job.parts == 1) {
-        const bool done = list_row(A, M.S, B.list, job.s, B.d0, B.d1, B.R, static_cast<int>(min(B.n, static_cast<unsigned>(kCap))), B.n <= kCap,
+        const bool done = list_row<HALF>(A, M.S, B.list, job.s, B.d0, B.d1, B.R, static_cast<int>(min(B.n, static_cast<unsigned>(kCap))), B.n <= kCap,
                                    B.low, mx, z, B.base);
         if (tid == 0) A.marks[job.s] = done ? 0 : 1;
       } else {
@@ -1268,6 +1275,7 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
   const int tid = threadIdx.x;
   M.S.count[tid] = 0;
   M.S.mass[tid] = 0;
+  make_table(M.S.table);
   __syncthreads();
   for (int s = A.whole_rows + blockIdx.x; s < A.n_seq; s += gridDim.x) {
     const int64_t d0 = __ldg(A.draw_offsets + s), d1 = __ldg(A.draw_offsets + s + 1);
@@ -1300,10 +1308,10 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
       }
     }
     __syncthreads();
-    const bool done = list_row(A, M.S, M.list, s, d0, d1, R, fits ? static_cast<int>(n) : 0, fits, low, mx, z, base);
+    const bool done = list_row<HALF>(A, M.S, M.list, s, d0, d1, R, fits ? static_cast<int>(n) : 0, fits, low, mx, z, base);
     __syncthreads();
     if (!done) {
-      whole_row<HALF>(A, M.whole, s);
+      whole_row<HALF>(A, M.whole, M.S.table, s);
       __syncthreads();
     }
   }
@@ -1312,7 +1320,7 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
     const int64_t mine = s0 + static_cast<int64_t>(tid & 31) * gridDim.x;
     unsigned marked = __ballot_sync(0xffffffffu, mine < A.whole_rows && A.marks[mine] != 0);
     for (; marked; marked &= marked - 1) {
-      whole_row<HALF>(A, M.whole, static_cast<int>(s0 + static_cast<int64_t>(__ffs(marked) - 1) * gridDim.x));
+      whole_row<HALF>(A, M.whole, M.S.table, static_cast<int>(s0 + static_cast<int64_t>(__ffs(marked) - 1) * gridDim.x));
       __syncthreads();
     }
   }
