@@ -150,300 +150,6 @@ __device__ __forceinline__ double warp_scan_d(double v, int lane) {
   return v;
 }
 
-// ---- any row, one block, several passes ------------------------------------------------------------------------------------------
-struct WholeShared {
-  double d[kWarps];
-  unsigned long long u[kWarps];
-  unsigned count[256];
-  unsigned long long mass[256];
-  double seg[kMaxVocab / kSeg];                // running sum of the kept tokens at every segment's end
-  Border border;
-  unsigned pick;
-  unsigned left;
-  double above;
-  int cut;
-};
-
-__device__ __forceinline__ double block_sum(WholeShared& S, double v) {
-  v = warp_sum_d(v);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) S.d[threadIdx.x >> 5] = v;
-  __syncthreads();
-  double t = 0.0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) t += S.d[w];
-  return t;
-}
-__device__ __forceinline__ unsigned long long block_sum_u(WholeShared& S, unsigned long long v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) S.u[threadIdx.x >> 5] = v;
-  __syncthreads();
-  unsigned long long t = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) t += S.u[w];
-  return t;
-}
-__device__ __forceinline__ unsigned long long block_max_u(WholeShared& S, unsigned long long v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) S.u[threadIdx.x >> 5] = v;
-  __syncthreads();
-  unsigned long long t = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) t = max(t, S.u[w]);
-  return t;
-}
-
-template <bool HALF>
-__device__ void whole_row(const Args& A, WholeShared& S, const double* table, int s) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = A.vocab;
-  const int64_t d0 = A.draw_offsets[s], d1 = A.draw_offsets[s + 1];
-  if (d1 <= d0 && !A.kept_out) return;
-  const void* row = row_of<HALF>(A, s);
-  const RowParams R = row_params(A, s);
-  auto give_all = [&](int token, int kept) {
-    for (int64_t d = d0 + tid; d < d1; d += kThreads) {
-      A.tokens_out[d] = token;
-      if (A.seq_out) A.seq_out[d] = s;
-    }
-    if (tid == 0 && A.kept_out) A.kept_out[s] = kept;
-  };
-  // ---- the maximum (lowest index first), what is no number, how many tokens there are
-  unsigned long long best = 0, finite = 0;
-  for (int v = tid; v < V; v += kThreads) {
-    const uint32_t k = key_of(load_logit<HALF>(row, v));
-    best = max(best, (static_cast<unsigned long long>(k < kNegInf ? 0xffffffffu : k) << 32) | static_cast<uint32_t>(~v));
-    finite += k > kNegInf ? 1 : 0;
-  }
-  best = block_max_u(S, best);
-  finite = block_sum_u(S, finite);
-  const uint32_t max_key = static_cast<uint32_t>(best >> 32);
-  if (max_key >= kPosInf || finite == 0 || !(R.temperature >= 0.f) || R.temperature == INFINITY) {
-    give_all(-1, 0);
-    return;
-  }
-  if (R.temperature == 0.f || R.top_k == 1 || R.top_p <= 0.f) {
-    give_all(static_cast<int>(~static_cast<uint32_t>(best)), 1);
-    return;
-  }
-  const Term e = term_of(logit_of(max_key), R.temperature, table);
-  // ---- top-k: the k-th largest key, eight bits at a time
-  Border border{kNegInf + 1, 0x7fffffff};
-  if (R.top_k > 0 && static_cast<unsigned long long>(R.top_k) < finite) {
-    uint32_t prefix = 0;
-    unsigned left = static_cast<unsigned>(R.top_k);
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      __syncthreads();
-      if (tid < 256) S.count[tid] = 0;
-      __syncthreads();
-      for (int v = tid; v < V; v += kThreads) {
-        const uint32_t k = key_of(load_logit<HALF>(row, v));
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&S.count[(k >> shift) & 255u], 1u);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        unsigned n = left;
-        int b = 255;
-        while (b > 0 && S.count[b] < n) n -= S.count[b--];
-        S.pick = b;
-        S.left = n;
-      }
-      __syncthreads();
-      prefix |= S.pick << shift;
-      left = S.left;
-    }
-    border = Border{prefix, static_cast<int>(left)};
-  }
-  const Border by_count = border;
-  // ---- top-p: bit by bit by sums in fixed point, which only lead the way; the sum above the key it comes to is fp64 and decides
-  if (R.top_p < 1.f) {
-    double mine = 0.0;
-    for (int v = tid; v < V; v += kThreads) {
-      const float x = load_logit<HALF>(row, v);
-      const uint32_t k = key_of(x);
-      if (k > by_count.key || (k == by_count.key && by_count.ties == 0x7fffffff)) mine += e(x);
-    }
-    double total = block_sum(S, mine);
-    if (by_count.ties != 0x7fffffff) total += by_count.ties * e(logit_of(by_count.key));
-    const double target = static_cast<double>(R.top_p) * total;
-    const double scale = ldexp(1.0, 62 - (32 - __clz(V)));
-    uint32_t prefix = 0;
-    double left = target;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      __syncthreads();
-      if (tid < 256) S.mass[tid] = 0;
-      __syncthreads();
-      for (int v = tid; v < V; v += kThreads) {
-        const float x = load_logit<HALF>(row, v);
-        const uint32_t k = key_of(x);
-        if (k > kNegInf && k >= by_count.key && (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))))
-          atomicAdd(&S.mass[(k >> shift) & 255u], static_cast<unsigned long long>(e(x) * scale));
-      }
-      __syncthreads();
-      if (tid == 0) {
-        double n = left;
-        int b = 255, last = 255;
-        for (; b >= 0; --b) {
-          if (S.mass[b] == 0) continue;
-          last = b;
-          const double m = static_cast<double>(S.mass[b]) / scale;
-          if (m >= n) break;
-          n -= m;
-        }
-        S.pick = b < 0 ? last : b;
-        S.above = b < 0 ? 0.0 : n;
-      }
-      __syncthreads();
-      prefix |= S.pick << shift;
-      left = S.above;
-    }
-    // The border's key has to have  above < target <= above + all of it: else to its neighbour on that side, and, where that is
-    // not enough (tails of tokens too light for the fixed point), by halves.
-    uint32_t key = prefix, low = kNegInf, high = max_key + 1;   // (the border lies between the last two)
-    Border by_sum = by_count;
-    for (int tries = 0; tries < 48; ++tries) {
-      double sum = 0.0;
-      unsigned long long equal = 0, up = 0xffffffffu, down = 0;
-      for (int v = tid; v < V; v += kThreads) {
-        const float x = load_logit<HALF>(row, v);
-        const uint32_t k = key_of(x);
-        if (k > key) {
-          sum += e(x);
-          up = min(up, static_cast<unsigned long long>(k));
-        } else if (k == key) {
-          ++equal;
-        } else if (k >= by_count.key) {
-          down = max(down, static_cast<unsigned long long>(k));
-        }
-      }
-      sum = block_sum(S, sum);
-      equal = block_sum_u(S, equal);
-      if (key == by_count.key && by_count.ties != 0x7fffffff) equal = by_count.ties;
-      up = 0xffffffffu - block_max_u(S, 0xffffffffu - up);
-      down = block_max_u(S, down);
-      const double one = e(logit_of(key)), all = sum + static_cast<double>(equal) * one;
-      if (sum >= target && up != 0xffffffffu) {
-        low = key;
-        key = tries < 4 || high - low < 4 ? static_cast<uint32_t>(up) : low + (high - low) / 2;
-      } else if (all < target && down > kNegInf) {
-        high = key;
-        key = tries < 4 || high - low < 4 ? static_cast<uint32_t>(down) : low + (high - low) / 2;
-      } else if (equal == 0) {
-        key = static_cast<uint32_t>(up);
-      } else {
-        double n = ceil((target - sum) / one);
-        if (!(n >= 1.0)) n = 1.0;
-        unsigned long long m = n < static_cast<double>(equal) ? static_cast<unsigned long long>(n) : equal;
-        while (m > 1 && sum + static_cast<double>(m - 1) * one >= target) --m;
-        while (m < equal && sum + static_cast<double>(m) * one < target) ++m;
-        by_sum = Border{key, static_cast<int>(m > 0 ? m : 1)};
-        break;
-      }
-    }
-    if (less(by_sum, border)) border = by_sum;
-  }
-  // ---- min-p
-  const Border by_size{min_p_key(e, R.temperature, R.min_p, max_key), 0x7fffffff};
-  if (less(by_size, border)) border = by_size;
-  if (static_cast<double>(R.min_p) > 1.0) border = Border{max_key, 1};
-
-  // ---- how many are kept, and the index up to which tokens with the border's key are
-  unsigned long long above = 0, equal = 0;
-  for (int v = tid; v < V; v += kThreads) {
-    const uint32_t k = key_of(load_logit<HALF>(row, v));
-    above += k > border.key ? 1 : 0;
-    equal += k == border.key ? 1 : 0;
-  }
-  above = block_sum_u(S, above);
-  equal = block_sum_u(S, equal);
-  int cut = V;
-  if (equal > static_cast<unsigned long long>(border.ties)) {
-    // index of the ties-th: stretches of tokens per thread, counted in order
-    const int stretch = (V + kThreads - 1) / kThreads, v0 = min(tid * stretch, V), v1 = min(v0 + stretch, V);
-    unsigned mine = 0;
-    for (int v = v0; v < v1; ++v) mine += key_of(load_logit<HALF>(row, v)) == border.key ? 1 : 0;
-    unsigned incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned x = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += x;
-    }
-    __syncthreads();
-    if (lane == 31) S.u[warp] = incl;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) incl += static_cast<unsigned>(S.u[w]);
-    unsigned n = incl - mine;
-    const unsigned ties = static_cast<unsigned>(border.ties);
-    if (n < ties && incl >= ties) {
-      for (int v = v0; v < v1; ++v)
-        if (key_of(load_logit<HALF>(row, v)) == border.key && ++n == ties) { S.cut = v; break; }
-    }
-    __syncthreads();
-    cut = S.cut;
-    equal = ties;
-  }
-  if (tid == 0 && A.kept_out) A.kept_out[s] = static_cast<int>(above + equal);
-  if (d1 <= d0) return;
-
-  // ---- sums of the kept tokens, segment by segment
-  auto kept_term = [&](int v) -> double {
-    if (v >= V) return 0.0;
-    const float x = load_logit<HALF>(row, v);
-    const uint32_t k = key_of(x);
-    return k > border.key || (k == border.key && v <= cut) ? e(x) : 0.0;
-  };
-  const int n_seg = (V + kSeg - 1) / kSeg;
-  for (int g = warp; g < n_seg; g += kWarps) {
-    double sum = 0.0;
-    for (int x = lane; x < kSeg; x += 32) sum += kept_term(g * kSeg + x);
-    sum = warp_sum_d(sum);
-    if (lane == 0) S.seg[g] = sum;
-  }
-  __syncthreads();
-  if (warp == 0) {
-    double run = 0.0;
-    for (int g0 = 0; g0 < n_seg; g0 += 32) {
-      const double incl = warp_scan_d(g0 + lane < n_seg ? S.seg[g0 + lane] : 0.0, lane) + run;
-      if (g0 + lane < n_seg) S.seg[g0 + lane] = incl;
-      run = __shfl_sync(0xffffffffu, incl, 31);
-    }
-  }
-  __syncthreads();
-  const double total = S.seg[n_seg - 1];
-  for (int64_t d = d0 + warp; d < d1; d += kWarps) {
-    const float u = A.uniforms[d];
-    const double target = (u < 1.f ? fmaxf(u, 0.f) : 1.f) * total;
-    int lo = 0, hi = n_seg;                                    // the first segment whose end exceeds the target
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (S.seg[mid] > target) hi = mid; else lo = mid + 1;
-    }
-    if (lo == n_seg) {                                         // none: the last one that adds something
-      lo = n_seg - 1;
-      while (lo > 0 && !(S.seg[lo] > S.seg[lo - 1])) --lo;
-    }
-    double run = lo > 0 ? S.seg[lo - 1] : 0.0;
-    int token = -1, last = -1;
-    for (int x = 0; x < kSeg && token < 0; x += 32) {
-      const int v = lo * kSeg + x + lane;
-      const double t = kept_term(v);
-      const double incl = warp_scan_d(t, lane) + run;
-      const unsigned over = __ballot_sync(0xffffffffu, t > 0.0 && incl > target), any = __ballot_sync(0xffffffffu, t > 0.0);
-      if (over) token = lo * kSeg + x + __ffs(over) - 1;
-      if (any) last = lo * kSeg + x + 31 - __clz(any);
-      run = __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane == 0) {
-      A.tokens_out[d] = token >= 0 ? token : last;             // (the two sums of a segment may differ in their last bits)
-      if (A.seq_out) A.seq_out[d] = s;
-    }
-  }
-  __syncthreads();
-}
-
 // ---- most rows: one pass over the row, the rest on a short list --------------------------------------------------------------------
 // What is kept is nearly always among the few largest logits, so one pass collects those above a THRESHOLD in shared memory (the
 // list) and, where top-p is over the whole row, adds up all terms in fp32 (with a bound: quick_error).  The threshold comes from a
@@ -482,8 +188,9 @@ struct ListShared {
     uint32_t token[kCap];
     uint4 ring[kListWarps][4][32];                             // in the pass
   };
-  unsigned long long mass[kBins];
+  unsigned long long order[kListThreads];                      // candidates in order; running sums of stretches of kept ones
   unsigned count[kBins];
+  unsigned part[3][kBins];                                     // a sum of terms in fixed point, see add_fixed
   double d[kListWarps];
   float group[kGroups];
   unsigned bin, moved;
@@ -524,6 +231,20 @@ __device__ __forceinline__ double block_scan_d(double* per_warp, double v, int w
   return incl + warps_before(per_warp, warp, lane);
 }
 
+// Terms in fixed point (at most 2^50) by 17 bits of them at a time: kCap of those fit 32 bits, which shared memory adds up by itself
+// (64 bits are a loop of compare-and-swaps: 0.27 ms a list where a bin has many).
+__device__ __forceinline__ void add_fixed(ListShared& S, int bin, unsigned long long m) {
+  atomicAdd(&S.part[0][bin], static_cast<unsigned>(m) & 0x1ffffu);
+  atomicAdd(&S.part[1][bin], static_cast<unsigned>(m >> 17) & 0x1ffffu);
+  atomicAdd(&S.part[2][bin], static_cast<unsigned>(m >> 34));
+}
+__device__ __forceinline__ unsigned long long take_fixed(ListShared& S, int bin) {   // and leaves 0
+  const unsigned long long m = S.part[0][bin] + (static_cast<unsigned long long>(S.part[1][bin]) << 17) +
+                               (static_cast<unsigned long long>(S.part[2][bin]) << 34);
+  S.part[0][bin] = S.part[1][bin] = S.part[2][bin] = 0;
+  return m;
+}
+
 struct Found {                                                 // where a running count or sum over falling keys reaches its target
   bool there;
   uint32_t key;
@@ -543,14 +264,14 @@ __device__ __forceinline__ Found find_on_list(ListShared& S, int n, uint32_t lo,
       uint32_t k;
       if (entry(i, k) && k >= lo && k <= hi) {
         const uint32_t b = (k - lo) >> shift;
-        if (MASS) atomicAdd(&S.mass[b], weight(k));
+        if (MASS) add_fixed(S, b, weight(k));
         else atomicAdd(&S.count[b], 1u);
       }
     }
     list_sync();
     const int bin = kBins - 1 - tid;                           // from the top
-    const unsigned long long here = MASS ? S.mass[bin] : static_cast<unsigned long long>(S.count[bin]);
-    if (MASS) S.mass[bin] = 0; else S.count[bin] = 0;
+    const unsigned long long here = MASS ? take_fixed(S, bin) : static_cast<unsigned long long>(S.count[bin]);
+    if (!MASS) S.count[bin] = 0;
     unsigned long long incl = here;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -617,9 +338,9 @@ __device__ __forceinline__ void unpack(const uint4& u, float* x) {
   }
 }
 
-// Many candidates, or an end that is none of a few: borders by find_on_list, the kept ones sorted by index, running sums in their
-// places.  Returns how many are kept; 0: the list cannot tell.
-__device__ __noinline__ int wide_list(ListShared& S, unsigned long long* list, const RowParams R, const Term e, int m_list, uint32_t low_key, uint32_t max_key, bool limit,
+// Many candidates, or an end that is none of a few: borders by find_on_list, the kept ones in the order of their indices.  Returns how
+// many are kept (S.token: their places on the list); 0: the list cannot tell.
+__device__ __noinline__ int wide_list(ListShared& S, unsigned long long* list, const RowParams R, const Term e, int V, int m_list, uint32_t low_key, uint32_t max_key, bool limit,
                                       bool greedy, bool whole, bool add_up, double total_quick, double error_quick) {
   const int tid = threadIdx.x % kListThreads, lane = tid & 31, warp = tid >> 5;
   bool sure = true;
@@ -706,7 +427,7 @@ __device__ __noinline__ int wide_list(ListShared& S, unsigned long long* list, c
   }
   if (!sure) return 0;
 
-  // ---- the kept ones: to the front of the list, lowest indices first among those with the border's key
+  // ---- the lowest indices among those with the border's key
   uint32_t cut = 0xffffffffu;
   {
     const Found f = border.ties == 0x7fffffff
@@ -718,47 +439,52 @@ __device__ __noinline__ int wide_list(ListShared& S, unsigned long long* list, c
                                               }, one);
     if (f.there) cut = ~f.key;
   }
-  if (tid == 0) S.moved = 0;
-  list_sync();
+  // ---- the kept ones by index: into 512 buckets by their leading bits, then by rank in their bucket; S.token: their places on the list
   auto keeps = [&](unsigned long long x) {
     const uint32_t k = static_cast<uint32_t>(x >> 32), v = static_cast<uint32_t>(x);
     return k > border.key || (k == border.key && v <= cut);
   };
-  auto turned = [](unsigned long long x) { return (x << 32) | (x >> 32); };
-  for (int i0 = 0; i0 < m_list; i0 += kListThreads) {
-    const unsigned long long x = i0 + tid < m_list ? list[i0 + tid] : 0;
-    const bool keep = i0 + tid < m_list && keeps(x);
-    list_sync();
-    if (keep) list[atomicAdd(&S.moved, 1u)] = turned(x);     // (not behind i0 + kListThreads: read by all already)
-    list_sync();
+  const int shift = max(0, 32 - __clz(V) - 9);
+  auto bucket = [&](unsigned long long x) { return static_cast<uint32_t>(x) >> shift; };
+  list_sync();
+  for (int i = tid; i < m_list; i += kListThreads)
+    if (keeps(list[i])) atomicAdd(&S.count[bucket(list[i])], 1u);
+  list_sync();
+  const unsigned in_bucket = S.count[tid];
+  unsigned start = in_bucket;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned up = __shfl_up_sync(0xffffffffu, start, o);
+    if (lane >= o) start += up;
   }
+  if (lane == 31) S.u[warp] = start;
+  list_sync();
+  start += static_cast<unsigned>(warps_before(S.u, warp, lane)) - in_bucket;
+  S.part[0][tid] = S.part[1][tid] = start;
+  if (tid == kListThreads - 1) S.moved = start + in_bucket;
+  list_sync();
   const int kept = static_cast<int>(S.moved);
-  int n2 = 1;
-  while (n2 < kept) n2 *= 2;
-  for (int i = kept + tid; i < n2; i += kListThreads) list[i] = ~0ull;
-  for (int size = 2; size <= n2; size *= 2) {
-    for (int stride = size / 2; stride > 0; stride /= 2) {
-      list_sync();
-      for (int x = tid; x < n2 / 2; x += kListThreads) {
-        const int i = 2 * x - (x & (stride - 1)), j = i + stride;
-        const unsigned long long a = list[i], b = list[j];
-        if ((a > b) == ((i & size) == 0)) { list[i] = b; list[j] = a; }
-      }
+  for (int i = tid; i < m_list; i += kListThreads)
+    if (keeps(list[i])) S.token[atomicAdd(&S.part[0][bucket(list[i])], 1u)] = static_cast<uint32_t>(i);
+  list_sync();
+  uint32_t move[kCap / kListThreads];                          // place on the list, place in order
+#pragma unroll
+  for (int y = 0; y < kCap / kListThreads; ++y) {
+    const int t = tid + y * kListThreads;
+    move[y] = 0;
+    if (t < kept) {
+      const uint32_t i = S.token[t], v = static_cast<uint32_t>(list[i]), b = bucket(list[i]);
+      const int b0 = S.part[1][b], b1 = b0 + S.count[b];
+      int at = b0;
+      for (int u = b0; u < b1; ++u) at += static_cast<uint32_t>(list[S.token[u]]) < v ? 1 : 0;
+      move[y] = i << 16 | static_cast<uint32_t>(at);
     }
   }
   list_sync();
-  // ---- running sums, a stretch per thread
-  const int stretch = (kept + kListThreads - 1) / kListThreads, i0 = min(tid * stretch, kept), i1 = min(i0 + stretch, kept);
-  double mine = 0.0;
-  for (int i = i0; i < i1; ++i) mine += e(logit_of(static_cast<uint32_t>(list[i])));
-  double run = block_scan_d(S.d, mine, warp, lane) - mine;
-  double* sums = reinterpret_cast<double*>(list);
-  for (int i = i0; i < i1; ++i) {
-    const unsigned long long x = list[i];
-    run += e(logit_of(static_cast<uint32_t>(x)));
-    S.token[i] = static_cast<uint32_t>(x >> 32);
-    sums[i] = run;
-  }
+#pragma unroll
+  for (int y = 0; y < kCap / kListThreads; ++y)
+    if (tid + y * kListThreads < kept) S.token[move[y] & 0xffffu] = move[y] >> 16;
+  S.count[tid] = S.part[0][tid] = S.part[1][tid] = 0;
   list_sync();
   return kept;
 }
@@ -1070,14 +796,13 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
         if (k < low_key) continue;
         const uint32_t b = (k - low_key) >> shift;
         if (limit) atomicAdd(&S.count[b], 1u);
-        else atomicAdd(&S.mass[b], fixed(k));
+        else add_fixed(S, b, fixed(k));
       }
       if (tid == 0) S.bin = 0;
       list_sync();
       const int bin = kBins - 1 - tid;
-      const unsigned long long here = limit ? static_cast<unsigned long long>(S.count[bin]) : S.mass[bin];
+      const unsigned long long here = limit ? static_cast<unsigned long long>(S.count[bin]) : take_fixed(S, bin);
       S.count[bin] = 0;
-      S.mass[bin] = 0;
       unsigned long long incl = here;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -1116,16 +841,15 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
     if (h <= kListThreads) {
       // in order: largest logit first, equal ones by index
       unsigned long long y = tid < h ? list[S.token[tid]] ^ 0xffffffffull : 0;
-      if (tid < h) S.mass[tid] = y;
+      if (tid < h) S.order[tid] = y;
       list_sync();
       int at = 0;
       if (tid < h)
-        for (int j = 0; j < h; ++j) at += S.mass[j] > y ? 1 : 0;
+        for (int j = 0; j < h; ++j) at += S.order[j] > y ? 1 : 0;
       list_sync();
-      if (tid < h) S.mass[at] = y;
+      if (tid < h) S.order[at] = y;
       list_sync();
-      y = tid < h ? S.mass[tid] : 0;
-      S.mass[tid] = 0;
+      y = tid < h ? S.order[tid] : 0;
       const double mine = tid < h ? e(logit_of(static_cast<uint32_t>(y >> 32))) : 0.0;
       const double sum = block_scan_d(S.d, mine, warp, lane);
       // The least of the ends that lie among the candidates; an end that does not is not less.
@@ -1183,23 +907,52 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
   }
   if (!sure) return false;
   if (kept == 0 && add_up && error_quick > kFixError) make_exact();
-  if (kept == 0) kept = wide_list(S, list, R, e, m_list, low_key, max_key, limit, greedy, whole, add_up, total_quick, error_quick);
+  const bool wide = kept == 0;
+  if (wide) kept = wide_list(S, list, R, e, A.vocab, m_list, low_key, max_key, limit, greedy, whole, add_up, total_quick, error_quick);
   if (kept == 0) return false;
   if (tid == 0 && A.kept_out) A.kept_out[s] = kept;
-  const double total = sums[kept - 1];
+  if (d1 <= d0) return true;
+  // Draws.  Few kept ones: their running sums, S.token their tokens.  Many: a running sum for every stretch of them (a thread's), terms
+  // made again within one.
+  const int stretch = wide ? (kept + kListThreads - 1) / kListThreads : 1, n_sums = (kept + stretch - 1) / stretch;
+  auto term_at = [&](int p) { return e(logit_of(static_cast<uint32_t>(list[S.token[p]] >> 32))); };
+  if (wide) {
+    sums = reinterpret_cast<double*>(S.order);
+    double mine = 0.0;
+    for (int p = tid * stretch; p < min((tid + 1) * stretch, kept); ++p) mine += term_at(p);
+    const double running = block_scan_d(S.d, mine, warp, lane);
+    sums[tid] = running;
+    list_sync();
+  }
+  const double total = sums[n_sums - 1];
   for (int64_t d = d0 + tid; d < d1; d += kListThreads) {
     const float u = __ldg(A.uniforms + d);
     const double target = (u < 1.f ? fmaxf(u, 0.f) : 1.f) * total;
-    int a = 0, b = kept;
+    int a = 0, b = n_sums;
     while (a < b) {
       const int mid = (a + b) >> 1;
       if (sums[mid] > target) b = mid; else a = mid + 1;
     }
-    if (a == kept) {                                           // none: the last one that adds something
+    if (a == n_sums) {                                         // none: the last one that adds something
       --a;
       while (a > 0 && !(sums[a] > sums[a - 1])) --a;
     }
-    A.tokens_out[d] = static_cast<int32_t>(S.token[a]);
+    uint32_t token;
+    if (wide) {
+      double run = a > 0 ? sums[a - 1] : 0.0;
+      int at = a * stretch, last = at;
+      for (int p = at; p < min((a + 1) * stretch, kept); ++p) {
+        const double t = term_at(p);
+        run += t;
+        if (t > 0.0) last = p;
+        at = p;
+        if (run > target && t > 0.0) break;
+      }
+      token = static_cast<uint32_t>(list[S.token[run > target ? at : last]]);   // (the two sums of a stretch may differ in their last bits)
+    } else {
+      token = S.token[a];
+    }
+    A.tokens_out[d] = static_cast<int32_t>(token);
     if (A.seq_out) A.seq_out[d] = s;
   }
   return true;
@@ -1229,7 +982,7 @@ __global__ void __launch_bounds__(kListThreads, 2) list_rows_kernel(const __grid
                                   : Job{A.whole_rows + block / A.parts, block % A.parts, A.parts};
   };
   M.S.count[tid] = 0;
-  M.S.mass[tid] = 0;
+  for (int x = 0; x < 3; ++x) M.S.part[x][tid] = 0;
   make_table(M.S.table);
   RowHead H = row_head<HALF>(A, job_of(0));
   for (int j = 0; j < jobs; ++j) {
@@ -1258,6 +1011,477 @@ __global__ void __launch_bounds__(kListThreads, 2) list_rows_kernel(const __grid
   }
 }
 
+// The border of a row whose kept tokens are too many for a list, by top-k or by top-p (not both), on a list of its surroundings: a
+// histogram over the logit (2048 bins, counts) says in which bin it lies - for top-p by the terms at the bins' middles, off by far less
+// than a bin - and one more pass adds up, in fp64, what lies above that bin and its neighbours, and collects those.  The list then
+// decides, and says whether the border is in it at all.  `kept`: how many are, `cut`: the last index of those with the border's key.
+struct Bracketed {
+  bool there;
+  Border border;
+  int kept, cut;
+};
+template <bool HALF>
+__device__ __noinline__ Bracketed bracket_row(ListShared& S, unsigned long long* list, const void* row, int V, const RowParams R, const Term e, float top,
+                                              unsigned long long finite) {
+  constexpr int kFine = 2048, kPer = kFine / kListThreads;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const Bracketed none{false, Border{0, 0}, 0, 0};
+  const bool limit = R.top_k > 0 && static_cast<unsigned long long>(R.top_k) < finite, by_p = R.top_p < 1.f;
+  if (limit == by_p) return none;
+  __syncthreads();
+  float least = INFINITY;
+  if (limit) {
+    for (int v = tid; v < V; v += kListThreads) {
+      const float x = load_logit<HALF>(row, v);
+      if (x > -INFINITY) least = fminf(least, x);
+    }
+  } else {
+    least = top - 40.f * R.temperature;                        // (what lies below adds up to less than 1e-11)
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+  if (lane == 0) S.group[warp] = least;
+  for (int x = 0; x < kPer; ++x) S.token[tid + x * kListThreads] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kListWarps; ++w) least = fminf(least, S.group[w]);
+  const float width = (top - least) / (kFine - 1), per_width = 1.f / width;
+  if (!(width > 0.f) || !(per_width < INFINITY)) return none;
+  auto bin_of = [&](float x) { return static_cast<int>(fminf(fmaxf((x - least) * per_width, 0.f), static_cast<float>(kFine - 1))); };
+  for (int v = tid; v < V; v += kListThreads) {
+    const float x = load_logit<HALF>(row, v);
+    if (x > -INFINITY) atomicAdd(&S.token[bin_of(x)], 1u);
+  }
+  if (tid == 0) { S.bin = 0; S.moved = 0; }
+  __syncthreads();
+  // counts and terms from the top, kPer bins a thread
+  unsigned counts[kPer];
+  double terms[kPer], terms_here = 0.0;
+  unsigned long long here = 0;
+#pragma unroll
+  for (int x = 0; x < kPer; ++x) {
+    const int b = kFine - 1 - (tid * kPer + x);
+    counts[x] = S.token[b];
+    here += counts[x];
+    terms[x] = by_p && counts[x] ? counts[x] * e(fminf(least + (static_cast<float>(b) + 0.5f) * width, top)) : 0.0;
+    terms_here += terms[x];
+  }
+  unsigned long long incl = here;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) S.u[warp] = incl;
+  const double terms_incl = block_scan_d(S.d, terms_here, warp, lane);          // (a barrier)
+  incl += warps_before(S.u, warp, lane);
+  if (tid == kListThreads - 1) S.z = terms_incl;
+  __syncthreads();
+  {
+    const double target = static_cast<double>(R.top_p) * S.z;
+    unsigned long long n = incl - here;
+    double m = terms_incl - terms_here;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const bool in = limit ? n < static_cast<unsigned long long>(R.top_k) && n + counts[x] >= static_cast<unsigned long long>(R.top_k)
+                            : m < target && m + terms[x] >= target;
+      if (in) S.bin = kFine - 1 - (tid * kPer + x);
+      n += counts[x];
+      m += terms[x];
+    }
+  }
+  __syncthreads();
+  const int bin = static_cast<int>(S.bin), b0 = limit ? bin : bin - 1, b1 = limit ? bin : bin + 1;
+  if (b0 < 1 && !limit) return none;                           // (the lowest bin holds all that is below)
+  // what lies above, and the surroundings
+  double above = 0.0, all = 0.0;
+  unsigned n_above = 0;
+  for (int v = tid; v < V; v += kListThreads) {
+    const float x = load_logit<HALF>(row, v);
+    if (!(x > -INFINITY)) continue;
+    const int b = bin_of(x);
+    if (by_p) {
+      const double t = e(x);
+      all += t;
+      above += b > b1 ? t : 0.0;
+    }
+    n_above += b > b1 ? 1 : 0;
+    if (b >= b0 && b <= b1) {
+      const unsigned at = atomicAdd(&S.moved, 1u);
+      if (at < kCap) list[at] = entry_of(x, v);
+    }
+  }
+  above = warp_sum_d(above);
+  all = warp_sum_d(all);
+  n_above = __reduce_add_sync(0xffffffffu, n_above);
+  __syncthreads();
+  if (lane == 0) { S.d[warp] = above; S.order[warp] = static_cast<unsigned long long>(__double_as_longlong(all)); S.u[warp] = n_above; }
+  __syncthreads();
+  above = all = 0.0;
+  unsigned long long larger = 0;
+#pragma unroll
+  for (int w = 0; w < kListWarps; ++w) {
+    above += S.d[w];
+    all += __longlong_as_double(static_cast<long long>(S.order[w]));
+    larger += S.u[w];
+  }
+  const unsigned n = S.moved;
+  if (n == 0 || n > kCap) return none;
+  auto by_key = [&](int i, uint32_t& k) { k = static_cast<uint32_t>(list[i] >> 32); return true; };
+  auto fixed = [&](uint32_t k) { return __double2ull_rn(e(logit_of(k)) * kFix); };
+  auto one = [](uint32_t) { return 1ull; };
+  Bracketed B = none;
+  unsigned long long ties, same;
+  if (limit) {
+    if (larger >= static_cast<unsigned long long>(R.top_k)) return none;
+    const Found f = find_on_list<false>(S, static_cast<int>(n), 0, 0xffffffffu, R.top_k - larger, by_key, one);
+    if (!f.there) return none;
+    ties = R.top_k - larger - f.above;
+    same = f.at_key;
+    B.border.key = f.key;
+  } else {
+    const double target = static_cast<double>(R.top_p) * all, slack = 4e-12 * all;    // (kCap 2^-51, and a share of it for the sums)
+    if (!(target - above > slack)) return none;
+    const unsigned long long need = __double2ull_ru((target - above - slack) * kFix);
+    const Found f = find_on_list<true>(S, static_cast<int>(n), 0, 0xffffffffu, need, by_key, fixed);
+    if (!f.there) return none;
+    const unsigned long long each = max(fixed(f.key), 1ull);
+    ties = (need - f.above + each - 1) / each;
+    if (!(static_cast<double>(f.above + ties * each) >= (target - above + slack) * kFix)) return none;
+    same = f.at_key / each;
+    B.border.key = f.key;
+  }
+  B.border.ties = ties < same ? static_cast<int>(ties) : 0x7fffffff;
+  B.cut = V;
+  if (ties < same) {
+    const Found f = find_on_list<false>(S, static_cast<int>(n), 0, 0xffffffffu, ties,
+                                        [&](int i, uint32_t& k) {
+                                          k = ~static_cast<uint32_t>(list[i]);
+                                          return static_cast<uint32_t>(list[i] >> 32) == B.border.key;
+                                        }, one);
+    if (!f.there) return none;
+    B.cut = static_cast<int>(~f.key);
+  }
+  int mine = 0;
+  for (unsigned i = tid; i < n; i += kListThreads) {
+    const uint32_t k = static_cast<uint32_t>(list[i] >> 32), v = static_cast<uint32_t>(list[i]);
+    mine += k > B.border.key || (k == B.border.key && v <= static_cast<uint32_t>(B.cut)) ? 1 : 0;
+  }
+  mine = __reduce_add_sync(0xffffffffu, mine);
+  __syncthreads();
+  if (lane == 0) S.u[warp] = mine;
+  __syncthreads();
+  unsigned long long kept = larger;
+#pragma unroll
+  for (int w = 0; w < kListWarps; ++w) kept += S.u[w];
+  B.kept = static_cast<int>(kept);
+  B.there = true;
+  __syncthreads();
+  return B;
+}
+
+// ---- any row, one block, several passes ------------------------------------------------------------------------------------------
+struct WholeShared {
+  double d[kWarps];
+  unsigned long long u[kWarps];
+  unsigned count[256];
+  unsigned long long mass[256];
+  double seg[kMaxVocab / kSeg];                // running sum of the kept tokens at every segment's end
+  Border border;
+  unsigned pick;
+  unsigned left;
+  double above;
+  int cut;
+};
+
+__device__ __forceinline__ double block_sum(WholeShared& S, double v) {
+  v = warp_sum_d(v);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) S.d[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double t = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) t += S.d[w];
+  return t;
+}
+__device__ __forceinline__ unsigned long long block_sum_u(WholeShared& S, unsigned long long v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) S.u[threadIdx.x >> 5] = v;
+  __syncthreads();
+  unsigned long long t = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) t += S.u[w];
+  return t;
+}
+__device__ __forceinline__ unsigned long long block_max_u(WholeShared& S, unsigned long long v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) S.u[threadIdx.x >> 5] = v;
+  __syncthreads();
+  unsigned long long t = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) t = max(t, S.u[w]);
+  return t;
+}
+
+template <bool HALF>
+__device__ void whole_row(const Args& A, WholeShared& S, ListShared& L, unsigned long long* list, int s) {   // (list: S's memory)
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = A.vocab;
+  const int64_t d0 = A.draw_offsets[s], d1 = A.draw_offsets[s + 1];
+  if (d1 <= d0 && !A.kept_out) return;
+  const void* row = row_of<HALF>(A, s);
+  const RowParams R = row_params(A, s);
+  auto give_all = [&](int token, int kept) {
+    for (int64_t d = d0 + tid; d < d1; d += kThreads) {
+      A.tokens_out[d] = token;
+      if (A.seq_out) A.seq_out[d] = s;
+    }
+    if (tid == 0 && A.kept_out) A.kept_out[s] = kept;
+  };
+  // ---- the maximum (lowest index first), what is no number, how many tokens there are
+  unsigned long long best = 0, finite = 0;
+  for (int v = tid; v < V; v += kThreads) {
+    const uint32_t k = key_of(load_logit<HALF>(row, v));
+    best = max(best, (static_cast<unsigned long long>(k < kNegInf ? 0xffffffffu : k) << 32) | static_cast<uint32_t>(~v));
+    finite += k > kNegInf ? 1 : 0;
+  }
+  best = block_max_u(S, best);
+  finite = block_sum_u(S, finite);
+  const uint32_t max_key = static_cast<uint32_t>(best >> 32);
+  if (max_key >= kPosInf || finite == 0 || !(R.temperature >= 0.f) || R.temperature == INFINITY) {
+    give_all(-1, 0);
+    return;
+  }
+  if (R.temperature == 0.f || R.top_k == 1 || R.top_p <= 0.f) {
+    give_all(static_cast<int>(~static_cast<uint32_t>(best)), 1);
+    return;
+  }
+  const Term e = term_of(logit_of(max_key), R.temperature, L.table);
+  const Bracketed bracketed = bracket_row<HALF>(L, list, row, V, R, e, logit_of(max_key), finite);
+  // ---- top-k: the k-th largest key, eight bits at a time
+  Border border{kNegInf + 1, 0x7fffffff};
+  if (bracketed.there) border = bracketed.border;
+  if (!bracketed.there && R.top_k > 0 && static_cast<unsigned long long>(R.top_k) < finite) {
+    uint32_t prefix = 0;
+    unsigned left = static_cast<unsigned>(R.top_k);
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      __syncthreads();
+      if (tid < 256) S.count[tid] = 0;
+      __syncthreads();
+      for (int v = tid; v < V; v += kThreads) {
+        const uint32_t k = key_of(load_logit<HALF>(row, v));
+        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&S.count[(k >> shift) & 255u], 1u);
+      }
+      __syncthreads();
+      if (tid == 0) {
+        unsigned n = left;
+        int b = 255;
+        while (b > 0 && S.count[b] < n) n -= S.count[b--];
+        S.pick = b;
+        S.left = n;
+      }
+      __syncthreads();
+      prefix |= S.pick << shift;
+      left = S.left;
+    }
+    border = Border{prefix, static_cast<int>(left)};
+  }
+  const Border by_count = border;
+  // ---- top-p: bit by bit by sums in fixed point, which only lead the way; the sum above the key it comes to is fp64 and decides
+  if (!bracketed.there && R.top_p < 1.f) {
+    double mine = 0.0;
+    for (int v = tid; v < V; v += kThreads) {
+      const float x = load_logit<HALF>(row, v);
+      const uint32_t k = key_of(x);
+      if (k > by_count.key || (k == by_count.key && by_count.ties == 0x7fffffff)) mine += e(x);
+    }
+    double total = block_sum(S, mine);
+    if (by_count.ties != 0x7fffffff) total += by_count.ties * e(logit_of(by_count.key));
+    const double target = static_cast<double>(R.top_p) * total;
+    const double scale = ldexp(1.0, 62 - (32 - __clz(V)));
+    uint32_t prefix = 0;
+    double left = target;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      __syncthreads();
+      if (tid < 256) S.mass[tid] = 0;
+      __syncthreads();
+      for (int v = tid; v < V; v += kThreads) {
+        const float x = load_logit<HALF>(row, v);
+        const uint32_t k = key_of(x);
+        if (k > kNegInf && k >= by_count.key && (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))))
+          atomicAdd(&S.mass[(k >> shift) & 255u], static_cast<unsigned long long>(e(x) * scale));
+      }
+      __syncthreads();
+      if (tid == 0) {
+        double n = left;
+        int b = 255, last = 255;
+        for (; b >= 0; --b) {
+          if (S.mass[b] == 0) continue;
+          last = b;
+          const double m = static_cast<double>(S.mass[b]) / scale;
+          if (m >= n) break;
+          n -= m;
+        }
+        S.pick = b < 0 ? last : b;
+        S.above = b < 0 ? 0.0 : n;
+      }
+      __syncthreads();
+      prefix |= S.pick << shift;
+      left = S.above;
+    }
+    // The border's key has to have  above < target <= above + all of it: else to its neighbour on that side, and, where that is
+    // not enough (tails of tokens too light for the fixed point), by halves.
+    uint32_t key = prefix, low = kNegInf, high = max_key + 1;   // (the border lies between the last two)
+    Border by_sum = by_count;
+    for (int tries = 0; tries < 48; ++tries) {
+      double sum = 0.0;
+      unsigned long long equal = 0, up = 0xffffffffu, down = 0;
+      for (int v = tid; v < V; v += kThreads) {
+        const float x = load_logit<HALF>(row, v);
+        const uint32_t k = key_of(x);
+        if (k > key) {
+          sum += e(x);
+          up = min(up, static_cast<unsigned long long>(k));
+        } else if (k == key) {
+          ++equal;
+        } else if (k >= by_count.key) {
+          down = max(down, static_cast<unsigned long long>(k));
+        }
+      }
+      sum = block_sum(S, sum);
+      equal = block_sum_u(S, equal);
+      if (key == by_count.key && by_count.ties != 0x7fffffff) equal = by_count.ties;
+      up = 0xffffffffu - block_max_u(S, 0xffffffffu - up);
+      down = block_max_u(S, down);
+      const double one = e(logit_of(key)), all = sum + static_cast<double>(equal) * one;
+      if (sum >= target && up != 0xffffffffu) {
+        low = key;
+        key = tries < 4 || high - low < 4 ? static_cast<uint32_t>(up) : low + (high - low) / 2;
+      } else if (all < target && down > kNegInf) {
+        high = key;
+        key = tries < 4 || high - low < 4 ? static_cast<uint32_t>(down) : low + (high - low) / 2;
+      } else if (equal == 0) {
+        key = static_cast<uint32_t>(up);
+      } else {
+        double n = ceil((target - sum) / one);
+        if (!(n >= 1.0)) n = 1.0;
+        unsigned long long m = n < static_cast<double>(equal) ? static_cast<unsigned long long>(n) : equal;
+        while (m > 1 && sum + static_cast<double>(m - 1) * one >= target) --m;
+        while (m < equal && sum + static_cast<double>(m) * one < target) ++m;
+        by_sum = Border{key, static_cast<int>(m > 0 ? m : 1)};
+        break;
+      }
+    }
+    if (less(by_sum, border)) border = by_sum;
+  }
+  // ---- min-p
+  const Border by_size{min_p_key(e, R.temperature, R.min_p, max_key), 0x7fffffff};
+  bool counted = bracketed.there;
+  if (less(by_size, border)) { border = by_size; counted = false; }
+  if (static_cast<double>(R.min_p) > 1.0) { border = Border{max_key, 1}; counted = false; }
+
+  // ---- how many are kept, and the index up to which tokens with the border's key are
+  unsigned long long above = 0, equal = 0;
+  int cut = V;
+  if (counted) {
+    above = bracketed.kept;
+    cut = bracketed.cut;
+  } else {
+    for (int v = tid; v < V; v += kThreads) {
+      const uint32_t k = key_of(load_logit<HALF>(row, v));
+      above += k > border.key ? 1 : 0;
+      equal += k == border.key ? 1 : 0;
+    }
+    above = block_sum_u(S, above);
+    equal = block_sum_u(S, equal);
+  }
+  if (equal > static_cast<unsigned long long>(border.ties)) {
+    // index of the ties-th: stretches of tokens per thread, counted in order
+    const int stretch = (V + kThreads - 1) / kThreads, v0 = min(tid * stretch, V), v1 = min(v0 + stretch, V);
+    unsigned mine = 0;
+    for (int v = v0; v < v1; ++v) mine += key_of(load_logit<HALF>(row, v)) == border.key ? 1 : 0;
+    unsigned incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    __syncthreads();
+    if (lane == 31) S.u[warp] = incl;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) incl += static_cast<unsigned>(S.u[w]);
+    unsigned n = incl - mine;
+    const unsigned ties = static_cast<unsigned>(border.ties);
+    if (n < ties && incl >= ties) {
+      for (int v = v0; v < v1; ++v)
+        if (key_of(load_logit<HALF>(row, v)) == border.key && ++n == ties) { S.cut = v; break; }
+    }
+    __syncthreads();
+    cut = S.cut;
+    equal = ties;
+  }
+  if (tid == 0 && A.kept_out) A.kept_out[s] = static_cast<int>(above + equal);
+  if (d1 <= d0) return;
+
+  // ---- sums of the kept tokens, segment by segment
+  auto kept_term = [&](int v) -> double {
+    if (v >= V) return 0.0;
+    const float x = load_logit<HALF>(row, v);
+    const uint32_t k = key_of(x);
+    return k > border.key || (k == border.key && v <= cut) ? e(x) : 0.0;
+  };
+  const int n_seg = (V + kSeg - 1) / kSeg;
+  for (int g = warp; g < n_seg; g += kWarps) {
+    double sum = 0.0;
+    for (int x = lane; x < kSeg; x += 32) sum += kept_term(g * kSeg + x);
+    sum = warp_sum_d(sum);
+    if (lane == 0) S.seg[g] = sum;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    double run = 0.0;
+    for (int g0 = 0; g0 < n_seg; g0 += 32) {
+      const double incl = warp_scan_d(g0 + lane < n_seg ? S.seg[g0 + lane] : 0.0, lane) + run;
+      if (g0 + lane < n_seg) S.seg[g0 + lane] = incl;
+      run = __shfl_sync(0xffffffffu, incl, 31);
+    }
+  }
+  __syncthreads();
+  const double total = S.seg[n_seg - 1];
+  for (int64_t d = d0 + warp; d < d1; d += kWarps) {
+    const float u = A.uniforms[d];
+    const double target = (u < 1.f ? fmaxf(u, 0.f) : 1.f) * total;
+    int lo = 0, hi = n_seg;                                    // the first segment whose end exceeds the target
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (S.seg[mid] > target) hi = mid; else lo = mid + 1;
+    }
+    if (lo == n_seg) {                                         // none: the last one that adds something
+      lo = n_seg - 1;
+      while (lo > 0 && !(S.seg[lo] > S.seg[lo - 1])) --lo;
+    }
+    double run = lo > 0 ? S.seg[lo - 1] : 0.0;
+    int token = -1, last = -1;
+    for (int x = 0; x < kSeg && token < 0; x += 32) {
+      const int v = lo * kSeg + x + lane;
+      const double t = kept_term(v);
+      const double incl = warp_scan_d(t, lane) + run;
+      const unsigned over = __ballot_sync(0xffffffffu, t > 0.0 && incl > target), any = __ballot_sync(0xffffffffu, t > 0.0);
+      if (over) token = lo * kSeg + x + __ffs(over) - 1;
+      if (any) last = lo * kSeg + x + 31 - __clz(any);
+      run = __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) {
+      A.tokens_out[d] = token >= 0 ? token : last;             // (the two sums of a segment may differ in their last bits)
+      if (A.seq_out) A.seq_out[d] = s;
+    }
+  }
+  __syncthreads();
+}
+
 // The rows that were split, from the lists of their parts, and all that a list was not enough for.
 struct FinishShared {
   union {
@@ -1274,7 +1498,7 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
   FinishShared& M = *reinterpret_cast<FinishShared*>(smem);
   const int tid = threadIdx.x;
   M.S.count[tid] = 0;
-  M.S.mass[tid] = 0;
+  for (int x = 0; x < 3; ++x) M.S.part[x][tid] = 0;
   make_table(M.S.table);
   __syncthreads();
   for (int s = A.whole_rows + blockIdx.x; s < A.n_seq; s += gridDim.x) {
@@ -1311,7 +1535,7 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
     const bool done = list_row<HALF>(A, M.S, M.list, s, d0, d1, R, fits ? static_cast<int>(n) : 0, fits, low, mx, z, base);
     __syncthreads();
     if (!done) {
-      whole_row<HALF>(A, M.whole, M.S.table, s);
+      whole_row<HALF>(A, M.whole, M.S, M.list, s);
       __syncthreads();
     }
   }
@@ -1320,7 +1544,7 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
     const int64_t mine = s0 + static_cast<int64_t>(tid & 31) * gridDim.x;
     unsigned marked = __ballot_sync(0xffffffffu, mine < A.whole_rows && A.marks[mine] != 0);
     for (; marked; marked &= marked - 1) {
-      whole_row<HALF>(A, M.whole, M.S.table, static_cast<int>(s0 + static_cast<int64_t>(__ffs(marked) - 1) * gridDim.x));
+      whole_row<HALF>(A, M.whole, M.S, M.list, static_cast<int>(s0 + static_cast<int64_t>(__ffs(marked) - 1) * gridDim.x));
       __syncthreads();
     }
   }
@@ -1371,7 +1595,7 @@ static int32_t launch(Args A, cudaStream_t st) {
   }
   const int grid = A.whole_rows >= blocks ? blocks : A.whole_rows > rest * A.parts ? A.whole_rows : rest * A.parts;
   SS_LAUNCH(list_rows_kernel<HALF>, grid, kListThreads, sizeof(RowsShared), st, A);
-  const int finish = A.n_seq < blocks ? A.n_seq : blocks;
+  const int finish = A.n_seq < blocks ? A.n_seq : blocks;      // (two blocks an SM here as well)
   SS_LAUNCH(finish_rows_kernel<HALF>, finish, kListThreads, sizeof(FinishShared), st, A);
   return SS_OK;
 }
