@@ -240,3 +240,20 @@ def test_graph_streams_and_offsets_that_do_not_start_at_zero():
         B.ss_filtered_sample(d2, ws2, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(tok, want) and torch.equal(tok2, want)
+
+
+@pytest.mark.parametrize("kind", ["normal", "grid", "head", "masked"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_that_keep_many(kind, dtype):
+    """More kept tokens than fit a list: by top-k, by top-p, by min-p, by nothing, and with two of them."""
+    V = 60001
+    for seed, f in enumerate([dict(k=20000), dict(k=9000, T=1.5), dict(p=0.99, T=1.5), dict(p=0.7, T=4.0), dict(m=1e-4, T=2.0),
+                              dict(k=20000, p=0.9, T=2.0), dict(p=0.99, m=0.003, T=1.5), dict(k=30000, m=0.01, T=1.5), dict(T=1.2), dict(k=59000, p=0.999, m=1e-5, T=3.0)]):
+        check(rows(seed + 20, 3, V, kind, dtype), [3, 0, 40], seed=seed, **f)
+
+
+def test_every_block_has_rows_and_parts():
+    """Row numbers around whole rounds of one row a block: left-over rows are split, into many parts or none."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for n in (1, 2, sms, 2 * sms - 1, 2 * sms, 2 * sms + 1, 2 * sms + sms // 2, 2 * sms + sms + 3):
+        check(rows(n, n, 9001, "head"), [1] * n, 0.9, 0, 0.9, 0.0, seed=n)
