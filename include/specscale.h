@@ -311,7 +311,7 @@ int32_t ss_kv_append(const ss_attn_desc_t* desc /* host */, const ss_rows_t* row
  *
  *   draft_parent  int32, by row of q (q_src_offsets[p] + t or q_offsets[p] + t; host bound: q_src_rows or total_q), or NULL: every
  *                 draft continues the one before it (the causal step of ss_tree_attention)
- *   T             0 .. SS_MAX_DRAFT (0: the path is skipped, its rows - none - are not written)
+ *   T             0 .. SS_MAX_DRAFT (0: the path is skipped)
  *   nodes         any length anywhere on a chain; pool, strides, alignments, out and lse as for ss_tree_attention; max_sms is kept to
  *   flags         as for ss_tree_attention: SS_FLAG_FORCE_GENERIC or SS_FLAG_NO_TCGEN05 run one row per warp on the CUDA cores (a
  *                 second opinion), the others make no difference (index arrays are always checked)
@@ -419,13 +419,13 @@ int32_t ss_branch_sample_upto(const float* logits, const int64_t* draw_offsets, 
  *   min-p      n_m = the tokens with  e >= m, at least one                             m <= 0 (or NaN): all
  *   kept       the first min(n_k, n_p, n_m) tokens
  *   a draw     with uniform u is the smallest kept v with  C_v > u * C,  C_v = sum of e over kept tokens up to index v, C over all
- * all evaluated in fp64 (so that a decision is that of the definition but for differences of about 1e-12 of a sum).  T = 0 keeps
+ * all evaluated in fp64 (so that a decision is that of the definition but for differences of about 1e-13 of a sum).  T = 0 keeps
  * the first token alone.  A row that holds a NaN or +inf, or no finite logit, or whose T is negative, NaN or infinite, has no
  * distribution: its draws are -1 and 0 tokens are kept.  A uniform outside [0, 1) counts as the nearer end, a NaN as the upper one.
  *
  *   logits        fp32 or bf16 [n_seq], rows of `vocab` at row_stride elements; any alignment of a row
  *   draw_offsets, uniforms, tokens_out, seq_out  as for ss_branch_sample; seq_out may be NULL; tokens_out and seq_out hold draws
- *                 draw_offsets[0] .. draw_offsets[n_seq]-1 at their own index
+ *                 draw_offsets[0] .. draw_offsets[n_seq]-1 at their own index (and may be NULL where there are none)
  *   temperature, top_k, top_p, min_p   [n_seq] on the device, or NULL: the scalar of that name for every sequence
  *   kept_out      int32 [n_seq] or NULL: tokens kept
  *   workspace     >= ss_filtered_sample_workspace_bytes(desc) bytes, 256-byte aligned.  Calls that share one must not overlap

@@ -141,6 +141,15 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _call(device, function, *args, stream=None) -> int:
+    """function(*args, stream) with `device` (an index; None: the current one) current: a kernel runs where its tensors are, on that
+    device's current stream unless one is given."""
+    if device is None or device == torch.cuda.current_device():
+        return function(*args, _stream(stream))
+    with torch.cuda.device(device):
+        return function(*args, _stream(stream))
+
+
 def _check(rc: int, where: str):
     if rc != SS_OK:
         raise SpecScaleError(rc, where)
@@ -370,6 +379,7 @@ def ss_tree_attention(desc: ss_attn_desc_t, workspace: torch.Tensor, stream=None
 
 # ---------------------------------------------------------------------------------------------------------
 class ss_rows_t(ctypes.Structure):
+    _device = None                           # (of make_rows' tensors)
     _fields_ = [
         ("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32),
         ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
@@ -410,13 +420,14 @@ def make_rows(*, q=None, k=None, v=None, q_out=None, k_out=None, positions=None,
     for w in (q_weight, k_weight):
         assert w is None or (w.dtype == torch.bfloat16 and w.numel() == 128)
     r.inv_freq, r.positions, r.q_weight, r.k_weight = _ptr(inv_freq), _ptr(positions), _ptr(q_weight), _ptr(k_weight)
+    r._device = device.index if device is not None else None
     r._keep = (q, k, v, q_out, k_out, positions, inv_freq, q_weight, k_weight)
     return r
 
 
 def ss_qk_norm_rope(rows: ss_rows_t, stream=None, check=True) -> int:
     """Norms of queries and / or keys per head (where there are weights) and the rotation to their positions, in one pass."""
-    rc = lib().ss_qk_norm_rope(ctypes.byref(rows), _stream(stream))
+    rc = _call(rows._device, lib().ss_qk_norm_rope, ctypes.byref(rows), stream=stream)
     if check:
         _check(rc, "ss_qk_norm_rope")
     return rc
@@ -425,7 +436,7 @@ def ss_qk_norm_rope(rows: ss_rows_t, stream=None, check=True) -> int:
 def ss_kv_append(desc: ss_attn_desc_t, rows: ss_rows_t, stream=None, check=True) -> int:
     """Keys (normalised, rotated) and values of a step into the pool slots that the attention with `desc` reads them from, queries
     (if given) into q_out."""
-    rc = lib().ss_kv_append(ctypes.byref(desc), ctypes.byref(rows), _stream(stream))
+    rc = _call(rows._device, lib().ss_kv_append, ctypes.byref(desc), ctypes.byref(rows), stream=stream)
     if check:
         _check(rc, "ss_kv_append")
     return rc
@@ -441,7 +452,9 @@ def ss_draft_attention(desc: ss_attn_desc_t, draft_parent: Optional[torch.Tensor
                        check=True) -> int:
     """ss_tree_attention's paths with a TREE of tokens (int32 parent by row, -1: the cached text) in place of the causal step."""
     assert draft_parent is None or draft_parent.dtype == torch.int32
-    rc = lib().ss_draft_attention(ctypes.byref(desc), _ptr(draft_parent), _ptr(workspace), workspace.numel(), _stream(stream))
+    assert draft_parent is None or draft_parent.device == workspace.device
+    rc = _call(workspace.device.index, lib().ss_draft_attention, ctypes.byref(desc), _ptr(draft_parent), _ptr(workspace),
+               workspace.numel(), stream=stream)
     if check:
         _check(rc, "ss_draft_attention")
     return rc
@@ -488,6 +501,7 @@ def ss_branch_sample(logits, draw_offsets, uniforms, n_seq, vocab, temperature, 
 
 
 class ss_sample_desc_t(ctypes.Structure):
+    _device = None                           # (of make_sample_desc's tensors)
     _fields_ = [
         ("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32),
         ("n_seq", ctypes.c_int32), ("vocab", ctypes.c_int32),
@@ -523,6 +537,7 @@ def make_sample_desc(*, logits, draw_offsets, uniforms, tokens_out, seq_out=None
             setattr(d, name + "_all", value)
     d.draw_offsets, d.uniforms, d.tokens_out = _ptr(draw_offsets), _ptr(uniforms), _ptr(tokens_out)
     d.seq_out, d.kept_out = _ptr(seq_out), _ptr(kept_out)
+    d._device = logits.device.index
     d._keep = (logits, draw_offsets, uniforms, tokens_out, seq_out, kept_out, temperature, top_k, top_p, min_p)
     return d
 
@@ -535,7 +550,8 @@ def ss_filtered_sample_workspace_bytes(desc: ss_sample_desc_t) -> int:
 
 def ss_filtered_sample(desc: ss_sample_desc_t, workspace: torch.Tensor, stream=None, check=True) -> int:
     """Draws behind temperature, top-k, top-p and min-p (see the header), any number for each sequence."""
-    rc = lib().ss_filtered_sample(ctypes.byref(desc), _ptr(workspace), workspace.numel(), _stream(stream))
+    assert desc._device in (None, workspace.device.index)
+    rc = _call(workspace.device.index, lib().ss_filtered_sample, ctypes.byref(desc), _ptr(workspace), workspace.numel(), stream=stream)
     if check:
         _check(rc, "ss_filtered_sample")
     return rc

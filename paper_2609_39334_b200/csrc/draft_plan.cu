@@ -48,6 +48,7 @@ __global__ void __launch_bounds__(kPlanThreads) draft_plan_kernel(const __grid_c
         }
         if (a >= 0) bad = a < P.num_nodes ? SS_ERR_UNSUPPORTED : SS_ERR_BAD_INPUT;       // deeper than SS_MAX_DEPTH
         if (I.leaf < 0 || I.leaf >= P.num_nodes || I.T < 0) bad = SS_ERR_BAD_INPUT;
+        if (pages > 0 && P.num_pages < 1) bad = SS_ERR_BAD_INPUT;
         if (I.T > SS_MAX_DRAFT || tokens > 0x3fffffff) bad = SS_ERR_UNSUPPORTED;
         if (bad == SS_OK && (I.src < 0 || I.src + I.T > P.q_rows || I.dst < 0 || I.dst + I.T > P.total_q)) bad = SS_ERR_BAD_INPUT;
         I.L = static_cast<int>(tokens);

@@ -331,7 +331,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         for (int c = 0; c < 64; c += 2) e[(c >> 1) & 3] = max3(e[(c >> 1) & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
         const float mx = fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
         float alpha = 1.f;
-        const bool move = mx > m + lazy_raw;                                     // (also for a row's first visible key)
+        const bool move = mx > m + lazy_raw || (m == -INFINITY && mx > -INFINITY);   // (the row's first visible key)
         if (move) {
           alpha = ex2((m - mx) * cl2);                                           // 0 for the first
           m = mx;
@@ -444,7 +444,8 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             store_lines(row_valid ? dst + c0 : nullptr, o, lane);
           }
         }
-        if (row_valid && !finite) C.redo[seq & 1] = 1;
+        // (hidden keys are drafts: where none is near, what is not finite is the result)
+        if (row_valid && !finite && (U.holes || (U.tile0 + n_tiles) * kTile > U.drafts0)) C.redo[seq & 1] = 1;
         if (row_valid && (dual || s == 0)) {
           if (U.slot >= 0) P.part_lse[static_cast<int64_t>(U.slot) * (2 * kRows) + (dual && s ? kRows : 0) + row] = lse;
           else if (P.lse) P.lse[(U.dst + tok_base + i) * P.Hq + U.g * G + hl] = lse;

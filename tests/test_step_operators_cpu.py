@@ -154,3 +154,25 @@ def test_sample_arguments(lib):
     size = B.ss_filtered_sample_workspace_bytes(sample())
     assert size % 256 == 0 and call(nbytes=size - 1) == B.SS_ERR_WORKSPACE_TOO_SMALL
     assert lib.ss_filtered_sample_workspace_bytes(ctypes.byref(sample()), None) == B.SS_ERR_INVALID_ARG
+
+
+def test_a_call_runs_on_the_device_of_its_tensors(monkeypatch):
+    at, seen = [0], []
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, at[0] = at[0], self.index
+
+        def __exit__(self, *a):
+            at[0] = self.before
+
+    monkeypatch.setattr(B.torch.cuda, "current_device", lambda: at[0])
+    monkeypatch.setattr(B.torch.cuda, "device", Device)
+    monkeypatch.setattr(B, "_raw_stream", lambda device: 40 + device)
+    call = lambda *a: seen.append((at[0],) + a) or B.SS_OK
+    for device, stream in ((None, None), (0, None), (2, None), (2, 7)):
+        B._call(device, call, "x", stream=stream)
+    assert seen == [(0, "x", 40), (0, "x", 40), (2, "x", 42), (2, "x", 7)] and at[0] == 0
