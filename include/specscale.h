@@ -7,6 +7,10 @@
  *                       multi-token step per path)
  *   ss_topk_prune       selection of the surviving candidates by score
  *
+ * and of what stands around the attention in a step of a model: ss_qk_norm_rope and ss_kv_append (norms and positions of queries
+ * and keys, a step's keys and values into the pool), ss_draft_attention (trees of drafted tokens), ss_branch_sample and
+ * ss_filtered_sample (tokens from logits).
+ *
  * Conventions (all entry points)
  *   - Unless a parameter says "host", every pointer is a DEVICE pointer owned by the caller.  The library
  *     allocates no memory and keeps no state between calls; scratch comes from a caller-provided workspace
@@ -165,7 +169,8 @@ int32_t ss_dedup_paths_static(const int32_t* tok_ids, const int64_t* tok_offsets
  *     no visible key  =>  out = 0, lse = -inf.
  *
  * The step's own keys/values are expected to be in the pool already (they are the last T tokens of the
- * path's leaf node; appending them is outside this call).  Positional encoding is outside this call.
+ * path's leaf node; ss_kv_append puts them there).  Positional encoding is outside this call (ss_qk_norm_rope, or on the
+ * way in ss_kv_append).
  *
  * Tree: nodes are numbered parents-before-children; node n holds node_kv_len[n] tokens in the pages
  * node_pages[node_page_offsets[n] .. node_page_offsets[n+1]) (16 tokens each; only the last page may be

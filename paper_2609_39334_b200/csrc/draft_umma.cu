@@ -13,10 +13,17 @@
 // A stream's products are issued by one lane: S(q) = Q K^T of half step q goes out before O += P(q-1) V, so that the next scores are
 // there when the softmax is through with the last ones.  tcgen05 instructions of one thread run in order: S(q) may overwrite P(q-2),
 // and when S(q) is there, the products up to P(q-2) V are in the accumulator.
-// (With scores of 128 keys and one buffer a stream waited for P V and Q K^T after every softmax: 4150 clocks a step of two tiles
-// against 2500 for the softmax.)
-// Softmax of a half step: the row's exact maximum (the reference moves when it is exceeded by 2^8 only: exponentials stay below 2^8
-// and the accumulator is hardly ever rescaled), exponentials, their fp32 sum, probabilities in bf16 over the scores they come from.
+// (With scores of 128 keys in one buffer, Q K^T then with N = 128, a stream waits for P V and Q K^T after every softmax: 64 paths of 64
+// drafts over 5120 keys, 32q / 8kv heads, 364 us with the streams' products in turn from one warp, against 350.)
+// Softmax of a half step: exponentials relative to the reference there is, their fp32 sum, probabilities in bf16 over the scores they
+// come from; nothing waits for a maximum.  Where the sum exceeds 2^16 (or is none), where the row has no reference yet, and in steps with
+// masks, the scores are read (again) for their exact maximum, which becomes the reference if it exceeds that by 2^8; the accumulator is
+// then rescaled.  So no exponential is ever larger than 2^16, and no row pays for another block's.
+// What bounds it: a half step of both streams takes the tensor cores 1280 clocks (Q K^T with N = 64 reads more shared memory than it
+// multiplies for: 48 clocks an instruction, 32 of them products) and the special-function units 1024 for its exponentials.  Every fourth pair of
+// exponentials goes to the FMA pipe instead (exp2_pair): 378 -> 350 us in that case, every eighth pair 352, three of eight 353.  Both
+// streams together then take some 1700 clocks: their tails (load, vote, store: 400) hardly overlap.  Two threads a row and strict turns
+// of the streams at their exponentials were slower.  Run back to back the case draws 1000 W and the clocks fall to some 1.4 GHz.
 // Masks: from 128 bits per row (which drafts it sees) and the page's place in the chain, in steps that reach the drafts only.
 // Keys that nobody may read (behind a node's end) have their V rows cleared in shared memory; a draft that holds NaN or an infinity
 // and is hidden from some rows reaches them as 0 * NaN: a row that is not finite is computed again, key by key, without it.
@@ -39,6 +46,7 @@ constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
 constexpr int kOffQ = 0, kOffK = 65536, kOffV = kOffK + kStagesK * kStageBytes;
 constexpr int kSmem = kOffV + kStagesV * kStageBytes;
 constexpr float kLazyLog2 = 8.0f;
+constexpr float kMostSum = 65536.0f;           // of a half step's exponentials
 
 struct Unit {
   int valid;                                   // 0: the block's work is done
@@ -76,6 +84,30 @@ __device__ __forceinline__ f32x2 pack2(float a, float b) { f32x2 r; asm("mov.b64
 __device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float clamped(float x) {              // to [-126, 127], NaN remains
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-126.f));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(127.f));
+  return x;
+}
+// 2^x of two values on the FMA pipe: n = the nearest integer to x, 2^(x - n) by a polynomial of degree 5 (its largest relative error on
+// [-1/2, 1/2] made smallest: 2.3e-7 with fp32's roundings, as the special-function unit's), n added to the exponent.  What lies outside
+// [-126, 127] counts as the end of it; a NaN or more than 2^126 comes out as that or as more than 2^126.
+__device__ __forceinline__ void exp2_pair(float& a, float& b) {
+  const float kRound = 12582912.0f;                              // 1.5 * 2^23
+  const f32x2 x = pack2(clamped(a), clamped(b)), t = add2(x, pack2(kRound, kRound)), n = add2(t, pack2(-kRound, -kRound));
+  const f32x2 f = fma2(n, pack2(-1.f, -1.f), x);
+  f32x2 p = pack2(0.0013276473619043827f, 0.0013276473619043827f);
+  p = fma2(p, f, pack2(0.009675541892647743f, 0.009675541892647743f));
+  p = fma2(p, f, pack2(0.05550713092088699f, 0.05550713092088699f));
+  p = fma2(p, f, pack2(0.24022120237350464f, 0.24022120237350464f));
+  p = fma2(p, f, pack2(0.6931469440460205f, 0.6931469440460205f));
+  p = fma2(p, f, pack2(1.0000001192092896f, 1.0000001192092896f));
+  float t0, t1, p0, p1;
+  unpack2(t, t0, t1);
+  unpack2(p, p0, p1);
+  a = __uint_as_float((__float_as_uint(t0) << 23) + __float_as_uint(p0));
+  b = __uint_as_float((__float_as_uint(t1) << 23) + __float_as_uint(p1));
+}
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 pk = __floats2bfloat162_rn(a, b);
@@ -311,49 +343,86 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           continue;
         }
         tc_fence_after();
-        uint32_t sr[64];
-        tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
-        tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
-        tmem_wait_ld();
-        if (U.holes || jt * kTile + hf * 64 + 64 > U.drafts0) {                   // (block-uniform) not everything is seen
-          const int pages = U.C.first[U.C.n];
+        uint32_t sr[64], pr[32];
+        uint32_t (&sr0)[32] = *reinterpret_cast<uint32_t(*)[32]>(&sr[0]), (&sr1)[32] = *reinterpret_cast<uint32_t(*)[32]>(&sr[32]);
+        const f32x2 cl2_2 = pack2(cl2, cl2);
+        f32x2 sum2[2];
+        // Exponentials of 32 scores; `fast`: some on the FMA pipe (where none is of a masked key).
+        auto exps = [&](int c0, f32x2 nmc2, bool fast) {
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int vp = jt * kTilePages + hf * 4 + w;
-            const uint32_t mask = vp < pages ? page_mask(U.C, segment_of(U.C, vp), vp, U.drafts0, seen) : 0u;
-#pragma unroll
-            for (int c = 0; c < 16; ++c)
-              if (!((mask >> c) & 1u)) sr[16 * w + c] = 0xff800000u;             // -inf
+          for (int c = c0; c < c0 + 32; c += 2) {
+            const f32x2 x = fma2(pack2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), cl2_2, nmc2);
+            float e0, e1;
+            unpack2(x, e0, e1);
+            if (fast && (c & 6) == 6) {
+              exp2_pair(e0, e1);
+            } else {
+              e0 = ex2(e0);
+              e1 = ex2(e1);
+            }
+            sum2[(c >> 1) & 1] = add2(sum2[(c >> 1) & 1], pack2(e0, e1));
+            pr[c >> 1] = pack_bf16(e0, e1);
           }
+        };
+        auto sum_of = [&]() {
+          float a0, a1, a2, a3;
+          unpack2(sum2[0], a0, a1);
+          unpack2(sum2[1], a2, a3);
+          return (a0 + a1) + (a2 + a3);
+        };
+        const bool masked = U.holes || jt * kTile + hf * 64 + 64 > U.drafts0;    // (block-uniform) not everything is seen
+        bool fits = !masked && !__any_sync(0xffffffffu, row_valid && m == -INFINITY);
+        float alpha = 1.f, sum = 0.f;
+        bool move = false;
+        tmem_ld32(t_s, sr0);
+        if (fits) {                            // by the reference there is
+          const f32x2 nmc2 = pack2(-m * cl2, -m * cl2);
+          sum2[0] = sum2[1] = pack2(0.f, 0.f);
+          tmem_wait_ld();
+          tmem_pin32(sr0);
+          tmem_ld32(t_s + 32, sr1);
+          exps(0, nmc2, true);
+          tmem_wait_ld();
+          tmem_pin32(sr1);
+          exps(32, nmc2, true);
+          sum = sum_of();
+          fits = !__any_sync(0xffffffffu, row_valid && !(sum <= kMostSum));      // (not for a NaN)
+          if (!fits) tmem_ld32(t_s, sr0);
         }
-        float e[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (!fits) {                           // by the maximum
+          tmem_ld32(t_s + 32, sr1);
+          tmem_wait_ld();
+          tmem_pin32(sr0);
+          tmem_pin32(sr1);
+          if (masked) {
+            const int pages = U.C.first[U.C.n];
 #pragma unroll
-        for (int c = 0; c < 64; c += 2) e[(c >> 1) & 3] = max3(e[(c >> 1) & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
-        const float mx = fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
-        float alpha = 1.f;
-        const bool move = mx > m + lazy_raw || (m == -INFINITY && mx > -INFINITY);   // (the row's first visible key)
-        if (move) {
-          alpha = ex2((m - mx) * cl2);                                           // 0 for the first
-          m = mx;
-          l *= alpha;
-        }
-        const float mc = m == -INFINITY ? 0.f : m * cl2;
-        const f32x2 cl2_2 = pack2(cl2, cl2), nmc2 = pack2(-mc, -mc);
-        f32x2 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-        uint32_t pr[32];
+            for (int w = 0; w < 4; ++w) {
+              const int vp = jt * kTilePages + hf * 4 + w;
+              const uint32_t mask = vp < pages ? page_mask(U.C, segment_of(U.C, vp), vp, U.drafts0, seen) : 0u;
 #pragma unroll
-        for (int c = 0; c < 64; c += 2) {
-          float x0, x1;
-          unpack2(fma2(pack2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), cl2_2, nmc2), x0, x1);
-          const float e0 = ex2(x0), e1 = ex2(x1);
-          sum2[(c >> 1) & 1] = add2(sum2[(c >> 1) & 1], pack2(e0, e1));
-          pr[c >> 1] = pack_bf16(e0, e1);
+              for (int c = 0; c < 16; ++c)
+                if (!((mask >> c) & 1u)) sr[16 * w + c] = 0xff800000u;           // -inf
+            }
+          }
+          float e[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < 64; c += 2) e[(c >> 1) & 3] = max3(e[(c >> 1) & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
+          const float mx = fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
+          move = row_valid && (mx > m + lazy_raw || (m == -INFINITY && mx > -INFINITY));    // (the row's first visible key)
+          if (move) {
+            alpha = ex2((m - mx) * cl2);                                         // 0 for the first
+            m = mx;
+            l *= alpha;
+          }
+          const float mc = m == -INFINITY ? 0.f : m * cl2;
+          sum2[0] = sum2[1] = pack2(0.f, 0.f);
+          exps(0, pack2(-mc, -mc), false);
+          exps(32, pack2(-mc, -mc), false);
+          sum = sum_of();
         }
         tmem_st32(t_s, pr);                                                      // over the scores they come from
-        float a0, a1, a2, a3;
-        unpack2(sum2[0], a0, a1);
-        unpack2(sum2[1], a2, a3);
-        l += (a0 + a1) + (a2 + a3);
+        l += sum;
         if (__any_sync(0xffffffffu, move && q > 0)) {                            // rescale O (warp-collective), once P(q-1) V is in it:
           // the scores of the half step after this one were asked for behind that product
           const uint32_t gn = gq + 1;

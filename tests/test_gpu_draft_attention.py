@@ -215,6 +215,49 @@ def test_scores_of_any_size(flags):
         c.check()
 
 
+def _key(c, p, t, g):
+    """Key row of token t of path p's own node."""
+    n = c.chain[p][-1]
+    return c.pool[int(c.pages[c.off[n] + t // 16]), 0, g, t % 16]
+
+
+@pytest.mark.parametrize("sms", [0, 2])
+@pytest.mark.parametrize("flags", PATHS)
+def test_scores_that_rise_along_the_sequence(flags, sms):
+    """A maximum that comes late: a little above what was before, far above, beyond what a float's exponent holds, again and again."""
+    c = Case(30, 8, 2, [[900], [700], [260]], [50, 3, 64])
+    c.desc.max_sms = sms
+    for t, f in ((70, 6.0), (133, 30.0), (200, 400.0), (500, 1.5), (640, 900.0)):
+        for g in range(2):
+            _key(c, 0, t, g).mul_(f)
+    for t in range(64, 700, 64):                                         # every half step above the last one
+        for g in range(2):
+            _key(c, 1, t, g).mul_(2.0 + t / 20)
+    for t in range(1, 324):                                              # and a slope without an end
+        _key(c, 2, t, 0).mul_(1 + t / 8)
+    assert c.run(flags) == B.SS_OK
+    c.check()
+
+
+@pytest.mark.parametrize("flags", PATHS)
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+def test_cached_key_that_is_no_number(flags, what):
+    """It is visible to every row of its head: none of them is finite, and the other head's are as they were."""
+    c = Case(31, 8, 2, [[600]], [20])
+    assert c.run(flags) == B.SS_OK
+    before = c.out[:20].clone()
+    _key(c, 0, 300, 0)[5] = what
+    assert c.run(flags) == B.SS_OK
+    finite = torch.isfinite(c.out[:20].double()).all(-1)
+    if what != what:
+        assert not bool(finite[:, :4].any())
+    else:
+        # a score of -inf has no weight, one of +inf leaves nothing else
+        up = c.q[:20, :4, 5] > 0
+        assert not bool(finite[:, :4][up].any()) and bool(finite[:, :4][c.q[:20, :4, 5] < 0].all())
+    assert torch.equal(c.out[:20, 4:], before[:, 4:])
+
+
 @pytest.mark.parametrize("flags", PATHS)
 def test_query_rows_elsewhere_padded_pool_and_live_paths(flags):
     T = [5, 9, 33, 2]
