@@ -149,6 +149,11 @@ __device__ __forceinline__ long long path_cost(const PathInfo& I, int Hkv) {
   return I.T > 0 ? static_cast<long long>(I.tiles) * I.blocks * Hkv : 0;
 }
 
+// (A division of 64 bits takes some hundred clocks.)
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return (a | b) >> 31 ? a / b : static_cast<int>(a) / static_cast<int>(b);
+}
+
 // The next unit of this block's line into slot `dst` (whole warp).
 __device__ __noinline__ void fetch_unit(Ctrl& C, const Params& P, int dst, int lane) {
   Unit& U = C.unit[dst];
@@ -160,15 +165,29 @@ __device__ __noinline__ void fetch_unit(Ctrl& C, const Params& P, int dst, int l
   }
   int path = C.path;
   long long off = C.off;
+  // (the chain's words are on their way while the path is looked at: it is the right one for all but a path's last unit)
+  constexpr int kWords = static_cast<int>(sizeof(Chain) / 4), kMine = (kWords + 31) / 32;
+  uint32_t word[kMine];
+  auto load_chain = [&]() {
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(P.chains + path);
+#pragma unroll
+    for (int x = 0; x < kMine; ++x) word[x] = x * 32 + lane < kWords ? from[x * 32 + lane] : 0u;
+  };
+  load_chain();
   PathInfo I = P.paths[path];
-  while (off >= path_cost(I, P.Hkv)) {         // (ends: steps are left)
-    off -= path_cost(I, P.Hkv);
-    I = P.paths[++path];
+  if (off >= path_cost(I, P.Hkv)) {            // (ends: steps are left)
+    do {
+      off -= path_cost(I, P.Hkv);
+      I = P.paths[++path];
+    } while (off >= path_cost(I, P.Hkv));
+    load_chain();
   }
-  const uint32_t* from = reinterpret_cast<const uint32_t*>(P.chains + path);
   uint32_t* to = reinterpret_cast<uint32_t*>(&U.C);
-  for (int i = lane; i < static_cast<int>(sizeof(Chain) / 4); i += 32) to[i] = from[i];
-  const int u = static_cast<int>(off / I.tiles), tile0 = static_cast<int>(off - static_cast<long long>(u) * I.tiles);
+#pragma unroll
+  for (int x = 0; x < kMine; ++x)
+    if (x * 32 + lane < kWords) to[x * 32 + lane] = word[x];
+  const int u = static_cast<int>(quotient(off, I.tiles));
+  const int tile0 = static_cast<int>(off - static_cast<long long>(u) * I.tiles);
   const int n_tiles = static_cast<int>(min(static_cast<long long>(I.tiles - tile0), end - pos));
   __syncwarp();
   if (lane == 0) {
@@ -186,7 +205,7 @@ __device__ __noinline__ void fetch_unit(Ctrl& C, const Params& P, int dst, int l
     const bool first = pos == quota * blockIdx.x, whole = n_tiles == I.tiles;
     U.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (first ? 0 : 1);
     if (!whole && tile0 == 0) {                // it starts here and ends with block `last`: the merge begins at this block
-      const int last = static_cast<int>((pos + I.tiles - 1) / quota);
+      const int last = static_cast<int>(quotient(pos + I.tiles - 1, quota));
       P.cuts[blockIdx.x] = CutUnit{last - static_cast<int>(blockIdx.x) + 1, U.slot, U.g, U.n_tok, U.dst};
     }
     C.pos = pos + n_tiles;
@@ -229,7 +248,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abort_flag = &C.abort_flag;
 
-  if (tid == 0) {
+  if (tid == kThreads - 32) {                  // (a warp that has few paths to look at)
     C.abort_flag = (smem_u32(smem) & 1023u) ? 1 : 0;
     C.redo[0] = C.redo[1] = C.stop = 0;
     for (int s = 0; s < 2; ++s) { mbar_init(&C.unit_ready[s], 1); mbar_init(&C.unit_free[s], kSoftmaxWarps + 3); }
@@ -278,9 +297,8 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     total += C.warp_total[w];
   }
   incl += before;
-  const long long quota = max((total + gridDim.x - 1) / gridDim.x, 1LL), start = quota * blockIdx.x;
-  if (tid == 0) { C.pos = start; C.end = min(start + quota, total); C.quota = quota; C.path = 0; C.off = 0; }
-  __syncthreads();
+  const long long quota = max(quotient(total + gridDim.x - 1, gridDim.x), 1LL), start = quota * blockIdx.x;
+  if (tid == 0) { C.pos = start; C.end = min(start + quota, total); C.quota = quota; }
   if (start < total && incl - mine <= start && start < incl) {
     C.path = p0;
     C.off = start - (incl - mine);
@@ -553,7 +571,6 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         }
         __syncwarp();
       };
-      if (which == 0 && seq == 0) load_q();
       // The pages of four steps at a time, one a lane, a block ahead of their use; one elected lane issues the copies.
       auto pool_row = [&](int j, int pg) -> int {
         const int vp = (U.tile0 + j) * kTilePages + pg;
@@ -562,6 +579,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       };
       int* coord = C.coord[which];
       int cur = pool_row(lane >> 3, lane & 7);
+      if (which == 0 && seq == 0) load_q();
       for (int j0 = 0; j0 < n_tiles && ok; j0 += 4) {
         const int nxt = pool_row(j0 + 4 + (lane >> 3), lane & 7);
         coord[lane] = cur;
