@@ -161,9 +161,7 @@ __device__ __forceinline__ double warp_scan_d(double v, int lane) {
 // a running sum (fp64).  Where more are kept: borders by find_on_list, the kept ones sorted by index.  A draw is a thread's.
 // Two blocks an SM, so that one is in its pass while the other is on its list.  In the pass every lane has the next four vectors on
 // their way to shared memory while it works on the last four: 16 warps then ask for as much as an SM's share of the bandwidth takes
-// (straight into registers, with room for four vectors, a block got 11.8 bytes a clock, alone or beside the other one), and the lines
-// behind those are asked into the L2 (922 rows of 151936: 151 -> 146 us, 300 of 128256 67.6 -> 63.5; with the next row's first lines, too,
-// asked for in front of the list 148 and 64.5).  Rows that are
+// (straight into registers, with room for four vectors, a block got 11.8 bytes a clock, alone or beside the other one).  Rows that are
 // left over behind whole rounds, one a block, are split over the blocks: each hands its part's list over in the workspace, the next
 // kernel puts them together.
 constexpr int kListThreads = 512, kListWarps = kListThreads / 32;
@@ -676,8 +674,6 @@ __device__ __forceinline__ void pass_row(const Args& A, uint4 (&ring)[4][32], Ro
     }
     __syncwarp();
     if (v0 + kStep < L.vec1) fetch(v0 + kStep);
-    const int far = v0 + 2 * kStep + lane * 8;                 // (a line is 8 vectors)
-    if (lane < 16 && far < L.vec1) asm volatile("prefetch.global.L2 [%0];" ::"l"(L.vecs + far));
     // 16 tokens at a time
 #pragma unroll
     for (int g = 0; g < (HALF ? 2 : 1); ++g) {
