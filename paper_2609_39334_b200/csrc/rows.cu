@@ -12,8 +12,9 @@
 // in fp32), the whole turns off, the rest through sincospif.  Sums, norm and rotation are fp32, two values an instruction, with
 // weight and angle in one factor per lane: y = r (x A + x' B), r the norm's.
 // Bound: HBM, every row read and written once, and issue slots not far behind (a row takes 22 clocks of an SM's share of the
-// bandwidth, and about 30 warp instructions).  What a token needs - row, place, position - is looked up by one lane each, for a
-// warp's whole run of tokens at once.
+// bandwidth, and about 30 warp instructions).  65536 tokens of 32 + 8 heads take 230 us, 5.8 TB/s; the steps of 64 of 1024 paths into the
+// pool, 32 + 16 heads, 286 us, 5.6 TB/s; eight tokens 4.5 us, the launch and three trips to memory.  What a token needs - row, place,
+// position - is looked up by one lane each, for a warp's whole run of tokens at once.
 #include "common.cuh"
 
 namespace ss {
