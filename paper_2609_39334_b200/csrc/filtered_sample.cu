@@ -870,17 +870,19 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
           if (limit || (whole && h == m_list)) { total = S.z; error = 0.0; }
           int least, most;
           double target;
+          // (a sum that is 0, infinite or none says nothing: terms out of range)
+          auto known = [](double x) { return x > 0.0 && x < static_cast<double>(INFINITY); };
           for (int round = 0;; ++round) {
             target = static_cast<double>(R.top_p) * total;
             least = 1 + list_count(tid < n && sum < target * (1.0 - error));
             most = 1 + list_count(tid < n && sum < target * (1.0 + error));
             // (too close to tell, and nothing else ends before: by the exact sum, whose own error no longer counts)
-            if (!add_up || round == 1 || !((least < most && least <= n && end > least) || !(target > 0.0))) break;
+            if (!add_up || round == 1 || !((least < most && least <= n && end > least) || !known(target))) break;
             make_exact();
             total = total_quick;
             error = 0.0;
           }
-          if (!(target > 0.0)) sure = false;
+          if (!known(target)) sure = false;
           else if (least == most && least <= n) end = min(end, least);
           else if (least <= n) sure = end <= least;            // too close to tell, unless something else ends before
         }
@@ -906,7 +908,7 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
     }
   }
   if (!sure) return false;
-  if (kept == 0 && add_up && error_quick > kFixError) make_exact();
+  if (kept == 0 && add_up && !(error_quick <= kFixError)) make_exact();
   const bool wide = kept == 0;
   if (wide) kept = wide_list(S, list, R, e, A.vocab, m_list, low_key, max_key, limit, greedy, whole, add_up, total_quick, error_quick);
   if (kept == 0) return false;
@@ -1523,7 +1525,8 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
     float mx = has ? parts[lane].max : -INFINITY;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    const float low = warp_max(has ? parts[lane].low : kLowest), base = parts[0].base;
+    // (the largest base is that of all: a part far below it adds nothing, and no factor exceeds 1)
+    const float low = warp_max(has ? parts[lane].low : kLowest), base = warp_max(has ? parts[lane].base : -INFINITY);
     const double z = warp_sum_d(has && add_up ? parts[lane].sum * exp2(static_cast<double>(parts[lane].base) - static_cast<double>(base)) : 0.0);
     if (fits) {
       for (int p = warp; p < A.parts; p += kListWarps) {

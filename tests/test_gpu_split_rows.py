@@ -1,0 +1,58 @@
+"""ss_filtered_sample on rows that several blocks share (few sequences, or those left over behind whole rounds), against the definition
+in 64 bits: the parts of such a row see only what is theirs, and their sums are relative to what each of them saw."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_filtered_sample as plain
+from paper_2609_39334_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+V = 151936
+
+
+def part_starts(n, dtype, vocab=V):
+    """First tokens of the parts of a row where n rows are left over (a part's first 16 bytes are among those that it samples)."""
+    per_vec = 4 if dtype == torch.float32 else 8
+    blocks = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    parts = min(blocks // n, vocab // 4096, 32)
+    assert parts >= 2 and vocab % per_vec == 0
+    per = -(-(vocab // per_vec) // parts)
+    return [p * per * per_vec for p in range(parts)]
+
+
+def answers(row, n, T, p, m, u=(0.0, 0.5, 1 - 2.0 ** -24)):
+    """(kept, tokens [n, len(u)]) of n copies of one row, top-p and min-p."""
+    x = row.to(DEV).expand(n, V).contiguous()
+    off = torch.arange(0, len(u) * n + 1, len(u), dtype=torch.int64, device=DEV)
+    tokens, kept = torch.full((len(u) * n,), -7, dtype=torch.int32, device=DEV), torch.full((n,), -7, dtype=torch.int32, device=DEV)
+    d = B.make_sample_desc(logits=x, draw_offsets=off, uniforms=torch.tensor(u, device=DEV).repeat(n), tokens_out=tokens, kept_out=kept,
+                           temperature=T, top_p=p, min_p=m)
+    B.ss_filtered_sample(d, B.alloc_workspace(B.ss_filtered_sample_workspace_bytes(d), DEV))
+    return kept.cpu().numpy(), tokens.view(n, -1).cpu().numpy()
+
+
+@pytest.mark.parametrize("n", [1, 9, 100, 148])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,top", [(0.014, 10.0), (0.014, 10.375), (0.01, 7.1875), (0.01, 7.375), (0.0121, 9.0), (0.014, 10.9375), (0.002, 5.0),
+                                   (1e-5, 10.0)])
+def test_parts_that_lie_a_float_s_exponent_apart(n, dtype, T, top):
+    """Sums of parts whose largest terms are 2^1024 and more apart: the larger one is what counts, and top-p ends where it says also
+    where min-p alone would keep more.  (Four equal tokens over noise 600 and more natural orders below them: whole numbers.)"""
+    starts = part_starts(n, dtype)
+    for at in {starts[len(starts) // 2 + len(starts) // 8], starts[-1]}:
+        x = 0.001 * torch.randn(1, V, generator=torch.Generator().manual_seed(1))
+        x[0, at:at + 4] = top
+        for p, m, want in ((0.4, 0.1, 2), (0.4, 0.0, 2), (0.9, 0.1, 4), (0.2, 0.5, 1)):
+            kept, tokens = answers(x.to(dtype), n, T, p, m)
+            assert (kept == want).all(), (p, m, kept)
+            assert (tokens == [at, at + want // 2, at + want - 1]).all()
+        if n == 1:
+            plain.check(x.to(dtype), [40], T, 0, 0.4, 0.1)
+    if dtype == torch.float32:
+        x[0, at + 1:at + 4] = top + T * math.log(0.05)
+        kept, tokens = answers(x, n, T, 0.8, 0.02)                          # (weights 1, 0.05, 0.05, 0.05: the first is 0.87)
+        assert (kept == 1).all() and (tokens == at).all()
