@@ -524,13 +524,15 @@ __device__ __forceinline__ RowKind kind_of(const RowParams& R, int V) {
   k.add_up = k.fine && !k.greedy && !k.whole && !k.by_k && R.top_p < 1.f;
   return k;
 }
-// Relative error of a quick sum: terms 2^(fma(l, c', -base)) by the special-function unit (documented: 2^-22), c' = log2(e) / T in fp32,
-// eight added pairwise (three roundings of 2^-24), from there in fp64.  An exponent x is off by 2^-24 |x| (its rounding) and 2^-25 |l c|
-// (that of c'); |x| is at most `far` for the largest term and log2 V further on average over the terms (the entropy of the row).  About
-// 3e-6: where a row's end by top-p lies closer to a token's than that, its sum is made again in fp64 (exact_total).
-__device__ __forceinline__ double quick_error(double base, double far, int V) {
-  const double x = 33 - __clz(V) + far;
-  return 0.6932 * (0x1p-24 * x + 0x1p-25 * (x + fabs(base))) + 0x1p-22 + 4 * 0x1p-24;
+// Bound of a quick sum's relative error: terms 2^(fma(l, c', -base)) by the special-function unit (documented: 2^-22), c' = log2(e) / T in
+// fp32, eight added pairwise (three roundings of 2^-24), from there in fp64.  The exponent x of a term is off by 2^-24 |x| (its rounding),
+// and relative to the largest term by 2^-24 of their distance (the rounding of c').  On average over the terms, each with its weight,
+// a distance from the largest is at most log2 V (the entropy of the row), |x| at most `far` more: the largest one's, or, of a row
+// in parts, which have bases of their own, the mean over the parts by their sums.  About 2e-6 where the sample saw the largest terms: where a
+// row's end by top-p lies closer to a token's than that, its sum is made again in fp64 (exact_total).
+__device__ __forceinline__ double quick_error(double far, int V) {
+  const double spread = 33 - __clz(V);
+  return 0.6932 * 0x1p-24 * (2.0 * spread + far) + 0x1p-22 + 4 * 0x1p-24;
 }
 __device__ __forceinline__ float quick_c(const RowParams& R) { return static_cast<float>(1.4426950408889634 / static_cast<double>(R.temperature)); }
 // The sum of all of a row's terms (the threads of a list).
@@ -727,10 +729,10 @@ __device__ __forceinline__ void passed(const RowBuffer& B, float& mx, double& z)
   for (int w = 1; w < kListWarps; ++w) { mx = max_nan(mx, B.max[w]); z += B.sum[w]; }
 }
 
-// Row s from its list (all of it): false, and nothing given, where the list cannot tell.
+// Row s from its list (all of it): false, and nothing given, where the list cannot tell.  z, base, far: its quick sum, see quick_error.
 template <bool HALF>
 __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned long long* list, int s, int64_t d0, int64_t d1, const RowParams& R,
-                                         int m_list, bool fits, float low, float mx, double z, float base) {
+                                         int m_list, bool fits, float low, float mx, double z, float base, double far) {
   const int tid = threadIdx.x % kListThreads, lane = tid & 31, warp = tid >> 5;
   const RowKind K = kind_of(R, A.vocab);
   const bool fine = K.fine, greedy = K.greedy, by_k = K.by_k, whole = K.whole, add_up = K.add_up;
@@ -756,7 +758,7 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
   if (add_up) {
     const double top = e.max * static_cast<double>(quick_c(R));
     total_quick = z * exp2(static_cast<double>(base) - top);
-    error_quick = quick_error(base, fabs(top - base), A.vocab);
+    error_quick = quick_error(far, A.vocab);
   }
   // (once it is needed)
   auto make_exact = [&]() {
@@ -818,8 +820,8 @@ __device__ __forceinline__ bool list_row(const Args& A, ListShared& S, unsigned 
         total = static_cast<double>(S.all) / kFix;
         error = kFixError;
       }
-      const double far = static_cast<double>(R.top_p) * total * (1.0 + 2.0 * error) * kFix;
-      const unsigned long long target = limit ? static_cast<unsigned long long>(R.top_k) : far < 1.8e19 ? __double2ull_ru(far) : ~0ull;
+      const double most = static_cast<double>(R.top_p) * total * (1.0 + 2.0 * error) * kFix;
+      const unsigned long long target = limit ? static_cast<unsigned long long>(R.top_k) : most < 1.8e19 ? __double2ull_ru(most) : ~0ull;
       if (incl >= target && incl - here < target) S.bin = bin;
       list_sync();
       // (top-p's share is of all that top-k keeps: min-p must not shorten those then)
@@ -1000,7 +1002,7 @@ __global__ void __launch_bounds__(kListThreads, 2) list_rows_kernel(const __grid
       passed(B, mx, z);
       if (job.parts == 1) {
         const bool done = list_row<HALF>(A, M.S, B.list, job.s, B.d0, B.d1, B.R, static_cast<int>(min(B.n, static_cast<unsigned>(kCap))), B.n <= kCap,
-                                   B.low, mx, z, B.base);
+                                   B.low, mx, z, B.base, fabs(static_cast<double>(mx) * quick_c(B.R) - B.base));
         if (tid == 0) A.marks[job.s] = done ? 0 : 1;
       } else {
         Part& P = A.part[block];
@@ -1527,7 +1529,9 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
     for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     // (the largest base is that of all: a part far below it adds nothing, and no factor exceeds 1)
     const float low = warp_max(has ? parts[lane].low : kLowest), base = warp_max(has ? parts[lane].base : -INFINITY);
-    const double z = warp_sum_d(has && add_up ? parts[lane].sum * exp2(static_cast<double>(parts[lane].base) - static_cast<double>(base)) : 0.0);
+    const double mine = has && add_up ? parts[lane].sum * exp2(static_cast<double>(parts[lane].base) - static_cast<double>(base)) : 0.0;
+    const double z = warp_sum_d(mine);
+    const double far = warp_sum_d(mine != 0.0 ? mine * fabs(static_cast<double>(parts[lane].max) * quick_c(R) - parts[lane].base) : 0.0) / z;
     if (fits) {
       for (int p = warp; p < A.parts; p += kListWarps) {
         const unsigned count = __shfl_sync(0xffffffffu, m, p), to = __shfl_sync(0xffffffffu, first, p);
@@ -1535,7 +1539,7 @@ __global__ void __launch_bounds__(kListThreads, 2) finish_rows_kernel(const __gr
       }
     }
     __syncthreads();
-    const bool done = list_row<HALF>(A, M.S, M.list, s, d0, d1, R, fits ? static_cast<int>(n) : 0, fits, low, mx, z, base);
+    const bool done = list_row<HALF>(A, M.S, M.list, s, d0, d1, R, fits ? static_cast<int>(n) : 0, fits, low, mx, z, base, far);
     __syncthreads();
     if (!done) {
       whole_row<HALF>(A, M.whole, M.S, M.list, s);

@@ -56,3 +56,24 @@ def test_parts_that_lie_a_float_s_exponent_apart(n, dtype, T, top):
         x[0, at + 1:at + 4] = top + T * math.log(0.05)
         kept, tokens = answers(x, n, T, 0.8, 0.02)                          # (weights 1, 0.05, 0.05, 0.05: the first is 0.87)
         assert (kept == 1).all() and (tokens == at).all()
+
+
+def test_a_part_whose_largest_terms_its_sample_missed():
+    """Two tokens that hold nearly all of the mass stand 65 powers of two above what their part's sample saw: their exponents are rounded
+    to 2^-17, by 2^-18 downwards here (M log2(e) + 64 lies that far above a multiple of 2^-17), so the part's rough sum lacks 2.6e-6 of
+    itself.  Top-p's target is a little above the first of them (1e-7 of it; 2^-24 of rounding in p)."""
+    M, low = 0.700008749961853, -44.25
+    starts = part_starts(1, torch.float32)
+    x = -40 - torch.rand(1, V, generator=torch.Generator().manual_seed(3))
+    a, b = starts[20], starts[21]
+    x[0, a:b] = low - torch.rand(b - a, generator=torch.Generator().manual_seed(4))
+    x[0, a:a + 4] = low                                                  # (sampled: what the part's sum is relative to)
+    x[0, a + 1089] = x[0, a + 3753] = M                                  # (not sampled: vectors 272 and 938 of 1187, 32 of every 74 are)
+    for beside in (1.0, 2.0, 3.0):
+        x[0, 0] = M - beside
+        total = float(np.exp(x[0].double().numpy() - float(np.float32(M))).sum())
+        p = np.float32(1.0 / total)
+        while float(p) * total <= 1 + 6e-8:
+            p = np.nextafter(p, np.float32(1))
+        assert float(p) * total < 1 + 3e-7
+        assert (plain.check(x, [5], 1.0, 0, p, 0.0) == 2).all()
