@@ -514,15 +514,15 @@ class ss_sample_desc_t(ctypes.Structure):
 
 def make_sample_desc(*, logits, draw_offsets, uniforms, tokens_out, seq_out=None, kept_out=None, temperature=1.0, top_k=0, top_p=1.0,
                      min_p=0.0) -> ss_sample_desc_t:
-    """Fills ss_sample_desc_t.  logits: fp32 or bf16 [n_seq][vocab] of any row stride; temperature, top_k, top_p, min_p: a number for
-    every sequence, or a device tensor with one each.  The returned object keeps references to the tensors."""
+    """Fills ss_sample_desc_t.  logits: fp32 or bf16 [n_seq][vocab] of any row stride from vocab on; temperature, top_k, top_p, min_p: a
+    number for every sequence, or a device tensor with one each.  The returned object keeps references to the tensors."""
     d = ss_sample_desc_t()
     d.struct_size = ctypes.sizeof(ss_sample_desc_t)
     assert logits.is_cuda and logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] <= 1)
     assert logits.dtype in (torch.float32, torch.bfloat16)
     d.n_seq, d.vocab = logits.shape
     d.logits_type = SS_LOGITS_BF16 if logits.dtype == torch.bfloat16 else SS_LOGITS_FP32
-    d.row_stride = max(logits.stride(0), d.vocab)
+    d.row_stride = logits.stride(0) if d.n_seq > 1 else max(logits.stride(0), d.vocab)      # (rows that overlap: the call refuses them)
     d.logits = logits.data_ptr()
     assert draw_offsets.dtype == torch.int64 and draw_offsets.numel() == d.n_seq + 1
     assert uniforms.dtype == torch.float32 and tokens_out.dtype == torch.int32
