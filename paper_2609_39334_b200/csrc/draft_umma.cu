@@ -29,7 +29,7 @@
 // and is hidden from some rows reaches them as 0 * NaN: a row that is not finite is computed again, key by key, without it.
 // Roles: warps 0-3, 4-7 streams; 8 K and Q through TMA and the next unit's description; 9 V through TMA; 10, 11 issue the streams'
 // products.  They go from unit to unit on their own (descriptions in two slots): while the streams write a unit's rows out, the
-// next one's first keys and its queries are on their way and multiplied.  Every wait is bounded (see umma.cuh).
+// next one's first keys and its queries are on their way and multiplied.  Every wait is bounded (see umma.cuh, wait_behind_rows).
 #include "draft_attn.cuh"
 #include "umma.cuh"
 
@@ -74,6 +74,26 @@ struct Ctrl {
 };
 static_assert(sizeof(Ctrl) + kSmem <= 232448, "shared memory of a block");
 
+// mbar_wait of a role that the softmax warps keep waiting while they compute rows again (unit_rows_exact: 0.35 us a row and key of a warp, 0.2 s
+// at 18000 keys of 256 rows, and no wait in it that could fail to end).  The limit counts from when they were last seen at that.
+__device__ __forceinline__ bool wait_behind_rows(uint64_t* bar, uint32_t parity, Ctrl& C) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const volatile int* redo = C.redo;
+  volatile int* abort_flag = &C.abort_flag;
+  long long t0 = 0;
+  uint32_t spins = 0;
+  while (!mbar_try_wait_suspend(bar, parity, 20000u)) {
+    if ((++spins & 15u) != 0u) continue;
+    if (*abort_flag) return false;
+    if (t0 == 0 || (redo[0] | redo[1]) != 0) {
+      t0 = clock64();
+    } else if (clock64() - t0 > kWaitCycles) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+  return true;
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -313,7 +333,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   uint32_t seq = 0;
 
   // The next unit, when its description is there; false: none, or a wait has run out.
-  auto unit_there = [&]() -> bool { return mbar_wait(&C.unit_ready[seq & 1], (seq >> 1) & 1, abort_flag); };
+  auto unit_there = [&]() -> bool { return wait_behind_rows(&C.unit_ready[seq & 1], (seq >> 1) & 1, C); };
   auto unit_done = [&]() {
     __syncwarp();
     if (lane == 0) mbar_arrive(&C.unit_free[seq & 1]);
@@ -558,7 +578,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       bool ok = true;
       // Q rows, once the products of the unit before have read theirs (behind the first steps' keys, which need not wait for that)
       auto load_q = [&]() {
-        if (seq > 0) ok = mbar_wait(&C.q_free, (seq - 1) & 1, abort_flag);
+        if (seq > 0) ok = wait_behind_rows(&C.q_free, (seq - 1) & 1, C);
         ok = __all_sync(0xffffffffu, ok);
         if (ok && elect_one()) {
           mbar_arrive_expect_tx(&C.q_full, static_cast<uint32_t>((dual ? 2 : 1) * 2 * 128 * G * tpt));
@@ -591,7 +611,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           const int n_pages = max(0, min(kTilePages, pages - jt * kTilePages));
           const bool last = (jt + 1) * kTilePages >= pages;
           const bool clear = which == 1 && (U.holes || (last && U.clear_last));
-          if (u > 0) ok = mbar_wait(&empty[st], (u - 1) & 1, abort_flag);
+          if (u > 0) ok = wait_behind_rows(&empty[st], (u - 1) & 1, C);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           uint8_t* dst = ring + st * kStageBytes;
@@ -613,7 +633,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           }
           __syncwarp();
           if (clear) {                                           // V rows of keys that are none
-            ok = mbar_wait(&C.v_land, n_land & 1, abort_flag);
+            ok = wait_behind_rows(&C.v_land, n_land & 1, C);
             ++n_land;
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -640,7 +660,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       }
       if (which == 0) {
         const int next = (seq & 1) ^ 1;
-        if (seq > 0) ok = mbar_wait(&C.unit_free[next], ((seq - 1) >> 1) & 1, abort_flag) && ok;
+        if (seq > 0) ok = wait_behind_rows(&C.unit_free[next], ((seq - 1) >> 1) & 1, C) && ok;
         __syncwarp();
         fetch_unit(C, P, next, lane);
         __syncwarp();
@@ -660,7 +680,7 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         auto issue_qk = [&](int q) -> bool {
           const uint32_t gq = n_half + q, gj = g_tile + (dual ? q >> 1 : q);
           const int sk = gj % kStagesK, hf = dual ? q & 1 : s;
-          if (!mbar_wait(&C.k_full[sk], (gj / kStagesK) & 1, abort_flag)) return false;
+          if (!wait_behind_rows(&C.k_full[sk], (gj / kStagesK) & 1, C)) return false;
           tc_fence_after();
           const uint64_t k_desc = smem_desc_advance(k_desc0, static_cast<uint32_t>(sk) * kStageBytes + hf * 16384u);
 #pragma unroll
@@ -672,12 +692,12 @@ draft_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           if (q + 1 == halves) mma_commit(&C.q_free);
           return true;
         };
-        bool ok = mbar_wait(&C.q_full, seq & 1, abort_flag) && issue_qk(0);
+        bool ok = wait_behind_rows(&C.q_full, seq & 1, C) && issue_qk(0);
         for (int q = 0; q < halves && ok; ++q) {
           if (q + 1 < halves) ok = issue_qk(q + 1);
           const uint32_t gq = n_half + q, gj = g_tile + (dual ? q >> 1 : q);
           const int sv = gj % kStagesV, hf = dual ? q & 1 : s;
-          ok = ok && mbar_wait(&C.v_full[sv], (gj / kStagesV) & 1, abort_flag) && mbar_wait(&C.p_full[s][gq & 1], (gq >> 1) & 1, abort_flag);
+          ok = ok && wait_behind_rows(&C.v_full[sv], (gj / kStagesV) & 1, C) && wait_behind_rows(&C.p_full[s][gq & 1], (gq >> 1) & 1, C);
           if (!ok) break;
           tc_fence_after();
           const uint64_t v_desc = smem_desc_advance(v_desc0, static_cast<uint32_t>(sv) * kStageBytes + hf * 16384u);
