@@ -238,11 +238,11 @@ extern "C" int32_t ss_draft_attention(const ss_attn_desc_t* d, const int32_t* dr
   if (d->max_sms > 0 && d->max_sms < sms) sms = d->max_sms;
   SS_LAUNCH(draft_plan_kernel, d->num_paths < 1 ? 1 : d->num_paths < 65535 ? d->num_paths : 65535, kPlanThreads, 0, st, P);
   if (d->num_paths == 0) return SS_OK;
-  if (d->flags & (SS_FLAG_FORCE_GENERIC | SS_FLAG_NO_TCGEN05)) {
+  // (without rows as well: it has none to work on then, and hands on what the planner found wrong)
+  if (d->total_q == 0 || (d->flags & (SS_FLAG_FORCE_GENERIC | SS_FLAG_NO_TCGEN05))) {
     SS_LAUNCH(draft_plain_kernel, static_cast<unsigned>(d->num_paths < 65535 ? d->num_paths : 65535) * kPlainBlocks, kPlainWarps * 32, 0, st, P);
     return SS_OK;
   }
-  if (d->total_q == 0) return SS_OK;
   const int32_t tiles = launch_tiles(P, st, sms);
   if (tiles != SS_OK) return tiles;
   SS_LAUNCH(draft_merge_kernel, sms * kMergeBlocks, kMergeWarps * 32, 0, st, P);

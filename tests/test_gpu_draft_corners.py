@@ -27,3 +27,28 @@ def test_rows_computed_again_over_a_long_cache():
     assert bool(torch.isfinite(got).all())
     assert bool(((got - o[rows]).abs() <= to[rows]).all()) and bool(((c.lse[rows].double() - l[rows]).abs() <= tl[rows]).all())
     assert bool(torch.isnan(c.out[hidden].double()).any(-1).all())
+
+
+@pytest.mark.parametrize("flags", draft.PATHS)
+def test_calls_without_rows_report_what_is_wrong(flags):
+    """total_q = 0: nothing is written, and the status is what it is for any other call."""
+    for what, want in (("nothing", B.SS_OK), ("steps", B.SS_ERR_BAD_INPUT), ("drafts", B.SS_ERR_UNSUPPORTED), ("leaf", B.SS_ERR_BAD_INPUT),
+                       ("length", B.SS_ERR_BAD_INPUT), ("depth", B.SS_ERR_UNSUPPORTED)):
+        chains = [[16] * (B.SS_MAX_DEPTH + 1), [40]] if what == "depth" else [[100], [40]]
+        c = draft.Case(13, 8, 2, chains, [0, 0])
+        node_parent, node_len, path_leaf, path_T, offs, q_offs = c.tensors
+        if what == "steps":
+            path_T[1] = 3
+        elif what == "drafts":
+            path_T[0] = B.SS_MAX_DRAFT + 1
+        elif what == "leaf":
+            path_leaf[1] = 2
+        elif what == "length":
+            node_len[0] = 1000
+        assert c.desc.total_q == 0
+        c.desc.q = c.desc.out = None                                     # (not needed without rows)
+        assert c.run(flags) == want, what
+        assert bool((c.out == 7).all()) and bool((c.lse == 7).all())
+    # (no paths at all)
+    c.desc.num_paths = 0
+    assert c.run(flags) == B.SS_OK
