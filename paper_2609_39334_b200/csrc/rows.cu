@@ -67,9 +67,10 @@ struct Lane {
 };
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
-struct WarpShared {
+struct alignas(16) WarpShared {                // (sines and cosines are read two at a time: 8 bytes)
   float cs[64], sn[64];
 };
+static_assert(alignof(WarpShared) % alignof(float2) == 0 && sizeof(WarpShared) % alignof(float2) == 0, "pairs of angles");
 
 __device__ __forceinline__ f32x2 pack2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
