@@ -199,7 +199,7 @@ struct ListShared {
   unsigned long long u[kListWarps];
   double z;
 };
-constexpr int kPartCap = 2048;                                 // entries of a part's list
+constexpr int kPartCap = kCap / 2;                             // entries of a part's list: twice what begin_row wants of one of two parts
 struct Part {                                                  // of a row, in the workspace
   unsigned n;
   float low, base, max;

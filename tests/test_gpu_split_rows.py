@@ -77,3 +77,30 @@ def test_a_part_whose_largest_terms_its_sample_missed():
             p = np.nextafter(p, np.float32(1))
         assert float(p) * total < 1 + 3e-7
         assert (plain.check(x, [5], 1.0, 0, p, 0.0) == 2).all()
+
+
+def times(n, vocab, dtype, **f):
+    """Shortest of some calls on n rows, us."""
+    x = plain.rows(n, n, vocab, "head").to(dtype).to(DEV)
+    off, u = torch.arange(n + 1, device=DEV), torch.rand(n, device=DEV, generator=torch.Generator(device=DEV).manual_seed(n))
+    d = B.make_sample_desc(logits=x, draw_offsets=off, uniforms=u, tokens_out=torch.empty(n, dtype=torch.int32, device=DEV), **f)
+    ws = B.alloc_workspace(B.ss_filtered_sample_workspace_bytes(d), DEV)
+    best = math.inf
+    for _ in range(8):
+        a, b = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        a.record()
+        B.ss_filtered_sample(d, ws)
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, 1e3 * a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("f", [dict(top_p=0.5), dict(top_k=2048, top_p=0.95)])
+def test_rows_in_two_parts_fit_their_lists(dtype, f):
+    """Half the SMs' worth of rows, in two parts each, go by their lists as one row more does, none of which is split: a list that
+    overflows sends its row through passes over all of it, which takes ten times as long.  (Shortest of eight calls; 1.1 to 1 measured.)"""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert times(sms, V, dtype, **f) < 3 * times(sms + 1, V, dtype, **f)
+    assert times(2 * sms // 3 + 1, V, dtype, **f) < 3 * times(sms + 1, V, dtype, **f)
