@@ -52,3 +52,26 @@ def test_calls_without_rows_report_what_is_wrong(flags):
     # (no paths at all)
     c.desc.num_paths = 0
     assert c.run(flags) == B.SS_OK
+
+
+def test_thousands_of_paths():
+    """More paths than threads of a block: their costs are summed by stretches.  Every sixteenth against the definition, all of them
+    against the plain kernel (both within their tolerance of 2e-2)."""
+    r = torch.Generator().manual_seed(2)
+    n = 3100
+    chains = [[32, int(x)] for x in torch.randint(0, 40, (n,), generator=r)]
+    T = torch.randint(0, 4, (n,), generator=r).tolist()
+    c = draft.Case(17, 4, 2, chains, T, shared=(0,))
+    assert c.run(B.SS_FLAG_FORCE_GENERIC) == B.SS_OK
+    plain = c.out.clone(), c.lse.clone()
+    for sms in (0, 3):
+        c.desc.max_sms = sms
+        c.out.fill_(7.0)
+        c.lse.fill_(7.0)
+        assert c.run() == B.SS_OK
+        assert float((c.out.float() - plain[0].float()).abs().max()) <= 4e-2 and float((c.lse - plain[1]).abs().max()) <= 2e-3
+        for p in range(0, n, 16):
+            if T[p]:
+                o, l, to, tl = c.exact(p)
+                rows = slice(c.rows[p], c.rows[p] + T[p])
+                assert bool(((c.out[rows].double() - o).abs() <= to).all()) and bool(((c.lse[rows].double() - l).abs() <= tl).all())

@@ -104,3 +104,32 @@ def test_rows_in_two_parts_fit_their_lists(dtype, f):
     sms = torch.cuda.get_device_properties(0).multi_processor_count
     assert times(sms, V, dtype, **f) < 3 * times(sms + 1, V, dtype, **f)
     assert times(2 * sms // 3 + 1, V, dtype, **f) < 3 * times(sms + 1, V, dtype, **f)
+
+
+@pytest.mark.parametrize("n", [1, 12, 99, 148])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_masked_heads_and_low_temperatures(n, dtype):
+    """Rows with a masked beginning, end or middle, and temperatures from where one token is kept to where hundreds are."""
+    rng, vocab = np.random.default_rng(n), V if n < 99 else 33001
+    x = plain.rows(n, n, vocab, "head").to(dtype)
+    for r in range(n):
+        cut = int(rng.integers(1, vocab - 1))
+        if r % 3 == 0:
+            x[r, :cut] = -math.inf
+        elif r % 3 == 1:
+            x[r, cut:] = -math.inf
+        else:
+            x[r, cut // 2:cut] = -math.inf
+    T = rng.choice([1e-30, 1e-5, 0.003, 0.02, 0.1, 0.3, 1.0], n)
+    draws = rng.integers(0, 3, n)
+    plain.check(x, draws, T, 0, 0.9, 0.0)
+    plain.check(x, draws, T, 0, 0.9, 0.05)
+    plain.check(x, draws, T, rng.choice([0, 3, 50], n), 0.97, 0.01)
+
+
+@pytest.mark.parametrize("n", [99, 100, 148])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_two_parts_a_row(n, dtype):
+    x = plain.rows(n, n, 40001, "head").to(dtype)
+    plain.check(x, [1] * n, 1.0, 0, 0.9, 0.0)
+    plain.check(x, [1] * n, 0.8, 2048, 0.95, 0.0)
