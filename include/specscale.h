@@ -268,7 +268,8 @@ int32_t ss_tree_attention(const ss_attn_desc_t* desc /* host */, void* workspace
  * ss_draft_attention with the same descriptor expect them - token t of path p with T tokens is token node_kv_len - T + t of its
  * leaf node, whose length already counts the step - and writes q_out from q at the same positions (q NULL: no queries).  Row of a
  * path's token t: q_src_offsets[p] + t where the descriptor has these, else q_offsets[p] + t, in q, k, v, q_out and positions.
- * Position: `positions`, or, where that is NULL, the token's index in the path's whole sequence.
+ * Position: `positions`, or, where that is NULL, the token's index in the path's whole sequence.  That is right for a step that is a chain;
+ * the drafts of a tree that branches stand at cached length + depth (see ss_draft_attention) and need `positions`.
  * Of the descriptor it reads the heads, the pool, the tree, and the paths (q, out, lse, hints and flags are not used).  Paths are
  * unique and leaves private, as for the attention: two paths with the same leaf race.
  * Left alone: pool slots of other tokens; rows of no path.  Not written: keys and values of tokens in front of the leaf's first
@@ -313,6 +314,8 @@ int32_t ss_kv_append(const ss_attn_desc_t* desc /* host */, const ss_rows_t* row
  *   s_j = sm_scale * <q[t,h,:], K[j,g,:]>,   j < L - T, or j = L - T + d with d = t or an ancestor of t  (j >= 0)
  *   out[t,h,:] = sum_j softmax(s)_j V[j,g,:],   lse[t,h] = ln sum_j exp(s_j);   no visible key  =>  out = 0, lse = -inf
  * Keys and values that a token does not see may hold anything, NaN and infinities included, without an effect on it.
+ * Positional encoding is outside this call.  Draft t stands at L - T + depth, depth = 0 where it continues the cached text, else that of its
+ * parent + 1: ss_kv_append has to be given these `positions` unless the drafts are a chain (its default is L - T + t).
  *
  *   draft_parent  int32, by row of q (q_src_offsets[p] + t or q_offsets[p] + t; host bound: q_src_rows or total_q), or NULL: every
  *                 draft continues the one before it (the causal step of ss_tree_attention)

@@ -435,7 +435,8 @@ def ss_qk_norm_rope(rows: ss_rows_t, stream=None, check=True) -> int:
 
 def ss_kv_append(desc: ss_attn_desc_t, rows: ss_rows_t, stream=None, check=True) -> int:
     """Keys (normalised, rotated) and values of a step into the pool slots that the attention with `desc` reads them from, queries
-    (if given) into q_out."""
+    (if given) into q_out.  Without positions in `rows` a token's is its index in its path's sequence: drafts of a tree that branches
+    need them (cached length + depth)."""
     rc = _call(rows._device, lib().ss_kv_append, ctypes.byref(desc), ctypes.byref(rows), stream=stream)
     if check:
         _check(rc, "ss_kv_append")
