@@ -14,16 +14,17 @@
 // there when the softmax is through with the last ones.  tcgen05 instructions of one thread run in order: S(q) may overwrite P(q-2),
 // and when S(q) is there, the products up to P(q-2) V are in the accumulator.
 // (With scores of 128 keys in one buffer, Q K^T then with N = 128, a stream waits for P V and Q K^T after every softmax: 64 paths of 64
-// drafts over 5120 keys, 32q / 8kv heads, 364 us with the streams' products in turn from one warp, against 350.)
+// drafts over 5120 keys, 32q / 8kv heads, 364 us with the streams' products in turn from one warp, against 350 on the same box.)
 // Softmax of a half step: exponentials relative to the reference there is, their fp32 sum, probabilities in bf16 over the scores they
 // come from; nothing waits for a maximum.  Where the sum exceeds 2^16 (or is none), where the row has no reference yet, and in steps with
 // masks, the scores are read (again) for their exact maximum, which becomes the reference if it exceeds that by 2^8; the accumulator is
 // then rescaled.  So no exponential is ever larger than 2^16, and no row pays for another block's.
 // What bounds it: a half step of both streams takes the tensor cores 1280 clocks (Q K^T with N = 64 reads more shared memory than it
 // multiplies for: 48 clocks an instruction, 32 of them products) and the special-function units 1024 for its exponentials.  Every fourth pair of
-// exponentials goes to the FMA pipe instead (exp2_pair): 378 -> 350 us in that case, every eighth pair 352, three of eight 353.  Both
+// exponentials goes to the FMA pipe instead (exp2_pair): 378 -> 350 us in that case on that box, every eighth pair 352, three of eight 353.  Both
 // streams together then take some 1700 clocks: their tails (load, vote, store: 400) hardly overlap.  Two threads a row and strict turns
-// of the streams at their exponentials were slower.  Run back to back the case draws 1000 W and the clocks fall to some 1.4 GHz.
+// of the streams at their exponentials were slower.  How long the case takes goes by the clock that the power cap leaves: back to back over
+// changing inputs 415 us at 1.46 GHz and 985 W, 374 us with pauses between the calls (another box than the figures above).
 // Masks: from 128 bits per row (which drafts it sees) and the page's place in the chain, in steps that reach the drafts only.
 // Keys that nobody may read (behind a node's end) have their V rows cleared in shared memory; a draft that holds NaN or an infinity
 // and is hidden from some rows reaches them as 0 * NaN: a row that is not finite is computed again, key by key, without it.
