@@ -8,8 +8,9 @@
  *   ss_topk_prune       selection of the surviving candidates by score
  *
  * and of what stands around the attention in a step of a model: ss_qk_norm_rope and ss_kv_append (norms and positions of queries
- * and keys, a step's keys and values into the pool), ss_draft_attention (trees of drafted tokens), ss_branch_sample and
- * ss_filtered_sample (tokens from logits).
+ * and keys, a step's keys and values into the pool; with positions on several axes: ss_qk_norm_rope_axes, ss_kv_append_axes),
+ * ss_draft_attention (trees of drafted tokens), ss_key_weights and ss_kv_evict (which cached keys matter, and the others out of the
+ * pool), ss_logit_rules (penalties, biases and grammar masks), ss_branch_sample and ss_filtered_sample (tokens from logits).
  *
  * Conventions (all entry points)
  *   - Unless a parameter says "host", every pointer is a DEVICE pointer owned by the caller.  The library
@@ -305,6 +306,31 @@ int32_t ss_qk_norm_rope(const ss_rows_t* rows /* host */, void* stream);
 int32_t ss_kv_append(const ss_attn_desc_t* desc /* host */, const ss_rows_t* rows /* host */, void* stream);
 
 /* =========================================================================================================
+ * ss_qk_norm_rope_axes, ss_kv_append_axes - the two calls above where a token has a position on each of several axes.
+ *
+ * (Prompts with pictures or video: time, height, width.  Also what a chain needs whose cache has been cut, see ss_kv_evict: a token's
+ * position is no longer its index.)  The angle of pair i of a row r is
+ *   f = positions[pair_axis[i] * position_stride + r] * inv_freq[i],   i < rot_dim / 2
+ * and everything else, checks, places and errors included, as in the call without axes.  rows->positions has to be NULL.
+ *
+ *   num_axes   1 .. SS_MAX_AXES;  pair_axis int32 [rot_dim / 2], what lies outside [0, num_axes) counts as the nearer end
+ *   positions  int32 [num_axes] rows of n_rows at position_stride elements (>= n_rows; 0: every axis has the same ones)
+ * rot_dim = 0: neither array is read.  Errors: as without axes; SS_ERR_INVALID_ARG for a null array or a stride that is too small.
+ * ======================================================================================================= */
+#define SS_MAX_AXES 4
+typedef struct ss_axes {
+  uint32_t struct_size;              /* = sizeof(ss_axes_t) */
+  int32_t num_axes;
+  int64_t position_stride;
+  const int32_t* positions;
+  const int32_t* pair_axis;
+} ss_axes_t;
+
+int32_t ss_qk_norm_rope_axes(const ss_rows_t* rows /* host */, const ss_axes_t* axes /* host */, void* stream);
+int32_t ss_kv_append_axes(const ss_attn_desc_t* desc /* host */, const ss_rows_t* rows /* host */, const ss_axes_t* axes /* host */,
+                          void* stream);
+
+/* =========================================================================================================
  * ss_draft_attention - attention of trees of drafted tokens over the paged cache.
  *
  * (Speculative decoding on the substrate of Section "Experimental Setup"; the paper prints no formula.)  The descriptor is that
@@ -336,6 +362,104 @@ int32_t ss_kv_append(const ss_attn_desc_t* desc /* host */, const ss_rows_t* row
 int32_t ss_draft_attention_workspace_bytes(const ss_attn_desc_t* desc /* host */, size_t* out_bytes /* host */);
 int32_t ss_draft_attention(const ss_attn_desc_t* desc /* host */, const int32_t* draft_parent, void* workspace,
                            size_t workspace_bytes, void* stream);
+
+/* =========================================================================================================
+ * ss_key_weights - the attention weight that every cached key receives in a step, added up over the steps.
+ *
+ * (What an eviction goes by; the paper keeps every key and prints no formula.)  The descriptor is that of ss_tree_attention with the
+ * step's q and the lse that the attention wrote for it (here an INPUT; out is not used).  For key i of a node on the chain of at least
+ * one path, kv head g with its G = Hq / Hkv query heads:
+ *   s = sm_scale * <q[t,h,:], K[i,g,:]>
+ *   weights_out = decay * weights_in + sum over the paths below the node, their tokens t that see the key, heads h of g of
+ *                 exp(s - lse[t,h])
+ * Token t of a step of T sees the keys up to its own, as in ss_tree_attention.  With last_tokens > 0 only the last last_tokens tokens
+ * of each path's step add to the sums (an observation window behind a long prompt).  The step's own keys (the last T of the leaf) are
+ * new: their weights_in is taken as 0, and `order` of theirs becomes path_order + t.  A row with lse = -inf adds nothing.
+ * Keys that a token does not see, and what lies behind a node's end, may hold anything without an effect on the others.
+ *
+ *   weights_in, weights_out  fp32, weights_out may be weights_in; weights_in NULL: zeros.  Arrays beside the pool: element
+ *                            (page, kv head, token-in-page) at (page * num_kv_heads + head) * 16 + token, for num_pages pages,
+ *                            64-byte aligned
+ *   order        int32, the same layout, or NULL: sequence number of a key (ss_kv_evict keeps the first and the last by it)
+ *   path_order   int32 [num_paths] or NULL: sequence number of the first token of a path's step; NULL: the index of that token in the
+ *                path's whole sequence (right as long as nothing has been evicted)
+ *   decay        finite, >= 0;  last_tokens >= 0
+ * Nodes may have any length.  T <= node_kv_len of the leaf (T = 0: the path adds nothing, its chain's keys are still written).  A leaf with
+ * other paths below it: T <= 1.  The paths below a node are contiguous.
+ * SS_FLAG_FORCE_GENERIC or SS_FLAG_NO_TCGEN05 run one key per warp on the CUDA cores (a second opinion); max_sms is kept to; the other flags
+ * make no difference (index arrays are always checked).
+ *   workspace    >= ss_key_weights_workspace_bytes(desc, kw) bytes, 256-byte aligned; its size depends on the number of SMs of the current
+ *                device, num_nodes, num_paths and total_q.  Calls that share one must not overlap
+ * Accuracy (inputs ~N(0,1) in bf16): relative error of a sum below 1e-5.  Results do not depend on the run.
+ * Not written: weights and order of keys on no live path's chain, and behind a node's end.
+ * Errors (host): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE_TOO_SMALL, SS_ERR_CUDA.  Errors (device, via
+ * ss_last_device_status; weights of the nodes concerned are unspecified): SS_ERR_UNSUPPORTED (depth, a step longer than its leaf, a longer
+ * step of a leaf with other paths below it), SS_ERR_BAD_INPUT (index arrays out of range, paths below a node not contiguous), SS_ERR_TIMEOUT.
+ * ======================================================================================================= */
+typedef struct ss_key_weights {
+  uint32_t struct_size;              /* = sizeof(ss_key_weights_t) */
+  uint32_t flags;                    /* 0 */
+  float decay;
+  int32_t last_tokens;               /* 0: every token */
+  const float* weights_in;
+  float* weights_out;
+  int32_t* order;
+  const int32_t* path_order;
+} ss_key_weights_t;
+
+int32_t ss_key_weights_workspace_bytes(const ss_attn_desc_t* desc /* host */, const ss_key_weights_t* kw /* host */,
+                                       size_t* out_bytes /* host */);
+int32_t ss_key_weights(const ss_attn_desc_t* desc /* host */, const ss_key_weights_t* kw /* host */, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* =========================================================================================================
+ * ss_kv_evict - the keys of least weight leave a node of the cache; what stays is brought together in its first pages.
+ *
+ * For each of n_nodes different nodes, of n = node_kv_len keys, and each kv head by itself:
+ *   rank       keys that must stay - order < sinks, or order > (largest order of the node) - recent - first, by slot; then by weight,
+ *              largest first, equal ones by slot; NaN is the smallest weight
+ *   stay       the first k = min(keep, n) of this ranking (a negative keep counts as 0)
+ *   places     a key that stays in a slot < k remains there; the others move, in slot order, into the slots < k that have become free, in
+ *              order.  K and V rows, weight and order move together.  What the slots from k on hold is left as it was
+ *   kv_len_out[node] = k
+ * Slot i of a node is token i % 16 of its page i / 16; afterwards its pages from ceil(k / 16) on are free for other use.  Keys keep
+ * the rotation of their old position, so later tokens need explicit positions (ss_kv_append, ss_kv_append_axes).  It is called behind a
+ * step's attention and ss_key_weights, never between them: the step's own keys move, too.  A node with several paths below it must keep
+ * a multiple of 16 tokens if ss_tree_attention is to take it.
+ *
+ *   nodes, keep   int32 [n_nodes] on the device
+ *   weights       fp32 as in ss_key_weights;  weights_out the same layout, or NULL: weights is updated in place (it may also be given twice)
+ *   order         int32 as in ss_key_weights or NULL: the slot's number;  order_out the same layout, or NULL: in place
+ *                 In either output only the slots < k of the nodes are written
+ *   source_out    int32, the same layout, or NULL: the slot that the key of a slot < k was in (for arrays of the caller's own)
+ *   kv_len_out    int32 [num_nodes] or NULL; may be the descriptor's node_kv_len; only the n_nodes entries are written
+ *   sinks, recent >= 0
+ *   max_keys      host bound of the nodes' lengths (0: 16 * total_node_pages); decides how many SMs work on a node.  Longer nodes are right, too
+ * Of the descriptor it reads the heads, the pool (and writes it), and the tree without node_parent.
+ *   workspace     >= ss_kv_evict_workspace_bytes(desc, ev) bytes, 256-byte aligned (4 bytes a slot and kv head).  Calls that share one must not
+ *                 overlap
+ * Errors (host): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE_TOO_SMALL, SS_ERR_CUDA.  Errors (device, via
+ * ss_last_device_status): SS_ERR_BAD_INPUT (a node out of range, a length that its pages do not hold: the node is left as it is; a page outside the
+ * pool: its keys rank last, and nothing moves from or to it).
+ * ======================================================================================================= */
+typedef struct ss_evict {
+  uint32_t struct_size;              /* = sizeof(ss_evict_t) */
+  uint32_t flags;                    /* 0 */
+  int32_t n_nodes, max_keys;
+  int32_t sinks, recent;
+  const int32_t* nodes;
+  const int32_t* keep;
+  float* weights;
+  float* weights_out;
+  int32_t* order;
+  int32_t* order_out;
+  int32_t* source_out;
+  int32_t* kv_len_out;
+} ss_evict_t;
+
+int32_t ss_kv_evict_workspace_bytes(const ss_attn_desc_t* desc /* host */, const ss_evict_t* ev /* host */, size_t* out_bytes /* host */);
+int32_t ss_kv_evict(const ss_attn_desc_t* desc /* host */, const ss_evict_t* ev /* host */, void* workspace, size_t workspace_bytes,
+                    void* stream);
 
 /* =========================================================================================================
  * ss_topk_prune - keep the k best-scored candidates of every problem.
@@ -465,6 +589,60 @@ typedef struct ss_sample_desc {
 
 int32_t ss_filtered_sample_workspace_bytes(const ss_sample_desc_t* desc /* host */, size_t* out_bytes /* host */);
 int32_t ss_filtered_sample(const ss_sample_desc_t* desc /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
+/* =========================================================================================================
+ * ss_logit_rules - penalties of repeated tokens, biases and grammar masks on logits, in front of the samplers.
+ *
+ * (Of the paper's samplers, Section "Experimental Setup", which prints no formula.)  Per sequence s and token v, with logit x,
+ * c = how often v is in the sequence's history, and whether v is in its prompt:
+ *   1. v in the prompt or the history:  x = x / r where x > 0, else x * r       (r = repetition > 0; other values and NaN count as 1)
+ *   2. c > 0:                           x = x - frequency * c - presence
+ *   3. v in the sequence's bias list:   x = x + bias                            (a token that is there twice: its last entry counts)
+ *   4. v not allowed by its mask:       x = -inf
+ * in fp32, rounded once to the type of the logits.  A row may come out with nothing allowed (all -inf): ss_filtered_sample then draws -1.
+ *
+ *   logits, out        fp32 or bf16 (both the same) [n_seq] rows of `vocab` at row_stride / out_row_stride elements, any alignment of a row;
+ *                      out may be logits (same stride): only what a rule changes is then written.  Any other overlap is undefined
+ *   history_offsets    int64 [n_seq + 1], history int32: CSR of the tokens that a sequence has generated; NULL: none
+ *   prompt_offsets     int64 [n_prompts + 1], prompts int32: CSR of prompts;  prompt_of int32 [n_seq] or NULL: sequence s has prompt s
+ *   bias_offsets       int64 [n_biases + 1], bias_tokens int32, bias_values fp32: CSR of bias lists;  bias_of int32 [n_seq] or NULL: list s
+ *   masks              uint32 [n_masks] rows of ceil(vocab / 32) words at mask_stride words: bit v % 32 of word v / 32 is set where token v is
+ *                      allowed;  mask_of int32 [n_seq] or NULL: mask s
+ *   An entry of prompt_of, bias_of or mask_of outside [0, n_*) means none.  Tokens outside [0, vocab) are ignored.  Offsets ascend and
+ *   are trusted.  (prompts, history, bias_tokens and bias_values may be NULL where they hold nothing.)
+ *   repetition, frequency, presence   fp32 [n_seq] on the device, or NULL: the scalar of that name for every sequence
+ * vocab <= 2097152 (else SS_ERR_UNSUPPORTED).  No workspace, one launch.  n_seq = 0 or vocab = 0: nothing is launched.
+ * Errors: SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_CUDA.
+ * ======================================================================================================= */
+typedef struct ss_logit_rules {
+  uint32_t struct_size;              /* = sizeof(ss_logit_rules_t) */
+  uint32_t flags;                    /* 0 */
+  int32_t n_seq, vocab;
+  int32_t logits_type;               /* SS_LOGITS_* */
+  int32_t n_prompts, n_biases, n_masks;
+  float repetition_all, frequency_all, presence_all;
+  int32_t reserved;
+  int64_t row_stride, out_row_stride;  /* elements, >= vocab */
+  int64_t mask_stride;               /* words, >= ceil(vocab / 32) */
+  const void* logits;
+  void* out;
+  const int32_t* history;
+  const int64_t* history_offsets;
+  const int32_t* prompts;
+  const int64_t* prompt_offsets;
+  const int32_t* prompt_of;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const int32_t* bias_tokens;
+  const float* bias_values;
+  const int64_t* bias_offsets;
+  const int32_t* bias_of;
+  const uint32_t* masks;
+  const int32_t* mask_of;
+} ss_logit_rules_t;
+
+int32_t ss_logit_rules(const ss_logit_rules_t* rules /* host */, void* stream);
 
 /* =========================================================================================================
  * ss_build_prefix_tree - radix tree of candidate paths over whole KV pages, from raw token ids.

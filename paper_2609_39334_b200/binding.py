@@ -33,6 +33,7 @@ SS_MAX_DEPTH = 16
 SS_STEP_COMPACT_TRANSFERS = 0x1
 SS_ROWS_INTERLEAVED = 0x1
 SS_MAX_DRAFT = 128
+SS_MAX_AXES = 4
 SS_LOGITS_FP32, SS_LOGITS_BF16 = 0, 1
 SS_DEDUP_STATIC_MAX_PATHS = 65536
 
@@ -46,6 +47,8 @@ EXPORTS = [
     "ss_candidate_step_host_2", "ss_branch_sample_upto",
     "ss_qk_norm_rope", "ss_kv_append", "ss_draft_attention_workspace_bytes", "ss_draft_attention",
     "ss_filtered_sample_workspace_bytes", "ss_filtered_sample",
+    "ss_qk_norm_rope_axes", "ss_kv_append_axes", "ss_key_weights_workspace_bytes", "ss_key_weights",
+    "ss_kv_evict_workspace_bytes", "ss_kv_evict", "ss_logit_rules",
 ]
 PHASES = ["plan", "tiles", "leaves", "generic", "merge"]
 
@@ -95,6 +98,8 @@ _SIGNATURES = {
     "ss_profile_read": "pp", "ss_debug_umma_tile": "pppiiipp", "ss_debug_bounded_wait": "pp",
     "ss_qk_norm_rope": "pp", "ss_kv_append": "ppp", "ss_draft_attention_workspace_bytes": "pp", "ss_draft_attention": "pppzp",
     "ss_filtered_sample_workspace_bytes": "pp", "ss_filtered_sample": "ppzp",
+    "ss_qk_norm_rope_axes": "ppp", "ss_kv_append_axes": "pppp", "ss_key_weights_workspace_bytes": "ppp", "ss_key_weights": "pppzp",
+    "ss_kv_evict_workspace_bytes": "ppp", "ss_kv_evict": "pppzp", "ss_logit_rules": "pp",
 }
 
 
@@ -443,6 +448,51 @@ def ss_kv_append(desc: ss_attn_desc_t, rows: ss_rows_t, stream=None, check=True)
     return rc
 
 
+class ss_axes_t(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("num_axes", ctypes.c_int32), ("position_stride", ctypes.c_int64),
+        ("positions", ctypes.c_void_p), ("pair_axis", ctypes.c_void_p),
+    ]
+
+
+def make_axes(*, positions, pair_axis) -> ss_axes_t:
+    """Fills ss_axes_t for ss_qk_norm_rope_axes / ss_kv_append_axes.  positions: int32 [axes][rows] of any row stride; pair_axis: int32, the
+    axis of every rotated pair.  The returned object keeps references to the tensors."""
+    a = ss_axes_t()
+    a.struct_size = ctypes.sizeof(ss_axes_t)
+    assert positions.is_cuda and positions.dtype == torch.int32 and positions.dim() == 2 and (positions.stride(1) == 1 or positions.shape[1] <= 1)
+    assert pair_axis.dtype == torch.int32
+    a.num_axes = positions.shape[0]
+    a.position_stride = positions.stride(0) if positions.shape[0] > 1 else positions.shape[1]
+    a.positions, a.pair_axis = positions.data_ptr(), _ptr(pair_axis)
+    a._rows, a._pairs = positions.shape[1], pair_axis.numel()
+    a._keep = (positions, pair_axis)
+    return a
+
+
+def _check_axes(rows: ss_rows_t, axes: ss_axes_t):
+    # (made by make_axes: their tensors hold what the call reads)
+    assert not hasattr(axes, "_rows") or (axes._rows >= rows.n_rows and 2 * axes._pairs >= rows.rot_dim)
+
+
+def ss_qk_norm_rope_axes(rows: ss_rows_t, axes: ss_axes_t, stream=None, check=True) -> int:
+    """ss_qk_norm_rope where a token has a position on each of several axes, and every rotated pair goes by one of them."""
+    _check_axes(rows, axes)
+    rc = _call(rows._device, lib().ss_qk_norm_rope_axes, ctypes.byref(rows), ctypes.byref(axes), stream=stream)
+    if check:
+        _check(rc, "ss_qk_norm_rope_axes")
+    return rc
+
+
+def ss_kv_append_axes(desc: ss_attn_desc_t, rows: ss_rows_t, axes: ss_axes_t, stream=None, check=True) -> int:
+    """ss_kv_append where a token has a position on each of several axes, and every rotated pair goes by one of them."""
+    _check_axes(rows, axes)
+    rc = _call(rows._device, lib().ss_kv_append_axes, ctypes.byref(desc), ctypes.byref(rows), ctypes.byref(axes), stream=stream)
+    if check:
+        _check(rc, "ss_kv_append_axes")
+    return rc
+
+
 def ss_draft_attention_workspace_bytes(desc: ss_attn_desc_t) -> int:
     out = ctypes.c_size_t(0)
     _check(lib().ss_draft_attention_workspace_bytes(ctypes.byref(desc), ctypes.byref(out)), "ss_draft_attention_workspace_bytes")
@@ -458,6 +508,94 @@ def ss_draft_attention(desc: ss_attn_desc_t, draft_parent: Optional[torch.Tensor
                workspace.numel(), stream=stream)
     if check:
         _check(rc, "ss_draft_attention")
+    return rc
+
+
+# ---------------------------------------------------------------------------------------------------------
+class ss_key_weights_t(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("decay", ctypes.c_float), ("last_tokens", ctypes.c_int32),
+    ] + [(n, ctypes.c_void_p) for n in ("weights_in", "weights_out", "order", "path_order")]
+
+
+def _beside_pool(s, **arrays):
+    """Arrays with an element for every key of the pool, [pages][kv heads][16]: their addresses into s, the smallest one's size noted."""
+    for name, (t, dtype) in arrays.items():
+        assert t is None or (t.dtype == dtype and t.dim() == 3 and t.shape[2] == 16), name
+        setattr(s, name, _ptr(t))
+    there = [t for t, _ in arrays.values() if t is not None]
+    s._keys = min((t.numel() for t in there), default=0)
+
+
+def make_key_weights(*, weights_out, weights_in=None, decay=1.0, order=None, path_order=None, last_tokens=0) -> ss_key_weights_t:
+    """Fills ss_key_weights_t.  weights_in, weights_out: fp32 [pages][kv heads][16] (they may be one tensor), order: int32 of that shape,
+    path_order: int32 [paths].  The returned object keeps references to the tensors."""
+    s = ss_key_weights_t()
+    s.struct_size = ctypes.sizeof(ss_key_weights_t)
+    s.decay, s.last_tokens = float(decay), int(last_tokens)
+    _beside_pool(s, weights_in=(weights_in, torch.float32), weights_out=(weights_out, torch.float32), order=(order, torch.int32))
+    assert path_order is None or path_order.dtype == torch.int32
+    s.path_order = _ptr(path_order)
+    s._paths = path_order.numel() if path_order is not None else None
+    s._keep = (weights_out, weights_in, order, path_order)
+    return s
+
+
+def ss_key_weights_workspace_bytes(desc: ss_attn_desc_t, kw: ss_key_weights_t) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().ss_key_weights_workspace_bytes(ctypes.byref(desc), ctypes.byref(kw), ctypes.byref(out)), "ss_key_weights_workspace_bytes")
+    return int(out.value)
+
+
+def ss_key_weights(desc: ss_attn_desc_t, kw: ss_key_weights_t, workspace: torch.Tensor, stream=None, check=True) -> int:
+    """The attention weight that every cached key receives in the step that `desc` describes (its lse is what the attention wrote), added
+    to what it had."""
+    assert not hasattr(kw, "_keys") or (kw._keys >= desc.num_pages * desc.num_kv_heads * 16 and (kw._paths is None or kw._paths >= desc.num_paths))
+    rc = _call(workspace.device.index, lib().ss_key_weights, ctypes.byref(desc), ctypes.byref(kw), _ptr(workspace), workspace.numel(),
+               stream=stream)
+    if check:
+        _check(rc, "ss_key_weights")
+    return rc
+
+
+class ss_evict_t(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("n_nodes", ctypes.c_int32), ("max_keys", ctypes.c_int32),
+        ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+    ] + [(n, ctypes.c_void_p) for n in ("nodes", "keep", "weights", "weights_out", "order", "order_out", "source_out", "kv_len_out")]
+
+
+def make_evict(*, nodes, keep, weights, weights_out=None, order=None, order_out=None, source_out=None, kv_len_out=None, sinks=0, recent=0,
+               max_keys=0) -> ss_evict_t:
+    """Fills ss_evict_t.  nodes, keep: int32 [n]; weights, order and their outputs: [pages][kv heads][16], updated in place where no output is
+    given; kv_len_out: int32 [nodes of the tree].  The returned object keeps references to the tensors."""
+    s = ss_evict_t()
+    s.struct_size = ctypes.sizeof(ss_evict_t)
+    assert nodes.dtype == torch.int32 and keep.dtype == torch.int32 and nodes.numel() == keep.numel()
+    s.n_nodes, s.max_keys, s.sinks, s.recent = nodes.numel(), int(max_keys), int(sinks), int(recent)
+    s.nodes, s.keep = _ptr(nodes), _ptr(keep)
+    _beside_pool(s, weights=(weights, torch.float32), weights_out=(weights_out, torch.float32), order=(order, torch.int32),
+                 order_out=(order_out, torch.int32), source_out=(source_out, torch.int32))
+    assert kv_len_out is None or kv_len_out.dtype == torch.int32
+    s.kv_len_out = _ptr(kv_len_out)
+    s._nodes = kv_len_out.numel() if kv_len_out is not None else None
+    s._keep = (nodes, keep, weights, weights_out, order, order_out, source_out, kv_len_out)
+    return s
+
+
+def ss_kv_evict_workspace_bytes(desc: ss_attn_desc_t, ev: ss_evict_t) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().ss_kv_evict_workspace_bytes(ctypes.byref(desc), ctypes.byref(ev), ctypes.byref(out)), "ss_kv_evict_workspace_bytes")
+    return int(out.value)
+
+
+def ss_kv_evict(desc: ss_attn_desc_t, ev: ss_evict_t, workspace: torch.Tensor, stream=None, check=True) -> int:
+    """Keys of least weight leave the nodes; what stays moves into the nodes' first slots (see the header)."""
+    assert not hasattr(ev, "_keys") or (ev._keys >= desc.num_pages * desc.num_kv_heads * 16 and (ev._nodes is None or ev._nodes >= desc.num_nodes))
+    rc = _call(workspace.device.index, lib().ss_kv_evict, ctypes.byref(desc), ctypes.byref(ev), _ptr(workspace), workspace.numel(),
+               stream=stream)
+    if check:
+        _check(rc, "ss_kv_evict")
     return rc
 
 
@@ -555,6 +693,79 @@ def ss_filtered_sample(desc: ss_sample_desc_t, workspace: torch.Tensor, stream=N
     rc = _call(workspace.device.index, lib().ss_filtered_sample, ctypes.byref(desc), _ptr(workspace), workspace.numel(), stream=stream)
     if check:
         _check(rc, "ss_filtered_sample")
+    return rc
+
+
+class ss_logit_rules_t(ctypes.Structure):
+    _device = None                           # (of make_logit_rules' tensors)
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("n_seq", ctypes.c_int32), ("vocab", ctypes.c_int32),
+        ("logits_type", ctypes.c_int32), ("n_prompts", ctypes.c_int32), ("n_biases", ctypes.c_int32), ("n_masks", ctypes.c_int32),
+        ("repetition_all", ctypes.c_float), ("frequency_all", ctypes.c_float), ("presence_all", ctypes.c_float), ("reserved", ctypes.c_int32),
+        ("row_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64), ("mask_stride", ctypes.c_int64),
+    ] + [(n, ctypes.c_void_p) for n in ("logits", "out", "history", "history_offsets", "prompts", "prompt_offsets", "prompt_of", "repetition",
+                                        "frequency", "presence", "bias_tokens", "bias_values", "bias_offsets", "bias_of", "masks", "mask_of")]
+
+
+def make_logit_rules(*, logits, out=None, history=None, history_offsets=None, prompts=None, prompt_offsets=None, prompt_of=None,
+                     repetition=1.0, frequency=0.0, presence=0.0, bias_tokens=None, bias_values=None, bias_offsets=None, bias_of=None,
+                     masks=None, mask_of=None) -> ss_logit_rules_t:
+    """Fills ss_logit_rules_t.  logits: fp32 or bf16 [n_seq][vocab] of any row stride from vocab on, out: of that type and shape, or None: in
+    place; history, prompts, bias lists: CSR (int32 tokens, int64 offsets); masks: int32 [masks][words of 32 tokens]; repetition, frequency,
+    presence: a number for every sequence, or a device tensor with one each.  The returned object keeps references to the tensors."""
+    d = ss_logit_rules_t()
+    d.struct_size = ctypes.sizeof(ss_logit_rules_t)
+    out = logits if out is None else out
+    for t in (logits, out):
+        assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1)
+        assert t.dtype in (torch.float32, torch.bfloat16) and t.dtype == logits.dtype and t.shape == logits.shape
+    d.n_seq, d.vocab = logits.shape
+    d.logits_type = SS_LOGITS_BF16 if logits.dtype == torch.bfloat16 else SS_LOGITS_FP32
+    d.row_stride, d.out_row_stride = (t.stride(0) if d.n_seq > 1 else max(t.stride(0), d.vocab) for t in (logits, out))
+    if logits.data_ptr() == out.data_ptr():
+        d.out_row_stride = d.row_stride if d.n_seq <= 1 else d.out_row_stride
+    d.logits, d.out = logits.data_ptr(), out.data_ptr()
+    for values, offsets, of, count, offsets_name, names in (
+            ((history,), history_offsets, None, None, "history_offsets", ("history",)),
+            ((prompts,), prompt_offsets, prompt_of, "n_prompts", "prompt_offsets", ("prompts",)),
+            ((bias_tokens, bias_values), bias_offsets, bias_of, "n_biases", "bias_offsets", ("bias_tokens", "bias_values"))):
+        assert (offsets is None) == (values[0] is None), offsets_name
+        if offsets is None:
+            continue
+        assert offsets.dtype == torch.int64 and offsets.numel() >= 1, offsets_name
+        assert count is not None or offsets.numel() == d.n_seq + 1, offsets_name
+        for name, t, dtype in zip(names, values, (torch.int32, torch.float32)):
+            assert t.dtype == dtype, name
+            setattr(d, name, _ptr(t) if t.numel() else None)
+        setattr(d, offsets_name, _ptr(offsets))
+        if count is not None:
+            setattr(d, count, offsets.numel() - 1)
+    if bias_tokens is not None:
+        assert bias_values.numel() == bias_tokens.numel()
+    if masks is not None:
+        assert masks.is_cuda and masks.dtype == torch.int32 and masks.dim() == 2 and masks.stride(1) == 1 and 32 * masks.shape[1] >= d.vocab
+        d.masks, d.n_masks = masks.data_ptr(), masks.shape[0]
+        d.mask_stride = masks.stride(0) if masks.shape[0] > 1 else masks.shape[1]
+    for name, of in (("prompt_of", prompt_of), ("bias_of", bias_of), ("mask_of", mask_of)):
+        assert of is None or (of.dtype == torch.int32 and of.numel() >= d.n_seq), name
+        setattr(d, name, _ptr(of))
+    for name, value in (("repetition", repetition), ("frequency", frequency), ("presence", presence)):
+        if isinstance(value, (int, float)):
+            setattr(d, name + "_all", value)
+        else:
+            assert value.dtype == torch.float32 and value.numel() >= d.n_seq, name
+            setattr(d, name, _ptr(value))
+    d._device = logits.device.index
+    d._keep = (logits, out, history, history_offsets, prompts, prompt_offsets, prompt_of, repetition, frequency, presence, bias_tokens,
+               bias_values, bias_offsets, bias_of, masks, mask_of)
+    return d
+
+
+def ss_logit_rules(rules: ss_logit_rules_t, stream=None, check=True) -> int:
+    """Penalties of repeated tokens, biases and grammar masks on logits, in one pass (see the header)."""
+    rc = _call(rules._device, lib().ss_logit_rules, ctypes.byref(rules), stream=stream)
+    if check:
+        _check(rc, "ss_logit_rules")
     return rc
 
 

@@ -1,0 +1,521 @@
+// ss_kv_evict: the keys of least weight leave the nodes of the cache, what stays is brought together in a node's first slots.
+//
+// Per node of n keys and kv head: k = min(keep, n) keys stay, chosen by (must stay, weight, slot).  Kept keys in slots < k remain where
+// they are; the i-th kept key behind them goes into the i-th free slot < k.  So no slot is read that another move writes, at most
+// min(k, n - k) keys move, and a call may be repeated.
+//
+//   evict_nodes_kernel   checks the nodes, copies what the next kernel needs of them, writes the new lengths (which may be the tree's own)
+//   evict_kernel         a cluster of blocks per node and kv head, each with a stretch of slots: the border between what stays and what
+//                        goes by three histograms of 2048 bins over a range that shrinks (the first from the smallest to the largest
+//                        weight), ranks by counts, lists of free slots and of late keys in the workspace, and the moves, dealt out evenly
+#include <string.h>
+
+#include "common.cuh"
+
+namespace ss {
+namespace evict {
+
+constexpr int kDim = 128, kPage = 16;
+constexpr int kNodesThreads = 1024;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kBins = 2048, kBinBits = 11;
+constexpr int kPasses = 3;                     // 33 bits
+constexpr int kMostCluster = 8;
+constexpr int kStaged = 8192;                 // ranks of a block's slots that are kept in shared memory; behind them they are made again
+constexpr uint32_t kMust = 0xffffffffu;
+
+struct Header {
+  int32_t status;                              // first: read by ss_last_device_status
+  int32_t pad[63];
+};
+struct alignas(16) Node {
+  int64_t page0;                               // its first entry in node_pages
+  int n, k;                                    // keys, keys that stay; k < 0: not a node to work on
+};
+struct Params {
+  int Hkv;
+  __nv_bfloat16 *k_pool, *v_pool;
+  int64_t num_pages, page_stride, head_stride, total_node_pages;
+  int num_nodes;
+  const int32_t *node_kv_len, *node_pages;
+  const int64_t* node_page_offsets;
+  int n, sinks, recent;
+  const int32_t *nodes, *keep;
+  const float* weights;
+  float* weights_out;
+  const int32_t* order;
+  int32_t *order_out, *source_out, *kv_len_out;
+  // workspace
+  Header* hdr;
+  Node* info;
+  int32_t* claim;                              // per node of the tree: the smallest index at which it is listed
+  int32_t* lists;                              // per slot of node_pages and head: free slots and late keys
+};
+
+__global__ void __launch_bounds__(kNodesThreads) evict_nodes_kernel(const __grid_constant__ Params P) {
+  ss::grid_dependency_enter();
+  __shared__ int bad;
+  if (threadIdx.x == 0) bad = 0;
+  // (a node that is listed twice is taken once: its blocks would write the same lists)
+  auto for_each = [&](auto f) {
+    for (int i = threadIdx.x; i < P.n; i += kNodesThreads) {
+      const int node = P.nodes[i];
+      f(i, node, node >= 0 && node < P.num_nodes);
+    }
+    __syncthreads();
+  };
+  for_each([&](int, int node, bool there) { if (there) P.claim[node] = INT32_MAX; });
+  for_each([&](int i, int node, bool there) { if (there) atomicMin(P.claim + node, i); });
+  for_each([&](int i, int node, bool there) {
+    Node I = {0, 0, -1};
+    if (there && P.claim[node] == i) {
+      const int n = P.node_kv_len[node];
+      const int64_t e0 = P.node_page_offsets[node], e1 = P.node_page_offsets[node + 1];
+      if (n >= 0 && e0 >= 0 && e1 <= P.total_node_pages && (static_cast<int64_t>(n) + kPage - 1) / kPage <= e1 - e0)
+        I = {e0, n, min(max(P.keep[i], 0), n)};
+    }
+    if (I.k < 0) bad = 1;
+    P.info[i] = I;
+  });
+  for_each([&](int i, int node, bool) {        // (behind all reads of the lengths, which these may be)
+    if (P.kv_len_out && P.info[i].k >= 0) P.kv_len_out[node] = P.info[i].k;
+  });
+  if (threadIdx.x == 0) P.hdr->status = bad ? SS_ERR_BAD_INPUT : SS_OK;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+// Address of the same variable in block `rank` of the cluster.
+__device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ uint32_t load_remote(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_remote(uint32_t at, uint32_t v) { asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+
+// What a block tells the others of its cluster.
+struct Told {
+  uint32_t lowest, highest, must;              // ranks that go by weight, number of keys that must stay
+  int last;                                    // largest order
+  uint32_t holes, late;
+};
+struct Shared {
+  uint32_t total[kPasses][kBins];              // (of block 0 of the cluster: the sums over all)
+  uint32_t own[kBins];                         // this block's keys in the last pass
+  Told told;
+  uint32_t warp_sum[2][kWarps + 1];
+  uint32_t warp_lo[kWarps], warp_hi[kWarps];
+  int warp_last[kWarps];
+  uint32_t pick_bin, pick_left;
+  uint32_t kept[kStaged / 32];
+};
+
+struct Work {                                  // a node and head
+  const Params* P;
+  int64_t page0;
+  int n, g;
+  __device__ __forceinline__ int64_t page(int slot) const {
+    const int64_t p = __ldg(P->node_pages + page0 + slot / kPage);
+    return p >= 0 && p < P->num_pages ? p : -1;
+  }
+  __device__ __forceinline__ int64_t beside(int64_t page, int slot) const { return (page * P->Hkv + g) * kPage + slot % kPage; }
+  // (signed values in an order of unsigned ones; -0 is 0, NaN ranks last)
+  __device__ __forceinline__ uint32_t rank(int slot, int last) const {
+    const int64_t pg = page(slot);
+    if (pg < 0) return 0u;
+    const int64_t at = beside(pg, slot);
+    const int o = P->order ? P->order[at] : slot;
+    if (o < P->sinks || static_cast<int64_t>(o) > static_cast<int64_t>(last) - P->recent) return kMust;
+    const float w = P->weights[at] + 0.f;
+    if (w != w) return 0u;
+    const uint32_t u = __float_as_uint(w);
+    return u >> 31 ? ~u : u | 0x80000000u;
+  }
+};
+
+// Sum over the block's warps in front of this one; *total: over all.  (One of two buffers: the other may still be read.)
+__device__ __forceinline__ uint32_t block_before(uint32_t warp_count, Shared& S, int buffer, uint32_t* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0) S.warp_sum[buffer][warp] = warp_count;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const uint32_t c = S.warp_sum[buffer][w];
+    before += w < warp ? c : 0u;
+    all += c;
+  }
+  *total = all;
+  return before;
+}
+
+__global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__ Params P) {
+  ss::grid_dependency_enter();
+  extern __shared__ uint32_t staged[];         // ranks of the first kStaged slots of the block
+  __shared__ Shared S;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t r = cluster_rank(), C = cluster_size();
+  const int64_t pair = blockIdx.x / C;
+  const Node I = P.info[pair / P.Hkv];
+  Work W;
+  W.P = &P;
+  W.page0 = I.page0;
+  W.n = I.n;
+  W.g = static_cast<int>(pair % P.Hkv);
+  const int n = I.n, k = I.k;
+  const int stretch = (static_cast<int>((static_cast<int64_t>(n) + C - 1) / C) + 31) / 32 * 32;    // slots of a block
+  const int s0 = static_cast<int>(min(static_cast<int64_t>(stretch) * r, static_cast<int64_t>(n))), s1 = min(s0 + stretch, n);
+  if (k <= 0) return;                // (the whole cluster)
+  if (k == n) {                                // nothing moves
+    for (int i = s0 + tid; i < s1; i += kThreads) {
+      const int64_t pg = W.page(i);
+      if (pg < 0) { set_status(&P.hdr->status, SS_ERR_BAD_INPUT); continue; }
+      const int64_t at = W.beside(pg, i);
+      if (P.weights_out != P.weights) P.weights_out[at] = P.weights[at];
+      if (P.order_out && P.order_out != P.order) P.order_out[at] = P.order ? P.order[at] : i;
+      if (P.source_out) P.source_out[at] = i;
+    }
+    return;
+  }
+  for (int i = tid; i < kPasses * kBins; i += kThreads) (&S.total[0][0])[i] = 0;
+
+  // ---- the largest order of the node
+  int last = n - 1;
+  if (P.order && P.recent > 0) {
+    int mine = INT32_MIN;
+    for (int i = s0 + tid; i < s1; i += kThreads) {
+      const int64_t pg = W.page(i);
+      if (pg >= 0) mine = max(mine, P.order[W.beside(pg, i)]);
+    }
+    mine = __reduce_max_sync(0xffffffffu, mine);
+    if (lane == 0) S.warp_last[warp] = mine;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kWarps; ++w) mine = max(mine, S.warp_last[w]);
+      S.told.last = mine;
+    }
+    cluster_sync();
+    last = INT32_MIN;
+    for (uint32_t c = 0; c < C; ++c) last = max(last, static_cast<int>(load_remote(remote(&S.told.last, c))));
+  } else if (P.order) {
+    last = INT32_MAX;                          // (recent = 0: no order is larger)
+  }
+
+  // ---- ranks, their range, how many must stay
+  uint32_t lo = 0xffffffffu, hi = 0, must = 0;
+  for (int i = s0 + tid; i < s1; i += kThreads) {
+    const uint32_t u = W.rank(i, last);
+    if (i - s0 < kStaged) staged[i - s0] = u;
+    if (W.page(i) < 0) set_status(&P.hdr->status, SS_ERR_BAD_INPUT);
+    if (u == kMust) ++must;
+    else { lo = min(lo, u); hi = max(hi, u); }
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  must = __reduce_add_sync(0xffffffffu, must);
+  if (lane == 0) { S.warp_lo[warp] = lo; S.warp_hi[warp] = hi; }
+  uint32_t must_here;
+  (void)block_before(must, S, 0, &must_here);
+  if (tid == 0) {
+    for (int w = 0; w < kWarps; ++w) { lo = min(lo, S.warp_lo[w]); hi = max(hi, S.warp_hi[w]); }
+    S.told.lowest = lo;
+    S.told.highest = hi;
+    S.told.must = must_here;
+  }
+  cluster_sync();                              // (also: the sums are zero, everywhere)
+  uint32_t must_all = 0;
+  lo = 0xffffffffu;
+  hi = 0;
+  for (uint32_t c = 0; c < C; ++c) {
+    lo = min(lo, load_remote(remote(&S.told.lowest, c)));
+    hi = max(hi, load_remote(remote(&S.told.highest, c)));
+    must_all += load_remote(remote(&S.told.must, c));
+  }
+  auto rank_of = [&](int i) { return i - s0 < kStaged ? staged[i - s0] : W.rank(i, last); };
+
+  // ---- the border: `border` the smallest rank that stays, `ties` how many keys of that rank do
+  uint32_t border = kMust, ties = static_cast<uint32_t>(k), ties_before = 0;
+  if (must_all >= static_cast<uint32_t>(k)) {  // among those that must stay, by slot
+    for (uint32_t c = 0; c < r; ++c) ties_before += load_remote(remote(&S.told.must, c));
+  } else {
+    uint32_t left = static_cast<uint32_t>(k) - must_all;       // of those that go by weight, in [lo, hi]
+    for (int pass = 0; pass < kPasses; ++pass) {
+      const uint32_t range = hi - lo;
+      const int shift = range >= kBins ? 32 - __clz(range) - kBinBits : 0;       // (range >> shift) < kBins
+      for (int i = tid; i < kBins; i += kThreads) S.own[i] = 0;
+      __syncthreads();
+      for (int i = s0 + tid; i < s1; i += kThreads) {
+        const uint32_t u = rank_of(i);
+        if (u != kMust && u >= lo && u <= hi) atomicAdd(&S.own[(u - lo) >> shift], 1u);
+      }
+      __syncthreads();
+      for (int i = tid; i < kBins; i += kThreads)
+        if (S.own[i]) add_remote(remote(&S.total[pass][i], 0), S.own[i]);
+      cluster_sync();
+      // the bin in which the border lies: bins from the top, four a thread
+      uint32_t c[4], sum = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        c[x] = load_remote(remote(&S.total[pass][kBins - 1 - (4 * tid + x)], 0));
+        sum += c[x];
+      }
+      uint32_t incl = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      uint32_t unused;
+      uint32_t above = block_before(__shfl_sync(0xffffffffu, incl, 31), S, pass & 1, &unused) + incl - sum;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (above < left && left <= above + c[x]) {
+          S.pick_bin = static_cast<uint32_t>(kBins - 1 - (4 * tid + x));
+          S.pick_left = left - above;
+        }
+        above += c[x];
+      }
+      __syncthreads();
+      const uint32_t bin = S.pick_bin;
+      left = S.pick_left;
+      lo += bin << shift;
+      hi = shift ? min(hi, lo + ((1u << shift) - 1u)) : lo;
+      if (lo == hi) {                          // (all blocks at once) this block's keys of the border's rank are in own[bin]
+        if (tid == 0) S.told.must = S.own[bin];
+        break;
+      }
+      __syncthreads();
+    }
+    border = lo;
+    ties = left;
+    cluster_sync();
+    for (uint32_t c = 0; c < r; ++c) ties_before += load_remote(remote(&S.told.must, c));
+  }
+
+  // ---- who stays.  A warp has a stretch of rows of 32 slots; ties by slot.
+  const int rows = (s1 - s0 + 31) / 32, per = (rows + kWarps - 1) / kWarps;
+  const int row0 = min(warp * per, rows), row1 = min(row0 + per, rows);
+  uint32_t mine = 0;
+  for (int w = row0; w < row1; ++w) {
+    const int i = s0 + 32 * w + lane;
+    mine += __popc(__ballot_sync(0xffffffffu, i < s1 && rank_of(i) == border));
+  }
+  uint32_t unused;
+  __syncthreads();
+  uint32_t tie = ties_before + block_before(mine, S, 0, &unused);
+  // Bits of the row's kept keys (whole warp, rows in order).
+  auto kept_row = [&](int w) {
+    const int i = s0 + 32 * w + lane;
+    const uint32_t u = i < s1 ? rank_of(i) : 0u;
+    const uint32_t even = __ballot_sync(0xffffffffu, i < s1 && u == border);
+    const uint32_t number = tie + __popc(even & ((1u << lane) - 1u));
+    tie += __popc(even);
+    return __ballot_sync(0xffffffffu, i < s1 && (u > border || (u == border && number < ties)));
+  };
+  const uint32_t tie0 = tie;
+  uint32_t holes = 0, late = 0;
+  auto below = [&](int w) -> uint32_t {        // bits of the row's slots < k
+    const int d = k - (s0 + 32 * w);
+    return d >= 32 ? 0xffffffffu : d <= 0 ? 0u : (1u << d) - 1u;
+  };
+  for (int w = row0; w < row1; ++w) {
+    const uint32_t bits = kept_row(w), front = below(w);
+    if (w < kStaged / 32 && lane == 0) S.kept[w] = bits;
+    holes += __popc(~bits & front);
+    late += __popc(bits & ~front);
+  }
+  __syncwarp();
+  uint32_t holes_here, late_here;
+  uint32_t hole_at = block_before(holes, S, 1, &holes_here);
+  __syncthreads();
+  uint32_t late_at = block_before(late, S, 0, &late_here);
+  if (tid == 0) { S.told.holes = holes_here; S.told.late = late_here; }
+  cluster_sync();
+  uint32_t moves = 0;
+  for (uint32_t c = 0; c < C; ++c) {
+    const uint32_t h = load_remote(remote(&S.told.holes, c));
+    if (c < r) { hole_at += h; late_at += load_remote(remote(&S.told.late, c)); }
+    moves += h;
+  }
+  const int pages = (n + kPage - 1) / kPage;
+  int32_t* free_list = P.lists + (W.page0 * P.Hkv + static_cast<int64_t>(W.g) * pages) * kPage;
+  int32_t* late_list = free_list + pages * (kPage / 2);
+  const bool noted = row1 <= kStaged / 32;     // (a row's ties go by all the rows in front of it)
+  tie = tie0;
+  for (int w = row0; w < row1; ++w) {
+    const uint32_t bits = noted ? S.kept[w] : kept_row(w), front = below(w), me = 1u << lane;
+    const uint32_t hole = ~bits & front, behind = bits & ~front;
+    const int i = s0 + 32 * w + lane;
+    if (hole & me) free_list[hole_at + __popc(hole & (me - 1u))] = i;
+    if (behind & me) late_list[late_at + __popc(behind & (me - 1u))] = i;
+    hole_at += __popc(hole);
+    late_at += __popc(behind);
+    if (bits & front & me) {                   // remains
+      const int64_t pg = W.page(i);
+      if (pg >= 0) {
+        const int64_t at = W.beside(pg, i);
+        if (P.weights_out != P.weights) P.weights_out[at] = P.weights[at];
+        if (P.order_out && P.order_out != P.order) P.order_out[at] = P.order ? P.order[at] : i;
+        if (P.source_out) P.source_out[at] = i;
+      }
+    }
+  }
+  cluster_sync();
+
+  // ---- moves: a warp per key, K in the lower half's lanes, V in the upper's; kBatch keys on their way
+  constexpr int kBatch = 4;
+  const int moves_each = static_cast<int>((moves + C - 1) / C);
+  const int m0 = min(moves_each * static_cast<int>(r), static_cast<int>(moves)), m1 = min(m0 + moves_each, static_cast<int>(moves));
+  __nv_bfloat16* pool = (lane < 16 ? P.k_pool : P.v_pool) + static_cast<int64_t>(W.g) * P.head_stride + (lane & 15) * 8;
+  for (int j0 = m0 + warp * kBatch; j0 < m1; j0 += kWarps * kBatch) {
+    uint4 data[kBatch];
+    int64_t to[kBatch];
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      to[x] = -1;
+      if (j0 + x < m1) {
+        const int dst = free_list[j0 + x], src = late_list[j0 + x];
+        const int64_t dp = W.page(dst), sp = W.page(src);
+        if (dp >= 0 && sp >= 0) {
+          to[x] = dp * P.page_stride + (dst % kPage) * kDim;
+          data[x] = *reinterpret_cast<const uint4*>(pool + sp * P.page_stride + (src % kPage) * kDim);
+          if (lane == 0) {
+            const int64_t a = W.beside(dp, dst), b = W.beside(sp, src);
+            P.weights_out[a] = P.weights[b];
+            if (P.order_out) P.order_out[a] = P.order ? P.order[b] : src;
+            if (P.source_out) P.source_out[a] = src;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x)
+      if (to[x] >= 0) *reinterpret_cast<uint4*>(pool + to[x]) = data[x];
+  }
+}
+
+static int32_t check(const ss_attn_desc_t* d, const ss_evict_t* e) {
+  if (!d || d->struct_size != sizeof(ss_attn_desc_t) || !e || e->struct_size != sizeof(ss_evict_t) || e->flags) return SS_ERR_INVALID_ARG;
+  if (d->num_kv_heads < 1 || d->num_nodes < 0 || d->total_node_pages < 0 || d->num_pages < 0) return SS_ERR_INVALID_ARG;
+  if (e->n_nodes < 0 || e->max_keys < 0 || e->sinks < 0 || e->recent < 0) return SS_ERR_INVALID_ARG;
+  if (d->head_dim != kDim || d->page_size != kPage || d->kv_token_stride != kDim || d->kv_page_stride % 128 || d->kv_head_stride % 128 ||
+      d->kv_page_stride <= 0 || d->kv_head_stride <= 0)
+    return SS_ERR_UNSUPPORTED;
+  if (d->num_kv_heads > 65536 || d->total_node_pages > 0x7ffffff || static_cast<int64_t>(e->n_nodes) * d->num_kv_heads > 0x7fffffffLL / kMostCluster)
+    return SS_ERR_UNSUPPORTED;
+  return SS_OK;
+}
+
+static size_t carve(const ss_attn_desc_t* d, const ss_evict_t* e, void* base, Params* P) {
+  Carver c(base);
+  P->hdr = c.take<Header>(1);
+  P->info = c.take<Node>(static_cast<size_t>(e->n_nodes) + 1);
+  P->claim = c.take<int32_t>(static_cast<size_t>(d->num_nodes) + 1);
+  P->lists = c.take<int32_t>(static_cast<size_t>(d->total_node_pages) * d->num_kv_heads * kPage + 1);
+  return c.off;
+}
+
+// Blocks of a cluster: as many as it takes for two blocks an SM, as long as each has a thousand slots.
+static int cluster_of(const ss_attn_desc_t* d, const ss_evict_t* e) {
+  const int64_t pairs = static_cast<int64_t>(e->n_nodes) * d->num_kv_heads, all = d->total_node_pages * kPage;
+  const int64_t keys = e->max_keys > 0 && e->max_keys < all ? e->max_keys : all;
+  int c = 1;
+  while (c < kMostCluster && pairs * c < 2 * sm_count_of_current_device() && keys >= 2048 * c) c *= 2;
+  return c;
+}
+
+static int32_t launch_evict(const Params& P, const ss_attn_desc_t* d, const ss_evict_t* e, cudaStream_t st) {
+  constexpr int kSmem = kStaged * 4;
+  static bool done[kDeviceSlots] = {false};
+  const int slot = current_device_slot();
+  if (slot < 0 || !done[slot]) {
+    if (cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return SS_ERR_CUDA;
+    }
+    if (slot >= 0) done[slot] = true;
+  }
+  const int c = cluster_of(d, e);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(static_cast<int64_t>(e->n_nodes) * d->num_kv_heads * c));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(c);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ss::pdl_enabled() ? 2 : 1;
+  const cudaError_t err = cudaLaunchKernelEx(&cfg, evict_kernel, P);
+  ss::g_launch_count.fetch_add(1, std::memory_order_relaxed);
+  if (err != cudaSuccess || cudaPeekAtLastError() != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SS_ERR_CUDA;
+  }
+  return SS_OK;
+}
+
+}  // namespace evict
+}  // namespace ss
+
+extern "C" int32_t ss_kv_evict_workspace_bytes(const ss_attn_desc_t* desc, const ss_evict_t* ev, size_t* out_bytes) {
+  using namespace ss::evict;
+  if (!out_bytes) return SS_ERR_INVALID_ARG;
+  const int32_t rc = check(desc, ev);
+  if (rc != SS_OK) return rc;
+  Params P;
+  *out_bytes = carve(desc, ev, nullptr, &P);
+  return SS_OK;
+}
+
+extern "C" int32_t ss_kv_evict(const ss_attn_desc_t* d, const ss_evict_t* e, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace ss::evict;
+  const int32_t rc = check(d, e);
+  if (rc != SS_OK) return rc;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % ss::kAlign) return SS_ERR_INVALID_ARG;
+  Params P;
+  memset(&P, 0, sizeof P);
+  if (workspace_bytes < carve(d, e, workspace, &P)) return SS_ERR_WORKSPACE_TOO_SMALL;
+  if (e->n_nodes > 0 && (!e->nodes || !e->keep || !e->weights || !d->k_pool || !d->v_pool || !d->node_kv_len || !d->node_page_offsets ||
+                         !d->node_pages))
+    return SS_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(d->k_pool) % 256 || reinterpret_cast<uintptr_t>(d->v_pool) % 256) return SS_ERR_UNSUPPORTED;
+  P.Hkv = d->num_kv_heads;
+  P.k_pool = static_cast<__nv_bfloat16*>(const_cast<void*>(d->k_pool));
+  P.v_pool = static_cast<__nv_bfloat16*>(const_cast<void*>(d->v_pool));
+  P.num_pages = d->num_pages;
+  P.page_stride = d->kv_page_stride;
+  P.head_stride = d->kv_head_stride;
+  P.total_node_pages = d->total_node_pages;
+  P.num_nodes = d->num_nodes;
+  P.node_kv_len = d->node_kv_len;
+  P.node_pages = d->node_pages;
+  P.node_page_offsets = d->node_page_offsets;
+  P.n = e->n_nodes;
+  P.sinks = e->sinks;
+  P.recent = e->recent;
+  P.nodes = e->nodes;
+  P.keep = e->keep;
+  P.weights = e->weights;
+  P.weights_out = e->weights_out ? e->weights_out : e->weights;
+  P.order = e->order;
+  P.order_out = e->order_out ? e->order_out : e->order;
+  P.source_out = e->source_out;
+  P.kv_len_out = e->kv_len_out;
+  cudaStream_t st = ss::as_stream(stream);
+  SS_LAUNCH(evict_nodes_kernel, 1, kNodesThreads, 0, st, P);
+  if (e->n_nodes == 0) return SS_OK;
+  return launch_evict(P, d, e, st);
+}

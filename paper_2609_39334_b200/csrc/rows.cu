@@ -1,9 +1,10 @@
-// ss_qk_norm_rope and ss_kv_append: head rows of 128 values on their way from a projection into the attention - normalised
+// ss_qk_norm_rope, ss_kv_append and their forms with several axes: head rows of 128 values on their way from a projection into the attention - normalised
 // (keys and queries of models that do), rotated to their positions, rounded once, and written to where the attention reads
 // them: the caller's tensors or, keys and values of a step, the slots of the paged pool.
 //
 //   y = x * w / sqrt(mean(x^2) + eps)                        (w absent: y = x)
 //   (y_a, y_b) -> (y_a cos f - y_b sin f, y_b cos f + y_a sin f)   f = position * inv_freq[i], pairs (i, i + R/2) or (2i, 2i + 1)
+//   with axes: f = positions[axis of pair i] * inv_freq[i]
 //
 // Eight lanes share a head row: each has two chunks of 8 values (16 bytes) that hold both members of its 8 pairs, so that a
 // rotation needs no exchange, and a row's sum of squares takes three shuffles.  A warp has four rows at a time and goes through
@@ -36,7 +37,10 @@ struct Args {
   TensorOut q_out, k_out;
   const float* inv_freq;
   const __nv_bfloat16 *q_weight, *k_weight;
-  const int32_t* positions;
+  const int32_t* positions;                  // of one axis, or of `axes` axes behind each other
+  const int32_t* pair_axis;
+  int64_t position_stride;
+  int axes;                                  // 0: the forms without axes
   int64_t n_rows;
   float eps;
   int rot, hq, hk, hv;                       // heads to go through (0: tensor absent)
@@ -51,10 +55,13 @@ struct Place {                               // where the rows of a step go
   int num_nodes, num_paths;
 };
 // What is to be known of a token; lane t of a warp has that of the run's token t.
+struct OneAxis { double v; };
+struct Axes { int v[SS_MAX_AXES]; };
+template <typename Position>
 struct Token {
   int64_t row;                               // of the inputs (and q_out); -1: skipped
   int64_t kv;                                // where its keys and values go, relative to kd / vd (elements); -1: nowhere
-  double position;
+  Position position;
 };
 
 // Fused factors of a lane's 16 values: y = x A + x' B, x' the other member of the pair.  Not INTER: pairs (value j of chunk c0, of
@@ -117,14 +124,46 @@ __device__ __forceinline__ void load_weights(uint4 (&w)[32], const Args& A) {
   __syncthreads();
 }
 
+__device__ __forceinline__ OneAxis of_lane(const OneAxis& p, int t) { return {__shfl_sync(0xffffffffu, p.v, t)}; }
+__device__ __forceinline__ Axes of_lane(const Axes& p, int t) {
+  Axes r;
+#pragma unroll
+  for (int a = 0; a < SS_MAX_AXES; ++a) r.v[a] = __shfl_sync(0xffffffffu, p.v[a], t);
+  return r;
+}
+__device__ __forceinline__ double along(const OneAxis& p, int) { return p.v; }
+__device__ __forceinline__ double along(const Axes& p, int axis) {
+  int v = p.v[0];
+#pragma unroll
+  for (int a = 1; a < SS_MAX_AXES; ++a) v = axis == a ? p.v[a] : v;
+  return static_cast<double>(v);
+}
+__device__ __forceinline__ void load_position(OneAxis& p, const Args& A, int64_t row) { p.v = static_cast<double>(__ldg(A.positions + row)); }
+__device__ __forceinline__ void load_position(Axes& p, const Args& A, int64_t row) {
+#pragma unroll
+  for (int a = 0; a < SS_MAX_AXES; ++a) p.v[a] = a < A.axes ? __ldg(A.positions + a * A.position_stride + row) : 0;
+}
+__device__ __forceinline__ void set_position(OneAxis& p, int64_t position) { p.v = static_cast<double>(position); }
+__device__ __forceinline__ void set_position(Axes&, int64_t) {}
+// The axes of a lane's two pairs, in a byte each.
+__device__ __forceinline__ int lane_axes(const Args& A, int lane) {
+  int r = 0;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int i = lane + 32 * x;
+    if (A.axes && i < A.rot / 2) r |= min(max(__ldg(A.pair_axis + i), 0), A.axes - 1) << (8 * x);
+  }
+  return r;
+}
 // Sines and cosines of a token's angles (whole warp).
-__device__ __forceinline__ void token_angles(WarpShared& W, const Args& A, double position, int lane) {
+template <typename Position>
+__device__ __forceinline__ void token_angles(WarpShared& W, const Args& A, const Position& position, int axes, int lane) {
   __syncwarp();
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const int i = lane + 32 * x;
     if (i < A.rot / 2) {
-      double turns = position * static_cast<double>(__ldg(A.inv_freq + i)) * 0.15915494309189533577;   // / (2 pi)
+      double turns = along(position, (axes >> (8 * x)) & 0xff) * static_cast<double>(__ldg(A.inv_freq + i)) * 0.15915494309189533577;   // / (2 pi)
       turns -= rint(turns);
       sincospif(static_cast<float>(2.0 * turns), &W.sn[i], &W.cs[i]);
     }
@@ -213,9 +252,9 @@ __device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
 // The heads of the run's tokens that are this warp's: of every tensor those part, part + split, .. in units of four, a lane group
 // each.  Keys of head h go to kd + kv + h * d_head, values to vd + kv + h * d_head.  Copies run kStages - 1 head rows ahead of
 // their use, across tensors and tokens; a lane reads only what it copied itself, so no barrier is needed.
-template <bool INTER>
-__device__ __forceinline__ void run_heads(const Args& A, const uint4* weights, WarpShared& W, uint4* ring, const Token& mine, int n_tok,
-                                          int part, int lane, __nv_bfloat16* kd, __nv_bfloat16* vd, int64_t d_head) {
+template <bool INTER, typename Position>
+__device__ __forceinline__ void run_heads(const Args& A, const uint4* weights, WarpShared& W, uint4* ring, const Token<Position>& mine, int n_tok,
+                                          int part, int lane, int axes, __nv_bfloat16* kd, __nv_bfloat16* vd, int64_t d_head) {
   Lane L;
   lane_setup<INTER>(L, A, lane & 7);
   const int step = 4 * A.split, h0 = 4 * part + (lane >> 3);
@@ -277,9 +316,9 @@ __device__ __forceinline__ void run_heads(const Args& A, const uint4* weights, W
 #pragma unroll 1
   for (int t = 0; t < n_tok; ++t) {
     const int64_t row = __shfl_sync(0xffffffffu, mine.row, t), kv = __shfl_sync(0xffffffffu, mine.kv, t);
-    const double position = __shfl_sync(0xffffffffu, mine.position, t);
+    const Position position = of_lane(mine.position, t);
     if (row < 0) continue;                                                        // (warp-uniform)
-    if (q_rounds | k_rounds) token_angles(W, A, position, lane);
+    if (q_rounds | k_rounds) token_angles(W, A, position, axes, lane);
     if (q_rounds) {
       lane_factors<INTER>(L, W, weights);
       through(Yes(), A.q_out.p + row * A.q_out.row + h0 * A.q_out.head, step * A.q_out.head, A.hq, q_rounds, A.q_weight != nullptr);
@@ -293,7 +332,7 @@ __device__ __forceinline__ void run_heads(const Args& A, const uint4* weights, W
   }
 }
 
-template <bool INTER>
+template <bool INTER, typename Position>
 __global__ void __launch_bounds__(kWarps * 32, kBlocks) norm_rope_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
   extern __shared__ uint4 ring[];
@@ -304,13 +343,14 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) norm_rope_kernel(const _
   const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + warp, r0 = w / A.split * A.run;
   const int n_tok = static_cast<int>(min(static_cast<int64_t>(A.run), A.n_rows - r0));
   if (n_tok <= 0) return;
-  Token mine{-1, 0, 0.0};
+  Token<Position> mine{-1, 0, {}};
+  const int axes = lane_axes(A, lane);
   if (lane < n_tok) {
     mine.row = r0 + lane;
     mine.kv = mine.row * A.k_out.row;
-    if (A.positions) mine.position = static_cast<double>(__ldg(A.positions + mine.row));
+    if (A.positions) load_position(mine.position, A, mine.row);
   }
-  run_heads<INTER>(A, weights, W[warp], ring + warp * (kStages * 64), mine, n_tok, static_cast<int>(w % A.split), lane, A.k_out.p, nullptr, A.k_out.head);
+  run_heads<INTER>(A, weights, W[warp], ring + warp * (kStages * 64), mine, n_tok, static_cast<int>(w % A.split), lane, axes, A.k_out.p, nullptr, A.k_out.head);
 }
 
 // Number of offsets[0 .. n] that are <= r, less one: the path of row r (whole warp; 32 probes a round).
@@ -326,7 +366,7 @@ __device__ __forceinline__ int path_of(const int64_t* offsets, int n, int64_t r,
   return lo;
 }
 
-template <bool INTER>
+template <bool INTER, typename Position>
 __global__ void __launch_bounds__(kWarps * 32, kBlocks) append_kernel(const __grid_constant__ Args A, const __grid_constant__ Place P) {
   ss::grid_dependency_enter();
   extern __shared__ uint4 ring[];
@@ -343,7 +383,8 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) append_kernel(const __gr
   if (n_tok <= 0) return;
   // the first token's path by the whole warp, the others' from there on
   int p = path_of(P.q_offsets, live, first + r0, lane);
-  Token mine{-1, -1, 0.0};
+  Token<Position> mine{-1, -1, {}};
+  const int axes = lane_axes(A, lane);
   if (lane < n_tok) {
     const int64_t r = first + r0 + lane;
     while (p + 1 < live && __ldg(P.q_offsets + p + 1) <= r) ++p;
@@ -359,21 +400,21 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) append_kernel(const __gr
           if (page >= 0 && page < P.num_pages) mine.kv = page * P.page_stride + static_cast<int64_t>(at % kPage) * kDim;
         }
       }
-      int64_t position = at;
       if (A.positions) {
-        position = __ldg(A.positions + row);
-      } else if (A.rot) {
+        load_position(mine.position, A, row);
+      } else if (A.rot) {                                      // (one axis: with several there are positions)
+        int64_t position = at;
         int a = __ldg(P.node_parent + leaf);
         for (int d = 1; d < SS_MAX_DEPTH && a >= 0 && a < P.num_nodes; ++d) {
           position += __ldg(P.node_kv_len + a);
           a = __ldg(P.node_parent + a);
         }
+        set_position(mine.position, position);
       }
-      mine.position = static_cast<double>(position);
     }
   }
   __syncwarp();
-  run_heads<INTER>(A, weights, W[warp], ring + warp * (kStages * 64), mine, n_tok, static_cast<int>(w % A.split), lane, P.k_pool, P.v_pool, P.head_stride);
+  run_heads<INTER>(A, weights, W[warp], ring + warp * (kStages * 64), mine, n_tok, static_cast<int>(w % A.split), lane, axes, P.k_pool, P.v_pool, P.head_stride);
 }
 
 // Checks what both calls share and fills the kernel's arguments.
@@ -434,20 +475,20 @@ static int32_t prepare(Kernel kernel, bool (&done)[kDeviceSlots]) {
   if (slot >= 0) done[slot] = true;
   return SS_OK;
 }
-template <bool INTER>
+template <bool INTER, typename Position>
 static int32_t launch_norm_rope(const Args& A, unsigned grid, cudaStream_t st) {
   static bool done[kDeviceSlots] = {false};
-  const int32_t rc = prepare(norm_rope_kernel<INTER>, done);
+  const int32_t rc = prepare(norm_rope_kernel<INTER, Position>, done);
   if (rc != SS_OK) return rc;
-  SS_LAUNCH(norm_rope_kernel<INTER>, grid, kWarps * 32, kSmem, st, A);
+  SS_LAUNCH((norm_rope_kernel<INTER, Position>), grid, kWarps * 32, kSmem, st, A);
   return SS_OK;
 }
-template <bool INTER>
+template <bool INTER, typename Position>
 static int32_t launch_append(const Args& A, const Place& P, unsigned grid, cudaStream_t st) {
   static bool done[kDeviceSlots] = {false};
-  const int32_t rc = prepare(append_kernel<INTER>, done);
+  const int32_t rc = prepare(append_kernel<INTER, Position>, done);
   if (rc != SS_OK) return rc;
-  SS_LAUNCH(append_kernel<INTER>, grid, kWarps * 32, kSmem, st, A, P);
+  SS_LAUNCH((append_kernel<INTER, Position>), grid, kWarps * 32, kSmem, st, A, P);
   return SS_OK;
 }
 static int32_t grid_of(int64_t tokens, const Args& A, unsigned* grid) {
@@ -457,28 +498,41 @@ static int32_t grid_of(int64_t tokens, const Args& A, unsigned* grid) {
   return SS_OK;
 }
 
-}  // namespace rows
-}  // namespace ss
+// The axes of a call that has them.
+static int32_t axes_args(const ss_rows_t* r, const ss_axes_t* x, Args* A) {
+  if (!x || x->struct_size != sizeof(ss_axes_t) || x->position_stride < 0 || r->positions) return SS_ERR_INVALID_ARG;
+  if (x->num_axes < 1) return SS_ERR_INVALID_ARG;
+  if (x->num_axes > SS_MAX_AXES) return SS_ERR_UNSUPPORTED;
+  if (x->num_axes > 1 && x->position_stride && x->position_stride < r->n_rows) return SS_ERR_INVALID_ARG;
+  if (r->n_rows == 0 || r->rot_dim == 0) return SS_OK;
+  if (!x->positions || !x->pair_axis) return SS_ERR_INVALID_ARG;
+  A->positions = x->positions;
+  A->pair_axis = x->pair_axis;
+  A->position_stride = x->position_stride;
+  A->axes = x->num_axes;
+  return SS_OK;
+}
 
-extern "C" int32_t ss_qk_norm_rope(const ss_rows_t* rows, void* stream) {
-  using namespace ss::rows;
+static int32_t norm_rope(const ss_rows_t* rows, const ss_axes_t* axes, bool with_axes, void* stream) {
   Args A = {};
-  const int32_t rc = rows_args(rows, &A);
+  int32_t rc = rows_args(rows, &A);
+  if (rc == SS_OK && with_axes) rc = axes_args(rows, axes, &A);
   if (rc != SS_OK || rows->n_rows == 0) return rc;
-  if ((!rows->q && !rows->k) || (rows->k != nullptr) != (rows->k_out != nullptr) || (rows->rot_dim && !rows->positions)) return SS_ERR_INVALID_ARG;
+  if ((!rows->q && !rows->k) || (rows->k != nullptr) != (rows->k_out != nullptr) || (rows->rot_dim && !A.positions)) return SS_ERR_INVALID_ARG;
   A.split = heads_split(rows->n_rows, A.hq + A.hk);
   A.run = run_of(rows->n_rows, A.split);
   unsigned grid = 0;
   const int32_t gc = grid_of(rows->n_rows, A, &grid);
   if (gc != SS_OK) return gc;
-  return rows->flags & SS_ROWS_INTERLEAVED ? launch_norm_rope<true>(A, grid, ss::as_stream(stream))
-                                           : launch_norm_rope<false>(A, grid, ss::as_stream(stream));
+  cudaStream_t st = ss::as_stream(stream);
+  if (rows->flags & SS_ROWS_INTERLEAVED) return A.axes ? launch_norm_rope<true, Axes>(A, grid, st) : launch_norm_rope<true, OneAxis>(A, grid, st);
+  return A.axes ? launch_norm_rope<false, Axes>(A, grid, st) : launch_norm_rope<false, OneAxis>(A, grid, st);
 }
 
-extern "C" int32_t ss_kv_append(const ss_attn_desc_t* d, const ss_rows_t* rows, void* stream) {
-  using namespace ss::rows;
+static int32_t append(const ss_attn_desc_t* d, const ss_rows_t* rows, const ss_axes_t* axes, bool with_axes, void* stream) {
   Args A = {};
-  const int32_t rc = rows_args(rows, &A);
+  int32_t rc = rows_args(rows, &A);
+  if (rc == SS_OK && with_axes) rc = axes_args(rows, axes, &A);
   if (rc != SS_OK) return rc;
   if (!d || d->struct_size != sizeof(ss_attn_desc_t)) return SS_ERR_INVALID_ARG;
   if (d->num_nodes < 0 || d->num_paths < 0 || d->total_q < 0 || d->total_node_pages < 0 || d->num_pages < 0) return SS_ERR_INVALID_ARG;
@@ -518,6 +572,21 @@ extern "C" int32_t ss_kv_append(const ss_attn_desc_t* d, const ss_rows_t* rows, 
   unsigned grid = 0;
   const int32_t gc = grid_of(d->total_q, A, &grid);
   if (gc != SS_OK) return gc;
-  return rows->flags & SS_ROWS_INTERLEAVED ? launch_append<true>(A, P, grid, ss::as_stream(stream))
-                                           : launch_append<false>(A, P, grid, ss::as_stream(stream));
+  cudaStream_t st = ss::as_stream(stream);
+  if (rows->flags & SS_ROWS_INTERLEAVED) return A.axes ? launch_append<true, Axes>(A, P, grid, st) : launch_append<true, OneAxis>(A, P, grid, st);
+  return A.axes ? launch_append<false, Axes>(A, P, grid, st) : launch_append<false, OneAxis>(A, P, grid, st);
+}
+
+}  // namespace rows
+}  // namespace ss
+
+extern "C" int32_t ss_qk_norm_rope(const ss_rows_t* rows, void* stream) { return ss::rows::norm_rope(rows, nullptr, false, stream); }
+extern "C" int32_t ss_qk_norm_rope_axes(const ss_rows_t* rows, const ss_axes_t* axes, void* stream) {
+  return ss::rows::norm_rope(rows, axes, true, stream);
+}
+extern "C" int32_t ss_kv_append(const ss_attn_desc_t* desc, const ss_rows_t* rows, void* stream) {
+  return ss::rows::append(desc, rows, nullptr, false, stream);
+}
+extern "C" int32_t ss_kv_append_axes(const ss_attn_desc_t* desc, const ss_rows_t* rows, const ss_axes_t* axes, void* stream) {
+  return ss::rows::append(desc, rows, axes, true, stream);
 }
