@@ -28,37 +28,43 @@ __device__ __forceinline__ long long load_remote(const long long* p, uint32_t ra
   asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
   return v;
 }
-// Sum over the cluster's threads in front of this one (and of all in *total).  A barrier over the cluster.
-__device__ __forceinline__ long long cluster_before(long long mine, long long (&warp_sum)[kPlanWarps], long long& block_sum, long long* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long incl = mine;
+// Sums over the cluster's threads in front of this one (and of all in *total_a, *total_b).  A barrier over the cluster.
+struct Scan { long long warp_a[kPlanWarps], warp_b[kPlanWarps], block_a, block_b; };
+__device__ __forceinline__ long long scanned(long long v, int lane) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long up = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += up;
+    const long long up = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += up;
   }
-  if (lane == 31) warp_sum[warp] = incl;
+  return v;
+}
+__device__ __forceinline__ void cluster_before(long long& a, long long& b, Scan& S, long long* total_a, long long* total_b) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long ia = scanned(a, lane), ib = scanned(b, lane);
+  if (lane == 31) { S.warp_a[warp] = ia; S.warp_b[warp] = ib; }
   __syncthreads();
-  long long before = 0, all = 0;
-  for (int w = 0; w < kPlanWarps; ++w) {
-    if (w < warp) before += warp_sum[w];
-    all += warp_sum[w];
+  if (warp == 0) {
+    const long long wa = S.warp_a[lane], wb = S.warp_b[lane], ja = scanned(wa, lane), jb = scanned(wb, lane);
+    S.warp_a[lane] = ja - wa;
+    S.warp_b[lane] = jb - wb;
+    if (lane == 31) { S.block_a = ja; S.block_b = jb; }
   }
-  if (threadIdx.x == 0) block_sum = all;
   cluster_sync();
   const uint32_t r = cluster_rank(), C = cluster_size();
-  *total = 0;
+  a = S.warp_a[warp] + ia - a;
+  b = S.warp_b[warp] + ib - b;
+  *total_a = *total_b = 0;
   for (uint32_t c = 0; c < C; ++c) {
-    const long long s = load_remote(&block_sum, c);
-    if (c < r) before += s;
-    *total += s;
+    const long long sa = load_remote(&S.block_a, c), sb = load_remote(&S.block_b, c);
+    if (c < r) { a += sa; b += sb; }
+    *total_a += sa;
+    *total_b += sb;
   }
-  return before + incl - mine;
 }
 
 __global__ void __launch_bounds__(kPlanThreads, 1) key_plan_kernel(const __grid_constant__ Params P, int grid_blocks) {
-  ss::grid_dependency_enter();
-  __shared__ long long warp_sum[kPlanWarps], block_sum[3];
+  ss::grid_dependency_enter_then_release();
+  __shared__ Scan scan[2];
   const uint32_t C = cluster_size();
   const int tid = static_cast<int>(cluster_rank()) * kPlanThreads + threadIdx.x, threads = static_cast<int>(C) * kPlanThreads;
   const int lane = threadIdx.x & 31;
@@ -67,7 +73,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) key_plan_kernel(const __grid_
     P.last[i] = -1;
     P.below[i] = P.fresh[i] = 0;
   }
-  for (int i = tid; i < grid_blocks; i += threads) P.arrived[i] = 0;
+  for (int i = tid; i < 2 * grid_blocks; i += threads) P.arrived[i] = 0;
   if (tid == 0) P.hdr->status = SS_OK;
   cluster_sync();
 
@@ -103,8 +109,8 @@ __global__ void __launch_bounds__(kPlanThreads, 1) key_plan_kernel(const __grid_
     P.path_row[p] = used_of(T);                                // (its place follows)
     used += used_of(T);
   }
-  long long all;
-  long long at = cluster_before(used, warp_sum, block_sum[0], &all);
+  long long all, unused, none = 0, at = used;
+  cluster_before(at, none, scan[0], &all, &unused);
   for (int p = p0; p < p1; ++p) {
     const int u = P.path_row[p];
     // (rows of different paths that overlap would not fit the table)
@@ -147,12 +153,13 @@ __global__ void __launch_bounds__(kPlanThreads, 1) key_plan_kernel(const __grid_
     R.len = len;
     R.row0 = P.path_row[first];
     R.rows = P.path_row[last + 1] - R.row0;
-    R.steps = max(1, static_cast<int>((static_cast<int64_t>(R.rows) * P.G + kCols - 1) / kCols));
+    R.steps = max(1, (R.rows + kCols / P.G - 1) / (kCols / P.G));
     R.known = len - fresh;
     R.hides = fresh > 0 && first == last ? R.rows : 0;
     R.order0 = fresh > 0 ? P.path_start[P.leaf_path[n]] : 0;
-    R.pad = 0;
-    return static_cast<long long>((len + kTile - 1) / kTile) * P.Hkv * R.steps;
+    const int per_step = kCols / P.G, last_rows = (R.rows - (R.steps - 1) * per_step) * P.G;
+    R.cost = kTileCost + (R.steps - 1) * ((per_step * P.G + 15) / 16) + max(1, (last_rows + 15) / 16);
+    return static_cast<long long>((len + kTile - 1) / kTile) * P.Hkv * R.cost;
   };
   Rec R;
   long long cost = 0, count = 0;
@@ -160,10 +167,8 @@ __global__ void __launch_bounds__(kPlanThreads, 1) key_plan_kernel(const __grid_
     cost += rec_of(n, R, true);
     count += R.len > 0;
   }
-  long long total, n_recs;
-  long long off = cluster_before(cost, warp_sum, block_sum[1], &total);
-  __syncthreads();
-  long long rec = cluster_before(count, warp_sum, block_sum[2], &n_recs);
+  long long total, n_recs, off = cost, rec = count;
+  cluster_before(off, rec, scan[1], &total, &n_recs);
   for (int n = n0; n < n1; ++n) {
     const long long c = rec_of(n, R, false);
     if (R.len == 0) continue;
@@ -246,8 +251,8 @@ static size_t carve(const ss_attn_desc_t* d, void* base, Params* P) {
   P->leaf_path = c.take<int>(nodes);
   P->path_row = c.take<int>(paths);
   P->path_start = c.take<int>(paths);
-  P->part = c.take<float>(blocks * 2 * kTile);
-  P->arrived = c.take<int>(blocks);
+  P->part = c.take<float>(blocks * 2 * 2 * kTile);
+  P->arrived = c.take<int>(blocks * 2);
   return c.off;
 }
 

@@ -8,17 +8,19 @@ namespace keyw {
 constexpr int kDim = 128, kPage = 16;
 constexpr int kTile = 128;                   // keys of a unit: 8 pages
 constexpr int kTilePages = kTile / kPage;
-constexpr int kCols = 128;                   // query rows (tokens x heads of a group) of a step
+constexpr int kCols = 128;                   // query rows (tokens x heads of a group) of a step, at most
+constexpr int kTileCost = 8;                 // (of keys and what a unit takes besides, in 16 query rows)
+constexpr int kLeastQuota = 2 * (kTileCost + kCols / 16);     // a block's share: at least a step of two tiles, wherever it starts
 
 struct Header {
   int32_t status;                            // first: read by ss_last_device_status
   int32_t n_recs;
-  int64_t total;                             // steps of all units
+  int64_t total;                             // cost of all units
   int32_t pad[60];
 };
-// A node with something to do.  Its units are (tile of keys, kv head), head by head; each has `steps` steps of kCols query rows.
+// A node with something to do.  Its units are (pair of tiles of keys, kv head), head by head; each has `steps` steps of kCols / G tokens.
 struct alignas(16) Rec {
-  int64_t off;                               // steps in front of it
+  int64_t off;                               // cost of what is in front of it
   int64_t page0;                             // its first entry in node_pages
   int len;                                   // keys
   int row0, rows;                            // tokens that add to them, in the table of rows
@@ -26,7 +28,7 @@ struct alignas(16) Rec {
   int known;                                 // keys in front of the step's own
   int hides;                                 // token x of the rows sees keys < len - hides + x + 1 only (0: all are seen)
   int order0;                                // sequence number of key `known`
-  int pad;
+  int cost;                                  // of a tile: kTileCost, and 1 for 16 query rows
 };
 
 struct Params {
@@ -54,8 +56,8 @@ struct Params {
   int2* rows;                                // of a token: row of q, row of lse
   int *first, *last, *below, *fresh, *leaf_path;     // by node: paths below it, their number, longest step that it is the leaf of, whose
   int *path_row, *path_start;                // by path: its first token in the table, sequence number of its step's first token
-  float* part;                               // 2 per block of the grid: sums of a unit's tile by key
-  int* arrived;                              // by block of the grid: how many have left their part of the unit that starts there and goes on
+  float* part;                               // [2 per block of the grid][2 tiles][kTile]: a block's sums of a unit that it shares
+  int* arrived;                              // [block of the grid][tile]: how many have left theirs of the unit that starts there and goes on
 };
 
 #ifdef __CUDACC__
