@@ -4,10 +4,11 @@
 // they are; the i-th kept key behind them goes into the i-th free slot < k.  So no slot is read that another move writes, at most
 // min(k, n - k) keys move, and a call may be repeated.
 //
-//   evict_nodes_kernel   checks the nodes, copies what the next kernel needs of them, writes the new lengths (which may be the tree's own)
-//   evict_kernel         a cluster of blocks per node and kv head, each with a stretch of slots: the border between what stays and what
-//                        goes by three histograms of 2048 bins over a range that shrinks (the first from the smallest to the largest
-//                        weight), ranks by counts, lists of free slots and of late keys in the workspace, and the moves, dealt out evenly
+//   evict_nodes_kernel   checks the nodes, copies what the others need of them, writes the new lengths (which may be the tree's own)
+//   evict_select_kernel  a cluster of blocks per node and kv head, each with a stretch of slots: the border between what stays and what goes
+//                        by at most three histograms of 2048 bins over a range that shrinks (the first from the smallest to the largest
+//                        weight; done when a bin stays as a whole), then ranks by counts, and lists of free slots and of late keys
+//   evict_move_kernel    blocks for every node and head: the moves
 #include <string.h>
 
 #include "common.cuh"
@@ -20,9 +21,13 @@ constexpr int kNodesThreads = 1024;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kBinBits = 11;
 constexpr int kPasses = 3;                     // 33 bits
+static_assert(kBins == 4 * kThreads, "four bins a thread");
 constexpr int kMostCluster = 8;
-constexpr int kStaged = 8192;                 // ranks of a block's slots that are kept in shared memory; behind them they are made again
+constexpr int kStaged = 16384;                 // ranks of a block's slots that are kept in shared memory, at most; behind them they are made again
+constexpr int kAhead = 4;                      // quads of slots that a thread has on their way
+constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32, kBatch = 4;
 constexpr uint32_t kMust = 0xffffffffu;
+constexpr uint32_t kAllTies = 0xffffffffu;
 
 struct Header {
   int32_t status;                              // first: read by ss_last_device_status
@@ -40,6 +45,8 @@ struct Params {
   const int32_t *node_kv_len, *node_pages;
   const int64_t* node_page_offsets;
   int n, sinks, recent;
+  int staged;                                  // room for so many ranks in a block's shared memory
+  int move_blocks;                             // of a node and head
   const int32_t *nodes, *keep;
   const float* weights;
   float* weights_out;
@@ -49,6 +56,7 @@ struct Params {
   Header* hdr;
   Node* info;
   int32_t* claim;                              // per node of the tree: the smallest index at which it is listed
+  int32_t* moves;                              // per node and head: how many
   int32_t* lists;                              // per slot of node_pages and head: free slots and late keys
 };
 
@@ -57,9 +65,10 @@ __global__ void __launch_bounds__(kNodesThreads) evict_nodes_kernel(const __grid
   __shared__ int bad;
   if (threadIdx.x == 0) bad = 0;
   // (a node that is listed twice is taken once: its blocks would write the same lists)
+  const int mine = static_cast<int>(threadIdx.x) < P.n ? P.nodes[threadIdx.x] : -1;
   auto for_each = [&](auto f) {
     for (int i = threadIdx.x; i < P.n; i += kNodesThreads) {
-      const int node = P.nodes[i];
+      const int node = i < kNodesThreads ? mine : P.nodes[i];
       f(i, node, node >= 0 && node < P.num_nodes);
     }
     __syncthreads();
@@ -100,7 +109,6 @@ __device__ __forceinline__ uint32_t load_remote(uint32_t at) {
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ void add_remote(uint32_t at, uint32_t v) { asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
 
 // What a block tells the others of its cluster.
 struct Told {
@@ -109,13 +117,12 @@ struct Told {
   uint32_t holes, late;
 };
 struct Shared {
-  uint32_t total[kPasses][kBins];              // (of block 0 of the cluster: the sums over all)
-  uint32_t own[kBins];                         // this block's keys in the last pass
+  uint32_t own[2][kBins];                      // this block's keys by bin, in passes in turn
   Told told;
   uint32_t warp_sum[2][kWarps + 1];
   uint32_t warp_lo[kWarps], warp_hi[kWarps];
   int warp_last[kWarps];
-  uint32_t pick_bin, pick_left;
+  uint32_t pick_bin, pick_left, pick_whole;
   uint32_t kept[kStaged / 32];
 };
 
@@ -129,18 +136,32 @@ struct Work {                                  // a node and head
   }
   __device__ __forceinline__ int64_t beside(int64_t page, int slot) const { return (page * P->Hkv + g) * kPage + slot % kPage; }
   // (signed values in an order of unsigned ones; -0 is 0, NaN ranks last)
-  __device__ __forceinline__ uint32_t rank(int slot, int last) const {
-    const int64_t pg = page(slot);
-    if (pg < 0) return 0u;
-    const int64_t at = beside(pg, slot);
-    const int o = P->order ? P->order[at] : slot;
+  __device__ __forceinline__ uint32_t rank_of(float weight, int o, int last) const {
     if (o < P->sinks || static_cast<int64_t>(o) > static_cast<int64_t>(last) - P->recent) return kMust;
-    const float w = P->weights[at] + 0.f;
+    const float w = weight + 0.f;
     if (w != w) return 0u;
     const uint32_t u = __float_as_uint(w);
     return u >> 31 ? ~u : u | 0x80000000u;
   }
+  __device__ __forceinline__ uint32_t rank(int slot, int last) const {
+    const int64_t pg = page(slot);
+    if (pg < 0) return 0u;
+    const int64_t at = beside(pg, slot);
+    return rank_of(P->weights[at], P->order ? P->order[at] : slot, last);
+  }
 };
+
+// f(first slot of the first of kAhead quads, 4 * kThreads apart and so at the same place of their pages; their pages, -1: bad, -2: behind the end)
+// for all quads of [s0, s1) (whole block; s0 a multiple of 32).
+template <typename F>
+__device__ __forceinline__ void for_quads(const Work& W, int s0, int s1, F f) {
+  for (int i0 = s0 + 4 * static_cast<int>(threadIdx.x); i0 < s1; i0 += 4 * kThreads * kAhead) {
+    int64_t page[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) page[x] = i0 + x * 4 * kThreads < s1 ? W.page(i0 + x * 4 * kThreads) : -2;
+    f(i0, page);
+  }
+}
 
 // Sum over the block's warps in front of this one; *total: over all.  (One of two buffers: the other may still be read.)
 __device__ __forceinline__ uint32_t block_before(uint32_t warp_count, Shared& S, int buffer, uint32_t* total) {
@@ -158,9 +179,9 @@ __device__ __forceinline__ uint32_t block_before(uint32_t warp_count, Shared& S,
   return before;
 }
 
-__global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__ Params P) {
+__global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_constant__ Params P) {
   ss::grid_dependency_enter();
-  extern __shared__ uint32_t staged[];         // ranks of the first kStaged slots of the block
+  extern __shared__ uint32_t staged[];         // ranks of the block's first slots
   __shared__ Shared S;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t r = cluster_rank(), C = cluster_size();
@@ -174,9 +195,9 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
   const int n = I.n, k = I.k;
   const int stretch = (static_cast<int>((static_cast<int64_t>(n) + C - 1) / C) + 31) / 32 * 32;    // slots of a block
   const int s0 = static_cast<int>(min(static_cast<int64_t>(stretch) * r, static_cast<int64_t>(n))), s1 = min(s0 + stretch, n);
-  if (k <= 0) return;                // (the whole cluster)
-  if (k == n) {                                // nothing moves
-    for (int i = s0 + tid; i < s1; i += kThreads) {
+  if (k <= 0 || k == n) {                      // (the whole cluster) nothing moves
+    if (r == 0 && tid == 0) P.moves[pair] = 0;
+    for (int i = s0 + tid; k > 0 && i < s1; i += kThreads) {
       const int64_t pg = W.page(i);
       if (pg < 0) { set_status(&P.hdr->status, SS_ERR_BAD_INPUT); continue; }
       const int64_t at = W.beside(pg, i);
@@ -186,16 +207,26 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
     }
     return;
   }
-  for (int i = tid; i < kPasses * kBins; i += kThreads) (&S.total[0][0])[i] = 0;
 
   // ---- the largest order of the node
   int last = n - 1;
   if (P.order && P.recent > 0) {
     int mine = INT32_MIN;
-    for (int i = s0 + tid; i < s1; i += kThreads) {
-      const int64_t pg = W.page(i);
-      if (pg >= 0) mine = max(mine, P.order[W.beside(pg, i)]);
-    }
+    for_quads(W, s0, s1, [&](int i0, const int64_t (&page)[kAhead]) {
+      int4 o[kAhead];
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x)
+        if (page[x] >= 0) o[x] = *reinterpret_cast<const int4*>(P.order + W.beside(page[x], i0));
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) {
+        const int i = i0 + x * 4 * kThreads;
+        if (page[x] < 0) continue;
+        mine = max(mine, o[x].x);
+        if (i + 1 < s1) mine = max(mine, o[x].y);
+        if (i + 2 < s1) mine = max(mine, o[x].z);
+        if (i + 3 < s1) mine = max(mine, o[x].w);
+      }
+    });
     mine = __reduce_max_sync(0xffffffffu, mine);
     if (lane == 0) S.warp_last[warp] = mine;
     __syncthreads();
@@ -212,13 +243,37 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
 
   // ---- ranks, their range, how many must stay
   uint32_t lo = 0xffffffffu, hi = 0, must = 0;
-  for (int i = s0 + tid; i < s1; i += kThreads) {
-    const uint32_t u = W.rank(i, last);
-    if (i - s0 < kStaged) staged[i - s0] = u;
-    if (W.page(i) < 0) set_status(&P.hdr->status, SS_ERR_BAD_INPUT);
-    if (u == kMust) ++must;
-    else { lo = min(lo, u); hi = max(hi, u); }
-  }
+  for_quads(W, s0, s1, [&](int i0, const int64_t (&page)[kAhead]) {
+    float4 w[kAhead];
+    int4 o[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int i = i0 + x * 4 * kThreads;
+      w[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+      o[x] = make_int4(i, i + 1, i + 2, i + 3);
+      if (page[x] >= 0) {
+        const int64_t at = W.beside(page[x], i0);
+        w[x] = *reinterpret_cast<const float4*>(P.weights + at);
+        if (P.order) o[x] = *reinterpret_cast<const int4*>(P.order + at);
+      } else if (page[x] == -1) {
+        set_status(&P.hdr->status, SS_ERR_BAD_INPUT);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int i = i0 + x * 4 * kThreads;
+      const float wx[4] = {w[x].x, w[x].y, w[x].z, w[x].w};
+      const int ox[4] = {o[x].x, o[x].y, o[x].z, o[x].w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        if (i + y >= s1) continue;
+        const uint32_t u = page[x] >= 0 ? W.rank_of(wx[y], ox[y], last) : 0u;
+        if (i + y - s0 < P.staged) staged[i + y - s0] = u;
+        if (u == kMust) ++must;
+        else { lo = min(lo, u); hi = max(hi, u); }
+      }
+    }
+  });
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
   must = __reduce_add_sync(0xffffffffu, must);
@@ -231,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
     S.told.highest = hi;
     S.told.must = must_here;
   }
-  cluster_sync();                              // (also: the sums are zero, everywhere)
+  cluster_sync();
   uint32_t must_all = 0;
   lo = 0xffffffffu;
   hi = 0;
@@ -240,34 +295,37 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
     hi = max(hi, load_remote(remote(&S.told.highest, c)));
     must_all += load_remote(remote(&S.told.must, c));
   }
-  auto rank_of = [&](int i) { return i - s0 < kStaged ? staged[i - s0] : W.rank(i, last); };
+  auto rank_of = [&](int i) { return i - s0 < P.staged ? staged[i - s0] : W.rank(i, last); };
 
-  // ---- the border: `border` the smallest rank that stays, `ties` how many keys of that rank do
+  // ---- the border: `border` the smallest rank that stays, `ties` how many keys of that rank do, by slot
   uint32_t border = kMust, ties = static_cast<uint32_t>(k), ties_before = 0;
-  if (must_all >= static_cast<uint32_t>(k)) {  // among those that must stay, by slot
+  if (must_all >= static_cast<uint32_t>(k)) {  // among those that must stay
     for (uint32_t c = 0; c < r; ++c) ties_before += load_remote(remote(&S.told.must, c));
   } else {
     uint32_t left = static_cast<uint32_t>(k) - must_all;       // of those that go by weight, in [lo, hi]
     for (int pass = 0; pass < kPasses; ++pass) {
+      uint32_t (&own)[kBins] = S.own[pass & 1];                // (the other one may still be read)
       const uint32_t range = hi - lo;
       const int shift = range >= kBins ? 32 - __clz(range) - kBinBits : 0;       // (range >> shift) < kBins
-      for (int i = tid; i < kBins; i += kThreads) S.own[i] = 0;
+      for (int i = tid; i < kBins; i += kThreads) own[i] = 0;
+      if (tid == 0) S.pick_bin = S.pick_left = S.pick_whole = 0;
       __syncthreads();
       for (int i = s0 + tid; i < s1; i += kThreads) {
         const uint32_t u = rank_of(i);
-        if (u != kMust && u >= lo && u <= hi) atomicAdd(&S.own[(u - lo) >> shift], 1u);
+        if (u != kMust && u >= lo && u <= hi) atomicAdd(&own[(u - lo) >> shift], 1u);
       }
-      __syncthreads();
-      for (int i = tid; i < kBins; i += kThreads)
-        if (S.own[i]) add_remote(remote(&S.total[pass][i], 0), S.own[i]);
       cluster_sync();
       // the bin in which the border lies: bins from the top, four a thread
-      uint32_t c[4], sum = 0;
+      uint32_t c[4] = {0u, 0u, 0u, 0u}, sum = 0;
+      for (uint32_t b = 0; b < C; ++b) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        c[x] = load_remote(remote(&S.total[pass][kBins - 1 - (4 * tid + x)], 0));
-        sum += c[x];
+        for (int x = 0; x < 4; ++x) {
+          const int bin = kBins - 1 - (4 * tid + x);
+          c[x] += C == 1 ? own[bin] : load_remote(remote(&own[bin], b));
+        }
       }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sum += c[x];
       uint32_t incl = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -281,33 +339,41 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
         if (above < left && left <= above + c[x]) {
           S.pick_bin = static_cast<uint32_t>(kBins - 1 - (4 * tid + x));
           S.pick_left = left - above;
+          S.pick_whole = left == above + c[x];
         }
         above += c[x];
       }
       __syncthreads();
       const uint32_t bin = S.pick_bin;
+      const bool whole = S.pick_whole != 0;
       left = S.pick_left;
       lo += bin << shift;
       hi = shift ? min(hi, lo + ((1u << shift) - 1u)) : lo;
-      if (lo == hi) {                          // (all blocks at once) this block's keys of the border's rank are in own[bin]
-        if (tid == 0) S.told.must = S.own[bin];
+      if (whole) {                             // (all blocks at once) all of the bin stay, and none of it is tied with what goes
+        left = kAllTies;
+        break;
+      }
+      if (lo == hi) {                          // this block's keys of the border's rank are in own[bin]
+        if (tid == 0) S.told.must = own[bin];
+        cluster_sync();
+        for (uint32_t c2 = 0; c2 < r; ++c2) ties_before += load_remote(remote(&S.told.must, c2));
         break;
       }
       __syncthreads();
     }
     border = lo;
     ties = left;
-    cluster_sync();
-    for (uint32_t c = 0; c < r; ++c) ties_before += load_remote(remote(&S.told.must, c));
   }
 
   // ---- who stays.  A warp has a stretch of rows of 32 slots; ties by slot.
   const int rows = (s1 - s0 + 31) / 32, per = (rows + kWarps - 1) / kWarps;
   const int row0 = min(warp * per, rows), row1 = min(row0 + per, rows);
   uint32_t mine = 0;
-  for (int w = row0; w < row1; ++w) {
-    const int i = s0 + 32 * w + lane;
-    mine += __popc(__ballot_sync(0xffffffffu, i < s1 && rank_of(i) == border));
+  if (ties != kAllTies) {
+    for (int w = row0; w < row1; ++w) {
+      const int i = s0 + 32 * w + lane;
+      mine += __popc(__ballot_sync(0xffffffffu, i < s1 && rank_of(i) == border));
+    }
   }
   uint32_t unused;
   __syncthreads();
@@ -346,11 +412,14 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
     if (c < r) { hole_at += h; late_at += load_remote(remote(&S.told.late, c)); }
     moves += h;
   }
+  if (r == 0 && tid == 0) P.moves[pair] = static_cast<int>(moves);
   const int pages = (n + kPage - 1) / kPage;
   int32_t* free_list = P.lists + (W.page0 * P.Hkv + static_cast<int64_t>(W.g) * pages) * kPage;
   int32_t* late_list = free_list + pages * (kPage / 2);
   const bool noted = row1 <= kStaged / 32;     // (a row's ties go by all the rows in front of it)
+  const bool copies = P.weights_out != P.weights || (P.order_out && P.order_out != P.order) || P.source_out;
   tie = tie0;
+#pragma unroll 4
   for (int w = row0; w < row1; ++w) {
     const uint32_t bits = noted ? S.kept[w] : kept_row(w), front = below(w), me = 1u << lane;
     const uint32_t hole = ~bits & front, behind = bits & ~front;
@@ -359,7 +428,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
     if (behind & me) late_list[late_at + __popc(behind & (me - 1u))] = i;
     hole_at += __popc(hole);
     late_at += __popc(behind);
-    if (bits & front & me) {                   // remains
+    if (copies && (bits & front & me)) {       // remains
       const int64_t pg = W.page(i);
       if (pg >= 0) {
         const int64_t at = W.beside(pg, i);
@@ -369,37 +438,59 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
       }
     }
   }
-  cluster_sync();
+  cluster_sync();                              // (no block leaves while another may read what it tells)
+}
 
-  // ---- moves: a warp per key, K in the lower half's lanes, V in the upper's; kBatch keys on their way
-  constexpr int kBatch = 4;
-  const int moves_each = static_cast<int>((moves + C - 1) / C);
-  const int m0 = min(moves_each * static_cast<int>(r), static_cast<int>(moves)), m1 = min(m0 + moves_each, static_cast<int>(moves));
+// The moves of a node and head, P.move_blocks blocks for them: kBatch at a time a warp, whose places are looked up, and whose weights and orders
+// moved, by a lane each, a batch ahead; their rows by the warp together, K in the lower lanes, V in the upper.
+// (Batches of 16, 8, 4 with 2, 4, 6 blocks an SM: 339, 313, 279 us a call for 256 nodes of 2048 to 4096 keys cut to half, 4 heads.)
+__global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __grid_constant__ Params P) {
+  ss::grid_dependency_enter();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t pair = blockIdx.x / P.move_blocks;
+  const int part = static_cast<int>(blockIdx.x - pair * P.move_blocks);
+  const int moves = P.moves[pair];
+  const Node I = P.info[pair / P.Hkv];
+  Work W;
+  W.P = &P;
+  W.page0 = I.page0;
+  W.n = I.n;
+  W.g = static_cast<int>(pair % P.Hkv);
+  const int pages = (I.n + kPage - 1) / kPage, stride = P.move_blocks * kMoveWarps * kBatch;
+  const int32_t* free_list = P.lists + (W.page0 * P.Hkv + static_cast<int64_t>(W.g) * pages) * kPage;
+  const int32_t* late_list = free_list + pages * (kPage / 2);
   __nv_bfloat16* pool = (lane < 16 ? P.k_pool : P.v_pool) + static_cast<int64_t>(W.g) * P.head_stride + (lane & 15) * 8;
-  for (int j0 = m0 + warp * kBatch; j0 < m1; j0 += kWarps * kBatch) {
-    uint4 data[kBatch];
-    int64_t to[kBatch];
-#pragma unroll
-    for (int x = 0; x < kBatch; ++x) {
-      to[x] = -1;
-      if (j0 + x < m1) {
-        const int dst = free_list[j0 + x], src = late_list[j0 + x];
-        const int64_t dp = W.page(dst), sp = W.page(src);
-        if (dp >= 0 && sp >= 0) {
-          to[x] = dp * P.page_stride + (dst % kPage) * kDim;
-          data[x] = *reinterpret_cast<const uint4*>(pool + sp * P.page_stride + (src % kPage) * kDim);
-          if (lane == 0) {
-            const int64_t a = W.beside(dp, dst), b = W.beside(sp, src);
-            P.weights_out[a] = P.weights[b];
-            if (P.order_out) P.order_out[a] = P.order ? P.order[b] : src;
-            if (P.source_out) P.source_out[a] = src;
-          }
-        }
+  int to = -1, from = -1;                      // of the lane's move: page * 16 + slot; -1: none
+  auto look = [&](int j0) {
+    to = from = -1;
+    if (lane < kBatch && j0 + lane < moves) {
+      const int dst = free_list[j0 + lane], src = late_list[j0 + lane];
+      const int64_t dp = W.page(dst), sp = W.page(src);
+      if (dp >= 0 && sp >= 0) {
+        to = static_cast<int>(dp) * kPage + dst % kPage;
+        from = static_cast<int>(sp) * kPage + src % kPage;
+        const int64_t a = W.beside(dp, dst), b = W.beside(sp, src);
+        P.weights_out[a] = P.weights[b];
+        if (P.order_out) P.order_out[a] = P.order ? P.order[b] : src;
+        if (P.source_out) P.source_out[a] = src;
       }
     }
+  };
+  int j0 = (part * kMoveWarps + warp) * kBatch;
+  if (j0 < moves) look(j0);
+  for (; j0 < moves; j0 += stride) {
+    uint4 data[kBatch];
+    int t[kBatch];
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      t[x] = __shfl_sync(0xffffffffu, to, x);
+      const int f = __shfl_sync(0xffffffffu, from, x);
+      if (t[x] >= 0) data[x] = *reinterpret_cast<const uint4*>(pool + (f / kPage) * P.page_stride + (f % kPage) * kDim);
+    }
+    look(j0 + stride);
 #pragma unroll
     for (int x = 0; x < kBatch; ++x)
-      if (to[x] >= 0) *reinterpret_cast<uint4*>(pool + to[x]) = data[x];
+      if (t[x] >= 0) *reinterpret_cast<uint4*>(pool + (t[x] / kPage) * P.page_stride + (t[x] % kPage) * kDim) = data[x];
   }
 }
 
@@ -410,7 +501,7 @@ static int32_t check(const ss_attn_desc_t* d, const ss_evict_t* e) {
   if (d->head_dim != kDim || d->page_size != kPage || d->kv_token_stride != kDim || d->kv_page_stride % 128 || d->kv_head_stride % 128 ||
       d->kv_page_stride <= 0 || d->kv_head_stride <= 0)
     return SS_ERR_UNSUPPORTED;
-  if (d->num_kv_heads > 65536 || d->total_node_pages > 0x7ffffff || static_cast<int64_t>(e->n_nodes) * d->num_kv_heads > 0x7fffffffLL / kMostCluster)
+  if (d->num_kv_heads > 65536 || d->total_node_pages > 0x7ffffff || d->num_pages > 0x7ffffff || static_cast<int64_t>(e->n_nodes) * d->num_kv_heads > 0x7fffffffLL / kMostCluster)
     return SS_ERR_UNSUPPORTED;
   return SS_OK;
 }
@@ -420,6 +511,7 @@ static size_t carve(const ss_attn_desc_t* d, const ss_evict_t* e, void* base, Pa
   P->hdr = c.take<Header>(1);
   P->info = c.take<Node>(static_cast<size_t>(e->n_nodes) + 1);
   P->claim = c.take<int32_t>(static_cast<size_t>(d->num_nodes) + 1);
+  P->moves = c.take<int32_t>(static_cast<size_t>(e->n_nodes) * d->num_kv_heads + 1);
   P->lists = c.take<int32_t>(static_cast<size_t>(d->total_node_pages) * d->num_kv_heads * kPage + 1);
   return c.off;
 }
@@ -433,22 +525,28 @@ static int cluster_of(const ss_attn_desc_t* d, const ss_evict_t* e) {
   return c;
 }
 
-static int32_t launch_evict(const Params& P, const ss_attn_desc_t* d, const ss_evict_t* e, cudaStream_t st) {
-  constexpr int kSmem = kStaged * 4;
+static int32_t launch_evict(Params P, const ss_attn_desc_t* d, const ss_evict_t* e, cudaStream_t st) {
   static bool done[kDeviceSlots] = {false};
   const int slot = current_device_slot();
   if (slot < 0 || !done[slot]) {
-    if (cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
+    if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStaged * 4) != cudaSuccess) {
       (void)cudaGetLastError();
       return SS_ERR_CUDA;
     }
     if (slot >= 0) done[slot] = true;
   }
   const int c = cluster_of(d, e);
+  const int64_t pairs = static_cast<int64_t>(e->n_nodes) * d->num_kv_heads, all = d->total_node_pages * kPage;
+  const int64_t keys = e->max_keys > 0 && e->max_keys < all ? e->max_keys : all, each = ceil_div64(ceil_div64(keys, c), 32) * 32;
+  P.staged = static_cast<int>(each < kStaged ? each : kStaged);
+  // eight blocks of moves an SM, as long as each has a batch for its warps; half of the keys move at most
+  const int64_t wanted = ceil_div64(8LL * sm_count_of_current_device(), pairs), most = ceil_div64(keys, 2 * kBatch * kMoveWarps);
+  P.move_blocks = static_cast<int>(wanted < most ? wanted : most < 1 ? 1 : most);
+  if (pairs * P.move_blocks > 0x7fffffffLL) return SS_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(static_cast<int64_t>(e->n_nodes) * d->num_kv_heads * c));
+  cfg.gridDim = dim3(static_cast<unsigned>(pairs * c));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem;
+  cfg.dynamicSmemBytes = static_cast<size_t>(P.staged) * 4;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -458,12 +556,13 @@ static int32_t launch_evict(const Params& P, const ss_attn_desc_t* d, const ss_e
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = ss::pdl_enabled() ? 2 : 1;
-  const cudaError_t err = cudaLaunchKernelEx(&cfg, evict_kernel, P);
+  const cudaError_t err = cudaLaunchKernelEx(&cfg, evict_select_kernel, P);
   ss::g_launch_count.fetch_add(1, std::memory_order_relaxed);
   if (err != cudaSuccess || cudaPeekAtLastError() != cudaSuccess) {
     (void)cudaGetLastError();
     return SS_ERR_CUDA;
   }
+  SS_LAUNCH(evict_move_kernel, static_cast<unsigned>(pairs * P.move_blocks), kMoveThreads, 0, st, P);
   return SS_OK;
 }
 
@@ -491,7 +590,10 @@ extern "C" int32_t ss_kv_evict(const ss_attn_desc_t* d, const ss_evict_t* e, voi
   if (e->n_nodes > 0 && (!e->nodes || !e->keep || !e->weights || !d->k_pool || !d->v_pool || !d->node_kv_len || !d->node_page_offsets ||
                          !d->node_pages))
     return SS_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(d->k_pool) % 256 || reinterpret_cast<uintptr_t>(d->v_pool) % 256) return SS_ERR_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(d->k_pool) % 256 || reinterpret_cast<uintptr_t>(d->v_pool) % 256 || reinterpret_cast<uintptr_t>(e->weights) % 64 ||
+      reinterpret_cast<uintptr_t>(e->weights_out) % 64 || reinterpret_cast<uintptr_t>(e->order) % 64 || reinterpret_cast<uintptr_t>(e->order_out) % 64 ||
+      reinterpret_cast<uintptr_t>(e->source_out) % 64)
+    return SS_ERR_UNSUPPORTED;
   P.Hkv = d->num_kv_heads;
   P.k_pool = static_cast<__nv_bfloat16*>(const_cast<void*>(d->k_pool));
   P.v_pool = static_cast<__nv_bfloat16*>(const_cast<void*>(d->v_pool));
