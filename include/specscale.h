@@ -383,7 +383,7 @@ int32_t ss_draft_attention(const ss_attn_desc_t* desc /* host */, const int32_t*
  *   order        int32, the same layout, or NULL: sequence number of a key (ss_kv_evict keeps the first and the last by it)
  *   path_order   int32 [num_paths] or NULL: sequence number of the first token of a path's step; NULL: the index of that token in the
  *                path's whole sequence (right as long as nothing has been evicted)
- *   decay        finite, >= 0;  last_tokens >= 0
+ *   decay        finite, >= 0 (0: weights_in is not read);  last_tokens >= 0
  * Nodes may have any length.  T <= node_kv_len of the leaf (T = 0: the path adds nothing, its chain's keys are still written).  A leaf with
  * other paths below it: T <= 1.  The paths below a node are contiguous.
  * SS_FLAG_FORCE_GENERIC or SS_FLAG_NO_TCGEN05 run one key per warp on the CUDA cores (a second opinion); max_sms is kept to; the other flags
@@ -427,7 +427,7 @@ int32_t ss_key_weights(const ss_attn_desc_t* desc /* host */, const ss_key_weigh
  * step's attention and ss_key_weights, never between them: the step's own keys move, too.  A node with several paths below it must keep
  * a multiple of 16 tokens if ss_tree_attention is to take it.
  *
- *   nodes, keep   int32 [n_nodes] on the device
+ *   nodes, keep   int32 [n_nodes] on the device (a node that is listed again is an error, the first time counts)
  *   weights       fp32 as in ss_key_weights;  weights_out the same layout, or NULL: weights is updated in place (it may also be given twice)
  *   order         int32 as in ss_key_weights or NULL: the slot's number;  order_out the same layout, or NULL: in place
  *                 In either output only the slots < k of the nodes are written
@@ -439,7 +439,7 @@ int32_t ss_key_weights(const ss_attn_desc_t* desc /* host */, const ss_key_weigh
  *   workspace     >= ss_kv_evict_workspace_bytes(desc, ev) bytes, 256-byte aligned (4 bytes a slot and kv head).  Calls that share one must not
  *                 overlap
  * Errors (host): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE_TOO_SMALL, SS_ERR_CUDA.  Errors (device, via
- * ss_last_device_status): SS_ERR_BAD_INPUT (a node out of range, a length that its pages do not hold: the node is left as it is; a page outside the
+ * ss_last_device_status): SS_ERR_BAD_INPUT (a node out of range, or a length that its pages do not hold: the node is left as it is; a node that is listed again; a page outside the
  * pool: its keys rank last, and nothing moves from or to it).
  * ======================================================================================================= */
 typedef struct ss_evict {

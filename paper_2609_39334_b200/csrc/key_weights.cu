@@ -170,7 +170,8 @@ __global__ void __launch_bounds__(kPlanThreads, 1) key_plan_kernel(const __grid_
   long long total, n_recs, off = cost, rec = count;
   cluster_before(off, rec, scan[1], &total, &n_recs);
   for (int n = n0; n < n1; ++n) {
-    const long long c = rec_of(n, R, false);
+    // (the one node that a thread of a small tree has is still there)
+    const long long c = n1 - n0 == 1 ? cost : rec_of(n, R, false);
     if (R.len == 0) continue;
     R.off = off;
     P.recs[rec++] = R;

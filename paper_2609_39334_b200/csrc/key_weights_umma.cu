@@ -136,7 +136,7 @@ template <bool BLOCKS>
 __global__ void __launch_bounds__(kThreads, 1)
 key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_step,
                 const __grid_constant__ CUtensorMap tmap_token, const __grid_constant__ Params P) {
-  ss::grid_dependency_release();
+  ss::grid_dependency_enter();
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ Ctrl C;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -160,7 +160,6 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  ss::grid_dependency_wait();                  // (the set-up above needs nothing of the planner's)
   const uint32_t tmem = C.tmem_slot;
   const int G = P.G, per_step = kCols / G;     // tokens
   auto tokens_of = [&](int rows, int step) { return min(per_step, rows - step * per_step); };

@@ -21,8 +21,8 @@ constexpr int kNodesThreads = 1024;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kBinBits = 11;
 constexpr int kPasses = 3;                     // 33 bits
-static_assert(kBins == 4 * kThreads, "four bins a thread");
 constexpr int kMostCluster = 8;
+static_assert(kBins == 4 * kThreads && kBins % kMostCluster == 0, "bins of a thread, and of a block");
 constexpr int kStaged = 16384;                 // ranks of a block's slots that are kept in shared memory, at most; behind them they are made again
 constexpr int kAhead = 4;                      // quads of slots that a thread has on their way
 constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32, kBatch = 4;
@@ -98,6 +98,9 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
+__device__ __forceinline__ void blocks_sync(uint32_t blocks) {
+  if (blocks == 1) __syncthreads(); else cluster_sync();
+}
 // Address of the same variable in block `rank` of the cluster.
 __device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {
   uint32_t r;
@@ -114,7 +117,7 @@ __device__ __forceinline__ uint32_t load_remote(uint32_t at) {
 struct Told {
   uint32_t lowest, highest, must;              // ranks that go by weight, number of keys that must stay
   int last;                                    // largest order
-  uint32_t holes, late;
+  uint32_t holes, late, share;
 };
 struct Shared {
   uint32_t own[2][kBins];                      // this block's keys by bin, in passes in turn
@@ -234,7 +237,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
       for (int w = 1; w < kWarps; ++w) mine = max(mine, S.warp_last[w]);
       S.told.last = mine;
     }
-    cluster_sync();
+    blocks_sync(C);
     last = INT32_MIN;
     for (uint32_t c = 0; c < C; ++c) last = max(last, static_cast<int>(load_remote(remote(&S.told.last, c))));
   } else if (P.order) {
@@ -285,8 +288,9 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
     S.told.lowest = lo;
     S.told.highest = hi;
     S.told.must = must_here;
+    S.pick_bin = S.pick_left = S.pick_whole = 0;
   }
-  cluster_sync();
+  blocks_sync(C);
   uint32_t must_all = 0;
   lo = 0xffffffffu;
   hi = 0;
@@ -308,45 +312,55 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
       const uint32_t range = hi - lo;
       const int shift = range >= kBins ? 32 - __clz(range) - kBinBits : 0;       // (range >> shift) < kBins
       for (int i = tid; i < kBins; i += kThreads) own[i] = 0;
-      if (tid == 0) S.pick_bin = S.pick_left = S.pick_whole = 0;
       __syncthreads();
       for (int i = s0 + tid; i < s1; i += kThreads) {
         const uint32_t u = rank_of(i);
         if (u != kMust && u >= lo && u <= hi) atomicAdd(&own[(u - lo) >> shift], 1u);
       }
-      cluster_sync();
-      // the bin in which the border lies: bins from the top, four a thread
+      blocks_sync(C);
+      // The bin in which the border lies.  Bins from the top; a block adds up its share of them over the cluster, then all look at the shares' sums, and
+      // the block that has the border in its share tells.  (All bins of all blocks read by every block: a cluster of 8 took 76 us for 131072 keys
+      // a head, one of 16 172.)
+      const int share = kBins / static_cast<int>(C), mine_n = max(1, share / kThreads), bin0 = static_cast<int>(r) * share + mine_n * tid;
       uint32_t c[4] = {0u, 0u, 0u, 0u}, sum = 0;
-      for (uint32_t b = 0; b < C; ++b) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int bin = kBins - 1 - (4 * tid + x);
-          c[x] += C == 1 ? own[bin] : load_remote(remote(&own[bin], b));
-        }
+      for (int x = 0; x < 4; ++x) {
+        if (x >= mine_n || mine_n * tid >= share) continue;
+        for (uint32_t b = 0; b < C; ++b) c[x] += load_remote(remote(&own[kBins - 1 - (bin0 + x)], b));
+        sum += c[x];
       }
-#pragma unroll
-      for (int x = 0; x < 4; ++x) sum += c[x];
       uint32_t incl = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += up;
       }
-      uint32_t unused;
-      uint32_t above = block_before(__shfl_sync(0xffffffffu, incl, 31), S, pass & 1, &unused) + incl - sum;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if (above < left && left <= above + c[x]) {
-          S.pick_bin = static_cast<uint32_t>(kBins - 1 - (4 * tid + x));
-          S.pick_left = left - above;
-          S.pick_whole = left == above + c[x];
-        }
-        above += c[x];
+      uint32_t share_sum;
+      uint32_t above = block_before(__shfl_sync(0xffffffffu, incl, 31), S, pass & 1, &share_sum) + incl - sum;
+      if (tid == 0) S.told.share = share_sum;
+      blocks_sync(C);
+      uint32_t before = 0, owner = 0;
+      for (uint32_t b = 0; b < C; ++b) {
+        const uint32_t t = load_remote(remote(&S.told.share, b));
+        if (before + t < left) { before += t; owner = b + 1; } else break;
       }
-      __syncthreads();
-      const uint32_t bin = S.pick_bin;
-      const bool whole = S.pick_whole != 0;
-      left = S.pick_left;
+      if (owner == r) {
+        above += before;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          if (c[x] && above < left && left <= above + c[x]) {
+            S.pick_bin = static_cast<uint32_t>(kBins - 1 - (bin0 + x));
+            S.pick_left = left - above;
+            S.pick_whole = left == above + c[x];
+          }
+          above += c[x];
+        }
+      }
+      owner = min(owner, C - 1);
+      blocks_sync(C);
+      const uint32_t bin = load_remote(remote(&S.pick_bin, owner));
+      const bool whole = load_remote(remote(&S.pick_whole, owner)) != 0;
+      left = load_remote(remote(&S.pick_left, owner));
       lo += bin << shift;
       hi = shift ? min(hi, lo + ((1u << shift) - 1u)) : lo;
       if (whole) {                             // (all blocks at once) all of the bin stay, and none of it is tied with what goes
@@ -355,7 +369,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
       }
       if (lo == hi) {                          // this block's keys of the border's rank are in own[bin]
         if (tid == 0) S.told.must = own[bin];
-        cluster_sync();
+        blocks_sync(C);
         for (uint32_t c2 = 0; c2 < r; ++c2) ties_before += load_remote(remote(&S.told.must, c2));
         break;
       }
@@ -405,7 +419,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
   __syncthreads();
   uint32_t late_at = block_before(late, S, 0, &late_here);
   if (tid == 0) { S.told.holes = holes_here; S.told.late = late_here; }
-  cluster_sync();
+  blocks_sync(C);
   uint32_t moves = 0;
   for (uint32_t c = 0; c < C; ++c) {
     const uint32_t h = load_remote(remote(&S.told.holes, c));
@@ -438,7 +452,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
       }
     }
   }
-  cluster_sync();                              // (no block leaves while another may read what it tells)
+  blocks_sync(C);                              // (no block leaves while another may read what it tells)
 }
 
 // The moves of a node and head, P.move_blocks blocks for them: kBatch at a time a warp, whose places are looked up, and whose weights and orders
