@@ -9,6 +9,8 @@
 //                        by at most three histograms of 2048 bins over a range that shrinks (the first from the smallest to the largest
 //                        weight; done when a bin stays as a whole), then ranks by counts, and lists of free slots and of late keys
 //   evict_move_kernel    blocks for every node and head: the moves
+// Bound: the moves by HBM, 256 bytes here and there (256 nodes of 2048 to 4096 keys cut to half, 4 heads: 268 us a call, some 4.5 TB/s while they move); the
+// selection by latency (131072 keys of 8 heads: 51 us of 112).  One kernel that selects and moves took 353 and 263 us.
 #include <string.h>
 
 #include "common.cuh"
