@@ -193,11 +193,9 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
       key0 = pair * 2 * kTile;
       off = R.off + pair * row + static_cast<long long>(g) * cost;
     }
-    // Pages of a pair of tiles, one a lane
-    auto pages_of = [&](const Rec& r, int key) -> int {
-      const int at = key / kPage + lane;
-      return lane < 2 * kTilePages && r.len > at * kPage ? __ldg(P.node_pages + r.page0 + at) : -1;
-    };
+    // Pages of a pair of tiles, one a lane (whether there is one goes by its place: an entry may hold anything)
+    auto has_page = [&](const Rec& r, int key) { return lane < 2 * kTilePages && r.len > (key / kPage + lane) * kPage; };
+    auto pages_of = [&](const Rec& r, int key) -> int { return has_page(r, key) ? __ldg(P.node_pages + r.page0 + key / kPage + lane) : -1; };
     auto pages_behind = [&]() { return key0 + 2 * kTile < R.len ? pages_of(R, key0 + 2 * kTile) : pages_of(N, 0); };
     int page = pages_of(R, key0);
     int ahead = pages_behind();
@@ -207,7 +205,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
       const int step0 = step_at(start - off, tiles, R.steps, step_cost), step1 = step_at(end - off, tiles, R.steps, step_cost);
       if (step0 < step1) {
         Unit& U = C.unit[seq % kUnits];
-        const bool bad = page != -1 && (page < 0 || page >= P.num_pages);
+        const bool bad = has_page(R, key0) && (page < 0 || page >= P.num_pages);
         if (bad) set_status(&P.hdr->status, SS_ERR_BAD_INPUT);
         int parts = 1, owner = 0;
         if (step1 - step0 < R.steps) {
