@@ -45,7 +45,7 @@ struct alignas(16) Unit {
   int parts, owner;                            // parts > 1: shared by so many blocks, the first of which is `owner`
   int row0, rows, len, known, hides, order0;   // of the node's Rec
   int pad[2];
-  int page[2 * kTilePages];                    // -1: none, or outside the pool
+  int page[2 * kTilePages];                    // -1: none, or outside the pool (whoever writes a key tells, by whether the node has it)
 };
 struct Ctrl {
   uint64_t unit_ready[kUnits], unit_free[kUnits];
@@ -169,6 +169,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     // =================================================== units ===================================================
     const long long total = P.hdr->total, quota = max(quotient(total + gridDim.x - 1, gridDim.x), static_cast<long long>(kLeastQuota)), start = quota * blockIdx.x;
     const long long end = min(start + quota, total);
+    const uint32_t pool_pages = static_cast<uint32_t>(min(P.num_pages, static_cast<int64_t>(0x7fffffff)));
     const int n_recs = P.hdr->n_recs, step_cost = (per_step * G + 15) / 16;
     bool ok = true;
     Rec R = {}, N = {}, M = {};                // the unit's node, the next one, the one behind that
@@ -193,9 +194,11 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
       key0 = pair * 2 * kTile;
       off = R.off + pair * row + static_cast<long long>(g) * cost;
     }
-    // Pages of a pair of tiles, one a lane (whether there is one goes by its place: an entry may hold anything)
-    auto has_page = [&](const Rec& r, int key) { return lane < 2 * kTilePages && r.len > (key / kPage + lane) * kPage; };
-    auto pages_of = [&](const Rec& r, int key) -> int { return has_page(r, key) ? __ldg(P.node_pages + r.page0 + key / kPage + lane) : -1; };
+    // Pages of a pair of tiles, one a lane
+    auto pages_of = [&](const Rec& r, int key) -> int {
+      const int at = key / kPage + lane;
+      return lane < 2 * kTilePages && r.len > at * kPage ? __ldg(P.node_pages + r.page0 + at) : -1;
+    };
     auto pages_behind = [&]() { return key0 + 2 * kTile < R.len ? pages_of(R, key0 + 2 * kTile) : pages_of(N, 0); };
     int page = pages_of(R, key0);
     int ahead = pages_behind();
@@ -205,8 +208,6 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
       const int step0 = step_at(start - off, tiles, R.steps, step_cost), step1 = step_at(end - off, tiles, R.steps, step_cost);
       if (step0 < step1) {
         Unit& U = C.unit[seq % kUnits];
-        const bool bad = has_page(R, key0) && (page < 0 || page >= P.num_pages);
-        if (bad) set_status(&P.hdr->status, SS_ERR_BAD_INPUT);
         int parts = 1, owner = 0;
         if (step1 - step0 < R.steps) {
           // (the first and the last block that its cost reaches into may have none of its steps, those between have: see kLeastQuota)
@@ -217,7 +218,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         if (seq >= kUnits) ok = mbar_wait(&C.unit_free[seq % kUnits], (seq / kUnits - 1) & 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        if (lane < 2 * kTilePages) U.page[lane] = bad ? -1 : page;
+        if (lane < 2 * kTilePages) U.page[lane] = static_cast<uint32_t>(page) < pool_pages ? page : -1;
         if (lane == 0) {
           int4* to = reinterpret_cast<int4*>(&U);
           to[0] = make_int4(1, key0, tiles, g);
@@ -476,6 +477,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
       }
       if (there && writes) {
         bool write = page >= 0;
+        if (!write && i < len) set_status(&P.hdr->status, SS_ERR_BAD_INPUT);
         if (U.parts > 1) {
           const int owner = U.owner, parts = U.parts;
           auto part_of = [&](int b) { return P.part + (static_cast<int64_t>(2 * b + (b == owner ? 1 : 0)) * 2 + w) * kTile + key; };

@@ -1,4 +1,6 @@
 """ss_key_weights where its inputs are at their ends."""
+import math
+
 import pytest
 import torch
 
@@ -6,6 +8,7 @@ import test_gpu_key_weights as weights
 from paper_2609_39334_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
 PATHS = [0, B.SS_FLAG_FORCE_GENERIC]
 
 
@@ -40,3 +43,59 @@ def test_entries_behind_a_nodes_keys_may_hold_anything(flags):
         c.pool[spare] = float("nan")
     assert c.run(flags) == B.SS_OK
     c.check()
+
+
+# ---- rows that add nothing, rows that are not finite -----------------------------------------------------
+@pytest.mark.parametrize("flags", PATHS)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_rows_that_are_switched_off_may_hold_anything(value, flags):
+    c = weights.Case(33, 12, 2, [[64, 200], [64, 9]], [40, 2], shared=(0,))
+    c.lse[7], c.lse[41], c.lse[20, 4], c.lse[33, 9] = (-math.inf,) * 4
+    c.q[7], c.q[41, :, 5], c.q[20, 4], c.q[33, 9, 17] = (value,) * 4
+    assert c.run(flags) == B.SS_OK
+    c.check()
+
+
+@pytest.mark.parametrize("flags", PATHS)
+@pytest.mark.parametrize("hq,hkv,T", [(12, 2, 40), (32, 8, 64), (128, 1, 3), (1, 1, 1)])
+def test_where_every_row_is_switched_off_the_weights_are_zero(hq, hkv, T, flags):
+    c = weights.Case(34, hq, hkv, [[64, 200], [64, 9]], [T, 2], shared=(0,), decay=0.0)
+    c.lse.fill_(-math.inf)
+    assert c.run(flags) == B.SS_OK
+    written = c.expected()[3]
+    assert (c.weights[written] == 0).all()
+    c.check()
+
+
+@pytest.mark.parametrize("flags", PATHS)
+@pytest.mark.parametrize("kind", ["nan", "inf", "lse nan", "lse inf", "lse far below"])
+@pytest.mark.parametrize("column", [0, 3, 14, 15, 46, 47, 62, 79, 100, 110, 111, 119])
+def test_a_row_that_is_not_finite(column, kind, flags):
+    """One query row of a step (token column / 6, head column % 6 of the second group of 6): what exp(s - lse) comes to reaches the weights of
+    the keys that it sees, whichever unit the exponential of its column is taken by, and no other."""
+    c = weights.Case(35, 12, 2, [[64, 200], [64, 9]], [20, 2], shared=(0,))
+    t, h = column // 6, 6 + column % 6
+    lse = float(c.lse[t, h])
+    c.lse[t, h] = -math.inf
+    want, tol, _, written = c.expected()
+    c.lse[t, h] = lse
+    if kind == "nan":
+        c.q[t, h, 9] = float("nan")
+    elif kind == "inf":
+        c.q[t, h, 9] = float("inf")
+    else:
+        c.lse[t, h] = {"lse nan": float("nan"), "lse inf": float("inf"), "lse far below": -3e38}[kind]
+    s, vis, _ = c.scores(0)
+    term = torch.where(vis[h, t], torch.exp(s[h, t] - c.lse[t, h].double()), 0)       # 0, inf or NaN
+    term = torch.where(term > 3.5e38, math.inf, term)                                # (as fp32 holds it)
+    assert not (torch.isfinite(term) & (term != 0)).any()
+    at = 0
+    for n in c.chain[0]:
+        i = torch.arange(c.lens[n], device=DEV)
+        want[c.pages.long()[c.off[n] + i // 16], 1, i % 16] += term[at:at + c.lens[n]]
+        at += c.lens[n]
+    assert c.run(flags) == B.SS_OK
+    got, fin = c.weights.double(), torch.isfinite(want)
+    assert torch.equal(torch.isnan(got)[written], torch.isnan(want)[written])
+    assert torch.equal(torch.isposinf(got)[written], torch.isposinf(want)[written])
+    assert ((got - want).abs() <= tol)[written & fin].all()
