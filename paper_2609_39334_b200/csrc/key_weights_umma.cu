@@ -55,7 +55,7 @@ struct Ctrl {
   uint32_t tmem_slot;
   int abort_flag;
   int last[4];
-  alignas(16) float minus_lse[kLse][kCols];    // - lse * log2(e) of a step's rows; -inf: the row adds nothing
+  alignas(16) float minus_lse[kLse][kCols];    // - lse * log2(e) of a step's rows; inf: the row adds nothing
   float other[2][2][kTile];                    // sums on their way from one group of a tile to the other
   Unit unit[kUnits];
 };
@@ -68,6 +68,12 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
+}
+__device__ __forceinline__ void tmem_ld2(uint32_t taddr, uint32_t (&r)[2]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];"
+               : "=r"(r[0]), "=r"(r[1])
+               : "r"(taddr)
+               : "memory");
 }
 __device__ __forceinline__ long long quotient(long long a, long long b) {        // (a division of 64 bits takes some hundred clocks)
   return (a | b) >> 31 ? a / b : static_cast<int>(a) / static_cast<int>(b);
@@ -93,7 +99,9 @@ __device__ __forceinline__ int step_at(long long at, int tiles, int steps, int p
 }
 __device__ __forceinline__ int columns_padded(int n) { return n <= 16 ? 16 : (n + 15) & ~15; }
 
-// Exponentials of 32 scores of a key, added up.
+// Exponentials of 32 scores of a key, added up.  A term that is not finite, and one of a row that adds nothing (which comes out as infinity, or
+// NaN), makes the sum kLarge or more, or a NaN (see exp2_pair): the step's columns are then added up again by sum_exps_masked<true>.
+constexpr float kLarge = 8.507059173e37f;      // 2^126
 __device__ __forceinline__ float sum_exps(const uint32_t (&s)[32], const float* minus_lse, float scale) {
   const f32x2 scale2 = pack2(scale, scale);
   f32x2 sum[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
@@ -119,14 +127,14 @@ __device__ __forceinline__ float sum_exps(const uint32_t (&s)[32], const float* 
   unpack2(sum[1], c, d);
   return (a + b) + (c + d);
 }
-// The same for columns [from, to) alone.
-template <int N>
+// The same for columns [from, to) alone; EXACT: of rows that add nothing, nothing, whatever their scores are, and infinities and NaN as they are.
+template <bool EXACT, int N>
 __device__ __forceinline__ float sum_exps_masked(const uint32_t (&s)[N], const float* minus_lse, float scale, int from, int to) {
   float sum[2] = {0.f, 0.f};
 #pragma unroll
   for (int c = 0; c < N; ++c) {
-    const float e = ex2(fmaf(__uint_as_float(s[c]), scale, minus_lse[c]));
-    sum[c & 1] += c >= from && c < to ? e : 0.f;
+    const float l = minus_lse[c], e = ex2(fmaf(__uint_as_float(s[c]), scale, l));
+    sum[c & 1] += c >= from && c < to && !(EXACT && l == INFINITY) ? e : 0.f;
   }
   return sum[0] + sum[1];
 }
@@ -392,7 +400,10 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
           }
         }
 #pragma unroll
-        for (int x = 0; x < 4; ++x) C.minus_lse[ls][32 * x + lane] = l[x] == -INFINITY ? -INFINITY : -l[x] * 1.4426950408889634f;
+        for (int x = 0; x < 4; ++x) {
+          const float m = -l[x] * 1.4426950408889634f;
+          C.minus_lse[ls][32 * x + lane] = l[x] != -INFINITY && m == INFINITY ? 3.402823466e38f : m;
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(&C.l_full[ls]);
       }
@@ -448,8 +459,19 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             uint32_t a[16];
             tmem_ld16(t_s + c, a);
             tmem_wait_ld();
-            part += sum_exps_masked<16>(a, minus_lse + c, scale, from - c, n - c);
+            part += sum_exps_masked<false>(a, minus_lse + c, scale, from - c, n - c);
             c += 16;
+          }
+          // (Hardly ever; two columns at a time, for what stands here is paid for by all: with sixteen 1024 paths of one token took 142 us, not 138)
+          if (__any_sync(0xffffffffu, page >= 0 && !(part < kLarge))) {         // (what lies behind a node's keys may be anything)
+            part = 0.f;
+#pragma unroll 1
+            for (c = 0; c < n; c += 2) {
+              uint32_t a[2];
+              tmem_ld2(t_s + c, a);
+              tmem_wait_ld();
+              part += sum_exps_masked<true>(a, minus_lse + c, scale, from - c, n - c);
+            }
           }
           tc_fence_before();
           sum += part;
