@@ -427,7 +427,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
       const int page = there && i < len ? U.page[w * kTilePages + key / kPage] : -1;
       const int64_t to = (static_cast<int64_t>(page) * P.Hkv + g) * kPage + key % kPage;
       const float before = writes && P.weights_in && page >= 0 && i < U.known ? P.weights_in[to] : 0.f;
-      const int hidden = (i - len + U.hides) * G;
+      const int hidden = max(i - len + U.hides, 0) * G;          // (no more than the rows there are: a product of all keys would not fit)
       float sum = 0.f;
       for (int j = step0; j < step1; ++j, ++step) {
         if (static_cast<int>(step & 1) != p) continue;

@@ -99,3 +99,48 @@ def test_a_row_that_is_not_finite(column, kind, flags):
     assert torch.equal(torch.isnan(got)[written], torch.isnan(want)[written])
     assert torch.equal(torch.isposinf(got)[written], torch.isposinf(want)[written])
     assert ((got - want).abs() <= tol)[written & fin].all()
+
+
+# ---- very many keys, very many rows ----------------------------------------------------------------------
+def alike(hq, lens, parent, leaf, pages, q, lse, T=None, lse_rows=None):
+    """A descriptor over a pool of one kv head and few pages, which nodes have many times over (a page's keys get the same weight wherever the
+    page is, so it may be written any number of times)."""
+    i32, i64 = dict(dtype=torch.int32, device=DEV), dict(dtype=torch.int64, device=DEV)
+    n = len(leaf) if isinstance(leaf, list) else leaf.numel()
+    off = [0]
+    for x in lens:
+        off.append(off[-1] + -(-x // 16))
+    pool = pages["pool"]
+    keep = [torch.tensor(parent, **i32), torch.tensor(lens, **i32), torch.tensor(off, **i64), torch.as_tensor(leaf, **i32),
+            torch.ones(n, **i32), torch.arange(n + 1, **i64), torch.zeros(n, **i64)]
+    d = B.make_attn_desc(
+        num_q_heads=hq, num_kv_heads=1, k_pool=pool[:, 0], v_pool=pool[:, 1], num_pages=pool.shape[0], kv_page_stride=pool.stride(0),
+        kv_head_stride=2048, kv_token_stride=128, node_parent=keep[0], node_kv_len=keep[1], node_page_offsets=keep[2], node_pages=pages["of"],
+        total_node_pages=off[-1], path_leaf_node=keep[3], path_q_len=keep[4], q_offsets=keep[5], total_q=n, q=q, out=torch.empty(n, 1, 1, device=DEV),
+        lse=lse, q_src_offsets=keep[6], q_src_rows=1)
+    d._alike = keep
+    return d
+
+
+@pytest.mark.parametrize("hq,hidden", [(128, True), (128, False), (32, True)])
+def test_keys_far_in_front_of_a_nodes_end(hq, hidden):
+    """More than 2^31 / heads keys in front of it: 17 million of 128 heads, 67 million of 32.  hidden: the node is the step's own leaf."""
+    g = torch.Generator(device=DEV).manual_seed(36)
+    n = (1 << 31) // hq + 2048
+    pool = torch.randn(2, 2, 1, 16, 128, generator=g, device=DEV).bfloat16()
+    lens = [n] if hidden else [n, 1]
+    of = torch.ones(sum(-(-x // 16) for x in lens), dtype=torch.int32, device=DEV)
+    of[:64] = 0                                                   # (page 0 holds the first 1024 keys, page 1 all others)
+    q = torch.randn(1, hq, 128, generator=g, device=DEV).bfloat16()
+    lse = torch.full((1, hq), 3.0, device=DEV)
+    d = alike(hq, lens, [-1] if hidden else [-1, 0], [0] if hidden else [1], dict(pool=pool, of=of), q, lse)
+    w = torch.full((2, 1, 16), 7.0, device=DEV)
+    kw = B.make_key_weights(weights_out=w)
+    ws = B.alloc_workspace(B.ss_key_weights_workspace_bytes(d, kw), DEV)
+    B.ss_key_weights(d, kw, ws)
+    assert B.ss_last_device_status(ws) == B.SS_OK
+    k, x = pool[:, 0, 0].double(), q[0].double()                 # [2][16][128], [hq][128]
+    s, size = k @ x.T / math.sqrt(128), k.abs() @ x.abs().T / math.sqrt(128)
+    e = torch.exp(s - 3)
+    tol = (e * (130 * 2.0 ** -23 * size + 2.0 ** -22 * (s.abs() + 3) + 2.0 ** -21)).sum(-1) + e.sum(-1) * 50 * 2.0 ** -24
+    assert ((w[:, 0].double() - e.sum(-1)).abs() <= tol).all()
