@@ -54,6 +54,7 @@ struct Ctrl {
   uint64_t other_full[2][2], other_free[2][2];
   uint32_t tmem_slot;
   int abort_flag;
+  int steps;                                   // that have been multiplied
   int last[4];
   alignas(16) float minus_lse[kLse][kCols];    // - lse * log2(e) of a step's rows; inf: the row adds nothing
   float other[2][2][kTile];                    // sums on their way from one group of a tile to the other
@@ -96,6 +97,29 @@ __device__ __forceinline__ int step_at(long long at, int tiles, int steps, int p
   const long long v = (tiles == 1 ? at : (at + 1) >> 1) - kTileCost;
   if (v <= 0) return 0;
   return static_cast<int>(min(quotient(v + per_step - 1, per_step), static_cast<long long>(steps)));
+}
+// mbar_wait of a role that waits for whole units of others: their steps may take longer than the limit (2500 clocks a step, and as many steps as
+// there are query rows), and no wait within a step is without one.  The limit counts from the last step that was seen to begin.
+__device__ __forceinline__ bool wait_behind_steps(uint64_t* bar, uint32_t parity, Ctrl& C) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const volatile int* steps = &C.steps;
+  volatile int* abort_flag = &C.abort_flag;
+  long long t0 = 0;
+  uint32_t spins = 0;
+  int seen = 0;
+  while (!mbar_try_wait_suspend(bar, parity, 20000u)) {
+    if ((++spins & 15u) != 0u) continue;
+    if (*abort_flag) return false;
+    const int now = *steps;
+    if (t0 == 0 || now != seen) {
+      t0 = clock64();
+      seen = now;
+    } else if (clock64() - t0 > kWaitCycles) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+  return true;
 }
 __device__ __forceinline__ int columns_padded(int n) { return n <= 16 ? 16 : (n + 15) & ~15; }
 
@@ -151,6 +175,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
   volatile int* abort_flag = &C.abort_flag;
   if (tid == 0) {
     C.abort_flag = (smem_u32(smem) & 1023u) ? 1 : 0;
+    C.steps = 0;
     for (int x = 0; x < kUnits; ++x) { mbar_init(&C.unit_ready[x], 1); mbar_init(&C.unit_free[x], kSumWarps + 1 + kQWarps + kKWarps); }
     for (int x = 0; x < kStagesK; ++x) { mbar_init(&C.k_full[x], 1); mbar_init(&C.k_empty[x], 1); }
     for (int x = 0; x < kStagesQ; ++x) { mbar_init(&C.q_full[x], 1); mbar_init(&C.q_empty[x], 1); }
@@ -223,7 +248,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
           owner = static_cast<int>(b0) + (step_at((b0 + 1) * quota - off, tiles, R.steps, step_cost) == 0 ? 1 : 0);
           parts = static_cast<int>(b1) + (step_at(b1 * quota - off, tiles, R.steps, step_cost) < R.steps ? 1 : 0) - owner;
         }
-        if (seq >= kUnits) ok = mbar_wait(&C.unit_free[seq % kUnits], (seq / kUnits - 1) & 1, abort_flag);
+        if (seq >= kUnits) ok = wait_behind_steps(&C.unit_free[seq % kUnits], (seq / kUnits - 1) & 1, C);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (lane < 2 * kTilePages) U.page[lane] = static_cast<uint32_t>(page) < pool_pages ? page : -1;
@@ -254,7 +279,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         ahead = pages_behind();
       }
     }
-    if (seq >= kUnits) ok = mbar_wait(&C.unit_free[seq % kUnits], (seq / kUnits - 1) & 1, abort_flag) && ok;
+    if (seq >= kUnits) ok = wait_behind_steps(&C.unit_free[seq % kUnits], (seq / kUnits - 1) & 1, C) && ok;
     __syncwarp();
     if (lane == 0) { C.unit[seq % kUnits].valid = 0; mbar_arrive(&C.unit_ready[seq % kUnits]); }
   } else if (warp >= kWarpK) {
@@ -280,7 +305,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         int rows[kTilePages];
 #pragma unroll
         for (int p = 0; p < kTilePages; ++p) rows[p] = __shfl_sync(0xffffffffu, row, x * kTilePages + p);
-        if (kt >= kStagesK) ok = mbar_wait(&C.k_empty[st], (kt / kStagesK - 1) & 1, abort_flag) && ok;
+        if (kt >= kStagesK) ok = wait_behind_steps(&C.k_empty[st], (kt / kStagesK - 1) & 1, C) && ok;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (elect_one()) {
@@ -316,6 +341,7 @@ key_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         mbar_arrive(&C.unit_free[seq % kUnits]);
         for (int j = step0; j < step1 && ok; ++j, ++step) {
           const int qs = step % kStagesQ;
+          *const_cast<volatile int*>(&C.steps) = static_cast<int>(step);
           ok = mbar_wait(&C.q_full[qs], (step / kStagesQ) & 1, abort_flag);
           const uint32_t idesc = instr_desc_bf16(128, columns_padded(tokens_of(rows, j) * G), false);
           const uint64_t q_desc = smem_desc_advance(q_desc0, static_cast<uint32_t>(qs) * kStageBytes);

@@ -144,3 +144,26 @@ def test_keys_far_in_front_of_a_nodes_end(hq, hidden):
     e = torch.exp(s - 3)
     tol = (e * (130 * 2.0 ** -23 * size + 2.0 ** -22 * (s.abs() + 3) + 2.0 ** -21)).sum(-1) + e.sum(-1) * 50 * 2.0 ** -24
     assert ((w[:, 0].double() - e.sum(-1)).abs() <= tol).all()
+
+
+def test_a_unit_of_more_steps_than_a_wait_is_long():
+    """260000 rows of 128 heads below 768 keys, on one SM: a pair of tiles takes a step for each of them, some 0.3 s, and the warps that load
+    the keys behind the next pair wait for all of it."""
+    g = torch.Generator(device=DEV).manual_seed(37)
+    hq, n = 128, 260000
+    pool = torch.randn(48, 2, 1, 16, 128, generator=g, device=DEV).bfloat16()
+    q = torch.randn(1, hq, 128, generator=g, device=DEV).bfloat16()
+    lse = torch.full((n, hq), 3.0, device=DEV)
+    d = alike(hq, [768], [-1], torch.zeros(n, dtype=torch.int32), dict(pool=pool, of=torch.arange(48, dtype=torch.int32, device=DEV)), q, lse)
+    d.max_sms = 1
+    w = torch.full((48, 1, 16), 7.0, device=DEV)
+    kw = B.make_key_weights(weights_out=w)
+    ws = B.alloc_workspace(B.ss_key_weights_workspace_bytes(d, kw), DEV)
+    B.ss_key_weights(d, kw, ws)
+    assert B.ss_last_device_status(ws) == B.SS_OK
+    k, x = pool[:, 0, 0].double(), q[0].double()
+    s, size = k @ x.T / math.sqrt(128), k.abs() @ x.abs().T / math.sqrt(128)
+    e = torch.exp(s - 3)
+    # (the same in every step, and the steps' sums are added up one by one)
+    off = (e * (130 * 2.0 ** -23 * size + 2.0 ** -22 * (s.abs() + 3) + 2.0 ** -21)).sum(-1) + e.sum(-1) * (50 + n) * 2.0 ** -24
+    assert ((w[:, 0].double() / n - e.sum(-1)).abs() <= off).all()
