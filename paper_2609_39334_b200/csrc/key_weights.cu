@@ -261,7 +261,7 @@ static size_t carve(const ss_attn_desc_t* d, void* base, Params* P) {
 static int32_t launch_plan(const Params& P, cudaStream_t st, int blocks) {
   // (small trees: one block, whose barriers are the cheapest)
   const int64_t size = static_cast<int64_t>(P.num_nodes) + P.num_paths + P.total_q / 32;
-  const int c = size <= 2 * kPlanThreads ? 1 : kPlanBlocks;
+  const int c = size <= 2 * kPlanThreads ? 1 : blocks < kPlanBlocks ? blocks : kPlanBlocks;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(c);
   cfg.blockDim = dim3(kPlanThreads);
@@ -348,7 +348,8 @@ extern "C" int32_t ss_key_weights(const ss_attn_desc_t* d, const ss_key_weights_
   const int32_t planned = launch_plan(P, st, sms);
   if (planned != SS_OK || d->num_paths == 0 || d->num_nodes == 0) return planned;
   if (d->flags & (SS_FLAG_FORCE_GENERIC | SS_FLAG_NO_TCGEN05)) {
-    SS_LAUNCH(key_plain_kernel, 8 * sms, kPlainThreads, 0, st, P);
+    // (blocks go to all SMs before any gets a second one)
+    SS_LAUNCH(key_plain_kernel, sms < ss::sm_count_of_current_device() ? sms : 8 * sms, kPlainThreads, 0, st, P);
     return SS_OK;
   }
   return launch_tiles(P, st, sms);

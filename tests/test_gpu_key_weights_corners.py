@@ -1,4 +1,5 @@
 """ss_key_weights where its inputs are at their ends."""
+import ctypes
 import math
 
 import pytest
@@ -167,3 +168,44 @@ def test_a_unit_of_more_steps_than_a_wait_is_long():
     # (the same in every step, and the steps' sums are added up one by one)
     off = (e * (130 * 2.0 ** -23 * size + 2.0 ** -22 * (s.abs() + 3) + 2.0 ** -21)).sum(-1) + e.sum(-1) * (50 + n) * 2.0 ** -24
     assert ((w[:, 0].double() / n - e.sum(-1)).abs() <= off).all()
+
+
+# ---- SMs -------------------------------------------------------------------------------------------------
+class KernelNode(ctypes.Structure):
+    _fields_ = [("func", ctypes.c_void_p)] + [(x, ctypes.c_uint) for x in ("gx", "gy", "gz", "bx", "by", "bz", "shared")] + \
+        [("params", ctypes.c_void_p), ("extra", ctypes.c_void_p), ("kern", ctypes.c_void_p), ("ctx", ctypes.c_void_p)]
+
+
+def grids(call):
+    """Blocks of the kernels that `call` launches (captured, not run)."""
+    cuda = ctypes.CDLL("libcuda.so.1")
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    raw, count = ctypes.c_void_p(graph.raw_cuda_graph()), ctypes.c_size_t(0)
+    assert cuda.cuGraphGetNodes(raw, None, ctypes.byref(count)) == 0
+    nodes = (ctypes.c_void_p * count.value)()
+    assert cuda.cuGraphGetNodes(raw, nodes, ctypes.byref(count)) == 0
+    blocks = []
+    for node in nodes:
+        kind = ctypes.c_int(-1)
+        assert cuda.cuGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind)) == 0
+        if kind.value == 0:                                       # a kernel
+            k = KernelNode()
+            assert cuda.cuGraphKernelNodeGetParams_v2(ctypes.c_void_p(node), ctypes.byref(k)) == 0
+            blocks.append(k.gx * k.gy * k.gz)
+    return blocks
+
+
+@pytest.mark.parametrize("flags", PATHS)
+@pytest.mark.parametrize("sms", [1, 6, 20])
+def test_a_bound_on_the_sms_is_kept_to(sms, flags):
+    """By every kernel of the call: blocks are spread over the SMs first, so there are no more of them than that."""
+    c = weights.Case(38, 12, 2, [[512, 1 + p % 50] for p in range(1024)], [1 + (p % 7 == 0) for p in range(1024)], shared=(0,))
+    c.desc.flags, c.desc.max_sms = flags, sms
+    blocks = grids(lambda: B.ss_key_weights(c.desc, c.kw, c.ws))
+    assert len(blocks) == 2 and max(blocks) <= sms, blocks
+    c.weights.copy_(c.untouched)
+    c.order.fill_(-7)
+    assert c.run(flags) == B.SS_OK
+    c.check()
