@@ -384,7 +384,8 @@ int32_t ss_draft_attention(const ss_attn_desc_t* desc /* host */, const int32_t*
  *   path_order   int32 [num_paths] or NULL: sequence number of the first token of a path's step; NULL: the index of that token in the
  *                path's whole sequence (right as long as nothing has been evicted)
  *   decay        finite, >= 0 (0: weights_in is not read);  last_tokens >= 0
- * Nodes may have any length.  T <= node_kv_len of the leaf (T = 0: the path adds nothing, its chain's keys are still written).  A leaf with
+ * Nodes may have any length up to 2^31 - 256 (total_node_pages <= 2^27 - 16, num_nodes and num_paths <= 2^30, else
+ * SS_ERR_UNSUPPORTED).  T <= node_kv_len of the leaf (T = 0: the path adds nothing, its chain's keys are still written).  A leaf with
  * other paths below it: T <= 1.  The paths below a node are contiguous.
  * SS_FLAG_FORCE_GENERIC or SS_FLAG_NO_TCGEN05 run one key per warp on the CUDA cores (a second opinion); max_sms is kept to; the other flags
  * make no difference (index arrays are always checked).

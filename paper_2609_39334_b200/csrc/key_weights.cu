@@ -15,6 +15,9 @@ int32_t launch_tiles(const Params& P, cudaStream_t st, int blocks);
 
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32, kPlanBlocks = 8;
 constexpr int kPlainThreads = 256;
+// (Loops over keys look two tiles ahead, those over nodes and paths step by the planner's threads, in 32 bits.)
+constexpr int64_t kMostPages = (0x80000000LL - 2 * kTile) / kPage;
+constexpr int kMostListed = 1 << 30;
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
@@ -235,7 +238,8 @@ static int32_t check_desc(const ss_attn_desc_t* d, const ss_key_weights_t* kw) {
     return SS_ERR_UNSUPPORTED;
   if (!(d->sm_scale >= 0.f) || isinf(d->sm_scale)) return SS_ERR_INVALID_ARG;
   const int64_t most = 0x7fffffffLL / d->num_q_heads;
-  if (d->total_q > most || (d->q_src_offsets && d->q_src_rows > most) || d->total_node_pages > 0x7ffffff) return SS_ERR_UNSUPPORTED;
+  if (d->total_q > most || (d->q_src_offsets && d->q_src_rows > most) || d->total_node_pages > kMostPages) return SS_ERR_UNSUPPORTED;
+  if (d->num_nodes > kMostListed || d->num_paths > kMostListed) return SS_ERR_UNSUPPORTED;
   return SS_OK;
 }
 
