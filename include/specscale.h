@@ -436,6 +436,7 @@ int32_t ss_key_weights(const ss_attn_desc_t* desc /* host */, const ss_key_weigh
  *   kv_len_out    int32 [num_nodes] or NULL; may be the descriptor's node_kv_len; only the n_nodes entries are written
  *   sinks, recent >= 0
  *   max_keys      host bound of the nodes' lengths (0: 16 * total_node_pages); decides how many SMs work on a node.  Longer nodes are right, too
+ *                 (total_node_pages <= 2^27 - 1024, else SS_ERR_UNSUPPORTED)
  * Of the descriptor it reads the heads, the pool (and writes it), and the tree without node_parent.
  *   workspace     >= ss_kv_evict_workspace_bytes(desc, ev) bytes, 256-byte aligned (4 bytes a slot and kv head).  Calls that share one must not
  *                 overlap

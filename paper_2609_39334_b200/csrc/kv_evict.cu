@@ -27,6 +27,7 @@ constexpr int kMostCluster = 8;
 static_assert(kBins == 4 * kThreads && kBins % kMostCluster == 0, "bins of a thread, and of a block");
 constexpr int kStaged = 16384;                 // ranks of a block's slots that are kept in shared memory, at most; behind them they are made again
 constexpr int kAhead = 4;                      // quads of slots that a thread has on their way
+constexpr int64_t kMostPages = (0x80000000LL - 2 * 4 * kThreads * kAhead) / kPage;       // (slots and what is looked at behind them, in 32 bits)
 constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32, kBatch = 4;
 constexpr uint32_t kMust = 0xffffffffu;
 constexpr uint32_t kAllTies = 0xffffffffu;
@@ -517,7 +518,7 @@ static int32_t check(const ss_attn_desc_t* d, const ss_evict_t* e) {
   if (d->head_dim != kDim || d->page_size != kPage || d->kv_token_stride != kDim || d->kv_page_stride % 128 || d->kv_head_stride % 128 ||
       d->kv_page_stride <= 0 || d->kv_head_stride <= 0)
     return SS_ERR_UNSUPPORTED;
-  if (d->num_kv_heads > 65536 || d->total_node_pages > 0x7ffffff || d->num_pages > 0x7ffffff || static_cast<int64_t>(e->n_nodes) * d->num_kv_heads > 0x7fffffffLL / kMostCluster)
+  if (d->num_kv_heads > 65536 || d->total_node_pages > kMostPages || d->num_pages > 0x7ffffff || static_cast<int64_t>(e->n_nodes) * d->num_kv_heads > 0x7fffffffLL / kMostCluster)
     return SS_ERR_UNSUPPORTED;
   return SS_OK;
 }
