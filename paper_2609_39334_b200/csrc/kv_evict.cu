@@ -203,9 +203,10 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
   const int s0 = static_cast<int>(min(static_cast<int64_t>(stretch) * r, static_cast<int64_t>(n))), s1 = min(s0 + stretch, n);
   if (k <= 0 || k == n) {                      // (the whole cluster) nothing moves
     if (r == 0 && tid == 0) P.moves[pair] = 0;
-    for (int i = s0 + tid; k > 0 && i < s1; i += kThreads) {
+    for (int i = s0 + tid; i < s1; i += kThreads) {
       const int64_t pg = W.page(i);
-      if (pg < 0) { set_status(&P.hdr->status, SS_ERR_BAD_INPUT); continue; }
+      if (pg < 0) set_status(&P.hdr->status, SS_ERR_BAD_INPUT);
+      if (pg < 0 || k == 0) continue;
       const int64_t at = W.beside(pg, i);
       if (P.weights_out != P.weights) P.weights_out[at] = P.weights[at];
       if (P.order_out && P.order_out != P.order) P.order_out[at] = P.order ? P.order[at] : i;
