@@ -611,7 +611,8 @@ int32_t ss_filtered_sample(const ss_sample_desc_t* desc /* host */, void* worksp
  *   masks              uint32 [n_masks] rows of ceil(vocab / 32) words at mask_stride words: bit v % 32 of word v / 32 is set where token v is
  *                      allowed;  mask_of int32 [n_seq] or NULL: mask s
  *   An entry of prompt_of, bias_of or mask_of outside [0, n_*) means none.  Tokens outside [0, vocab) are ignored.  Offsets ascend and
- *   are trusted.  (prompts, history, bias_tokens and bias_values may be NULL where they hold nothing.)
+ *   are trusted; of a list the first 2^31 - 2049 entries count.  (prompts, history, bias_tokens and bias_values may be NULL where they
+ *   hold nothing.)
  *   repetition, frequency, presence   fp32 [n_seq] on the device, or NULL: the scalar of that name for every sequence
  * vocab <= 2097152 (else SS_ERR_UNSUPPORTED).  No workspace, at most two launches.  n_seq = 0 or vocab = 0: nothing is launched.
  * Errors: SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_CUDA.

@@ -20,6 +20,7 @@ constexpr int kThreads = 512;
 constexpr int kTable = 49152;                  // bytes of shared memory of the list kernel
 constexpr int kSlots = 4096;                   // of the hash table: a token, its word, its bias entry
 constexpr int kMostHashed = 2816;              // entries of a row's lists that it takes
+constexpr int64_t kMostEntries = 0x7fffffff - 4 * kThreads;    // of a list; a thread's next quad has to fit 32 bits
 constexpr int kPartTokens = kTable / 4;        // a row has a block of the list kernel for so many tokens of the vocabulary, or fewer blocks
 static_assert(kSlots * 12 <= kTable && kTable / 4 / kThreads <= 32, "tables");
 
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_co
 #pragma unroll 1
     for (int kind = 0; kind < 3; ++kind) {
       const int32_t* tokens = (kind == 0 ? A.history.tokens : kind == 1 ? A.prompts.tokens : A.bias.tokens) + range[kind].lo;
-      const int n = static_cast<int>(min(range[kind].hi - range[kind].lo, static_cast<int64_t>(0x7fffffff)));
+      const int n = static_cast<int>(min(range[kind].hi - range[kind].lo, kMostEntries));
       // quads on 16-byte boundaries; the first and the last may reach over the list's ends, and take the tokens that are there
       const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(tokens) & 15) / 4);
 #pragma unroll 1
