@@ -41,20 +41,5 @@ __device__ __forceinline__ void exp2_pair(float& a, float& b, float least) {
   b = __uint_as_float((__float_as_uint(t1) << 23) + __float_as_uint(p1));
 }
 
-// The same of one value, in scalar instructions, down to 2^-127 (2^-149, and so does what is smaller); for a result that is a float: what is
-// larger than 127 or a NaN comes out as anything.
-__device__ __forceinline__ float exp2_fma(float x) {
-  const float kRound = 12582912.0f;
-  x = fmaxf(x, -127.f);
-  const float t = x + kRound, f = x - (t - kRound);
-  float p = 0.0013276473619043827f;
-  p = fmaf(p, f, 0.009675541892647743f);
-  p = fmaf(p, f, 0.05550713092088699f);
-  p = fmaf(p, f, 0.24022120237350464f);
-  p = fmaf(p, f, 0.6931469440460205f);
-  p = fmaf(p, f, 1.0000001192092896f);
-  return __uint_as_float((__float_as_uint(t) << 23) + __float_as_uint(p));
-}
-
 }  // namespace umma
 }  // namespace ss
