@@ -205,7 +205,8 @@ __global__ void __launch_bounds__(kPlainThreads) key_plain_kernel(const __grid_c
       for (int i = tile * kTile + warp; i < min(R.len, (tile + 1) * kTile); i += kPlainThreads / 32) {
         const int64_t page = page_of(P, R, i);
         if (page < 0) continue;
-        float k[4], sum = 0.f;
+        float k[4];
+        double sum = 0.;                       // (of as many tokens as there are, one by one)
         load4(P.k_pool + page * P.page_stride + static_cast<int64_t>(g) * P.head_stride + (i % kPage) * kDim + 4 * lane, k);
         for (int t = max(0, i - R.len + R.hides); t < R.rows; ++t) {
           const int2 row = P.rows[R.row0 + t];
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(kPlainThreads) key_plain_kernel(const __grid_c
           }
           sum += part;
         }
-        if (lane == 0) store_key(P, R, page, g, i, sum, load_before(P, R, page, g, i));
+        if (lane == 0) store_key(P, R, page, g, i, static_cast<float>(sum), load_before(P, R, page, g, i));
       }
     }
   }

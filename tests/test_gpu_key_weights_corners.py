@@ -103,7 +103,7 @@ def test_a_row_that_is_not_finite(column, kind, flags):
 
 
 # ---- very many keys, very many rows ----------------------------------------------------------------------
-def alike(hq, lens, parent, leaf, pages, q, lse, T=None, lse_rows=None):
+def alike(hq, lens, parent, leaf, pages, q, lse):
     """A descriptor over a pool of one kv head and few pages, which nodes have many times over (a page's keys get the same weight wherever the
     page is, so it may be written any number of times)."""
     i32, i64 = dict(dtype=torch.int32, device=DEV), dict(dtype=torch.int64, device=DEV)
@@ -113,13 +113,13 @@ def alike(hq, lens, parent, leaf, pages, q, lse, T=None, lse_rows=None):
         off.append(off[-1] + -(-x // 16))
     pool = pages["pool"]
     keep = [torch.tensor(parent, **i32), torch.tensor(lens, **i32), torch.tensor(off, **i64), torch.as_tensor(leaf, **i32),
-            torch.ones(n, **i32), torch.arange(n + 1, **i64), torch.zeros(n, **i64)]
+            torch.ones(n, **i32), torch.arange(n + 1, **i64), torch.zeros(n, **i64), pool, pages["of"], q, lse]
     d = B.make_attn_desc(
         num_q_heads=hq, num_kv_heads=1, k_pool=pool[:, 0], v_pool=pool[:, 1], num_pages=pool.shape[0], kv_page_stride=pool.stride(0),
         kv_head_stride=2048, kv_token_stride=128, node_parent=keep[0], node_kv_len=keep[1], node_page_offsets=keep[2], node_pages=pages["of"],
         total_node_pages=off[-1], path_leaf_node=keep[3], path_q_len=keep[4], q_offsets=keep[5], total_q=n, q=q, out=torch.empty(n, 1, 1, device=DEV),
         lse=lse, q_src_offsets=keep[6], q_src_rows=1)
-    d._alike = keep
+    d._keep = keep                                                # (a descriptor holds addresses alone)
     return d
 
 
@@ -209,3 +209,22 @@ def test_a_bound_on_the_sms_is_kept_to(sms, flags):
     c.order.fill_(-7)
     assert c.run(flags) == B.SS_OK
     c.check()
+
+
+@pytest.mark.parametrize("flags", PATHS)
+def test_a_million_rows(flags):
+    """Queries of zero, so that every term is exp(-lse): off by 2^-21 at most, and by 2^-22 of |lse|.  The plain form adds them up in 64 bits, the
+    tensor-core form by 128 and then, in two groups of half of the steps each, step by step."""
+    n, lse = 1 << 20, 0.1
+    pool = torch.randn(4, 2, 1, 16, 128, device=DEV).bfloat16()
+    d = alike(1, [64], [-1], torch.zeros(n, dtype=torch.int32), dict(pool=pool, of=torch.arange(4, dtype=torch.int32, device=DEV)),
+              torch.zeros(1, 1, 128, dtype=torch.bfloat16, device=DEV), torch.full((n, 1), lse, device=DEV))
+    d.flags = flags
+    w = torch.full((4, 1, 16), 7.0, device=DEV)
+    kw = B.make_key_weights(weights_out=w)
+    ws = B.alloc_workspace(B.ss_key_weights_workspace_bytes(d, kw), DEV)
+    B.ss_key_weights(d, kw, ws)
+    assert B.ss_last_device_status(ws) == B.SS_OK
+    want = n * math.exp(-float(torch.tensor(lse)))
+    steps = 0 if flags else n // 128 // 2 + 48
+    assert ((w.double() - want).abs() <= want * (2.0 ** -21 + 0.1 * 2.0 ** -22 + 2.0 ** -23 + steps * 2.0 ** -24)).all()
