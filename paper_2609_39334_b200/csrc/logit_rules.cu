@@ -124,7 +124,7 @@ constexpr uint32_t kInPrompt = 0x80000000u;    // the top bit of a token's word;
 // (Its code runs once or twice a block, so it is short: nothing is unrolled but the four tokens of a load, one loop goes through all three lists and
 // serves both tables.  With a loop for each, four loads ahead, the call took 21 us for eight rows instead of 15.)
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) rules_list_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
   extern __shared__ uint4 smem[];
   __shared__ uint16_t list[kTable / 4];
