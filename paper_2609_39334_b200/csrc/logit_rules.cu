@@ -122,7 +122,8 @@ __device__ __forceinline__ float ruled(float x, const Row& R, uint32_t count, bo
 constexpr uint32_t kInPrompt = 0x80000000u;    // the top bit of a token's word; the rest: how often it is in the history
 
 // (Its code runs once or twice a block, so it is short: nothing is unrolled but the four tokens of a load, one loop goes through all three lists and
-// serves both tables.  With a loop for each, four loads ahead, the call took 21 us for eight rows instead of 15.)
+// serves both tables.  With a loop for each, four loads ahead, the call took 21 us for eight rows instead of 15.  Three blocks fit an SM beside their
+// tables; bounded to three, with 39 registers instead of 31, it takes as long.)
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
@@ -153,7 +154,6 @@ __global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_co
   int* key = reinterpret_cast<int*>(entry + places);
   for (int64_t first64 = static_cast<int64_t>(part) * window; first64 < A.vocab; first64 += static_cast<int64_t>(A.parts) * window) {
     const int first = static_cast<int>(first64);
-    const uint32_t count = static_cast<uint32_t>(min(window, A.vocab - first));
 #pragma unroll 1
     for (int i = tid; i < kTable / 16; i += kThreads) smem[i] = hashed && i >= 2 * kSlots / 4 ? make_uint4(~0u, ~0u, ~0u, ~0u) : make_uint4(0, 0, 0, 0);
     if (tid == 0) n_found = 0;
@@ -189,10 +189,11 @@ __global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_co
 #pragma unroll
           for (int y = 0; y < 4; ++y) q[y] = i0 + y >= 0 && i0 + y < n ? __ldg(tokens + i0 + y) : -1;
         }
-        // (a token in front of the window, or none, comes out as a large difference)
+        // (A token in front of the window, or none, comes out as a large difference.  Not by the window's number of tokens, the last one's a smaller
+        // number: in a build of 39 registers nvcc 12.9's code went on with the first window's, and wrote behind the row.)
         uint32_t hit = 0;
 #pragma unroll
-        for (int y = 0; y < 4; ++y) hit |= (static_cast<uint32_t>(q[y]) - static_cast<uint32_t>(first) < count ? 1u : 0u) << y;
+        for (int y = 0; y < 4; ++y) hit |= (static_cast<uint32_t>(q[y]) - static_cast<uint32_t>(first) < static_cast<uint32_t>(window) && q[y] < A.vocab ? 1u : 0u) << y;
         for (; hit; hit &= hit - 1) {
           const int y = __ffs(hit) - 1;
           note(kind, static_cast<uint32_t>((y & 2 ? (y & 1 ? q[3] : q[2]) : (y & 1 ? q[1] : q[0])) - first), i0 + y);

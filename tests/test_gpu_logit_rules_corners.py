@@ -25,6 +25,32 @@ def test_many_rows_with_long_lists(bias, half, in_place):
     c.check()
 
 
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("v", [100, 5000, 6144, 6145, 7000, 9924, 12288, 12289, 20000, 151936])
+@pytest.mark.parametrize("kind", ["history", "prompts", "bias", "all"])
+def test_tokens_behind_the_vocabulary_are_in_no_window(kind, v, half):
+    """Lists too long for the hash table, with tokens that a whole window at the vocabulary's end would reach, and further ones.  Behind every row
+    there is room for them, which is left alone."""
+    r = np.random.default_rng(v)
+    rows, room = 5, 20000
+    tokens = [int(t) for t in np.concatenate([r.integers(max(0, v - 3000), v + 100, 2000), r.integers(v - 5, v + 13000, 2500), [-1, -2, -(1 << 31), (1 << 31) - 1]])]
+    r.shuffle(tokens)
+    kw = dict(r=1.2, f=0.5)
+    if kind in ("history", "all"):
+        kw["history"] = [tokens] * rows
+    if kind in ("prompts", "all"):
+        kw.update(prompts=[tokens], prompt_of=[0] * rows)
+    if kind in ("bias", "all"):
+        kw.update(bias=[[(t, float(b)) for t, b in zip(tokens, r.normal(size=len(tokens)))]], bias_of=[0] * rows)
+    for in_place in (False, True):
+        c = rules.Case(v, rows, v, half, in_place=in_place, stride=v + room, **kw)
+        behind = c.out.as_strided((rows, room), (v + room, 1), v)
+        before = behind.clone()
+        B.ss_logit_rules(c.rules)
+        c.check()
+        assert torch.equal(behind, before)
+
+
 def test_the_longest_list():
     """More entries than 32 bits number: it ends, and the first 2^31 - 2049 count."""
     n = (1 << 31) + 100
