@@ -154,6 +154,9 @@ __global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_co
   int* key = reinterpret_cast<int*>(entry + places);
   for (int64_t first64 = static_cast<int64_t>(part) * window; first64 < A.vocab; first64 += static_cast<int64_t>(A.parts) * window) {
     const int first = static_cast<int>(first64);
+    // (In 64 bits: of min(window, A.vocab - first) in 32, signed or not, nvcc 12.9 made code in a build of 39 registers that went on with the first
+    // window's number in the last one, whose tokens behind the vocabulary were then written behind the row.)
+    const uint32_t count = static_cast<uint32_t>(min(static_cast<int64_t>(window), A.vocab - first64));
 #pragma unroll 1
     for (int i = tid; i < kTable / 16; i += kThreads) smem[i] = hashed && i >= 2 * kSlots / 4 ? make_uint4(~0u, ~0u, ~0u, ~0u) : make_uint4(0, 0, 0, 0);
     if (tid == 0) n_found = 0;
@@ -189,11 +192,10 @@ __global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_co
 #pragma unroll
           for (int y = 0; y < 4; ++y) q[y] = i0 + y >= 0 && i0 + y < n ? __ldg(tokens + i0 + y) : -1;
         }
-        // (A token in front of the window, or none, comes out as a large difference.  Not by the window's number of tokens, the last one's a smaller
-        // number: in a build of 39 registers nvcc 12.9's code went on with the first window's, and wrote behind the row.)
+        // (a token in front of the window, or none, comes out as a large difference)
         uint32_t hit = 0;
 #pragma unroll
-        for (int y = 0; y < 4; ++y) hit |= (static_cast<uint32_t>(q[y]) - static_cast<uint32_t>(first) < static_cast<uint32_t>(window) && q[y] < A.vocab ? 1u : 0u) << y;
+        for (int y = 0; y < 4; ++y) hit |= (static_cast<uint32_t>(q[y]) - static_cast<uint32_t>(first) < count ? 1u : 0u) << y;
         for (; hit; hit &= hit - 1) {
           const int y = __ffs(hit) - 1;
           note(kind, static_cast<uint32_t>((y & 2 ? (y & 1 ? q[3] : q[2]) : (y & 1 ? q[1] : q[0])) - first), i0 + y);
