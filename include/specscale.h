@@ -374,7 +374,8 @@ int32_t ss_draft_attention(const ss_attn_desc_t* desc /* host */, const int32_t*
  *                 exp(s - lse[t,h])
  * Token t of a step of T sees the keys up to its own, as in ss_tree_attention.  With last_tokens > 0 only the last last_tokens tokens
  * of each path's step add to the sums (an observation window behind a long prompt).  The step's own keys (the last T of the leaf) are
- * new: their weights_in is taken as 0, and `order` of theirs becomes path_order + t.  A row with lse = -inf adds nothing.
+ * new: their weights_in is taken as 0, and `order` of theirs becomes path_order + t.  A row with lse = -inf adds nothing, whatever its
+ * q holds; of other rows infinities and NaN go their way by the formula.
  * Keys that a token does not see, and what lies behind a node's end, may hold anything without an effect on the others.
  *
  *   weights_in, weights_out  fp32, weights_out may be weights_in; weights_in NULL: zeros.  Arrays beside the pool: element
@@ -387,15 +388,17 @@ int32_t ss_draft_attention(const ss_attn_desc_t* desc /* host */, const int32_t*
  * Nodes may have any length up to 2^31 - 256 (total_node_pages <= 2^27 - 16, num_nodes and num_paths <= 2^30, else
  * SS_ERR_UNSUPPORTED).  T <= node_kv_len of the leaf (T = 0: the path adds nothing, its chain's keys are still written).  A leaf with
  * other paths below it: T <= 1.  The paths below a node are contiguous.
- * SS_FLAG_FORCE_GENERIC or SS_FLAG_NO_TCGEN05 run one key per warp on the CUDA cores (a second opinion); max_sms is kept to; the other flags
- * make no difference (index arrays are always checked).
+ * SS_FLAG_FORCE_GENERIC or SS_FLAG_NO_TCGEN05 run one key per warp on the CUDA cores (a second opinion); max_sms is kept to in either form;
+ * the other flags make no difference (index arrays are always checked).
  *   workspace    >= ss_key_weights_workspace_bytes(desc, kw) bytes, 256-byte aligned; its size depends on the number of SMs of the current
  *                device, num_nodes, num_paths and total_q.  Calls that share one must not overlap
- * Accuracy (inputs ~N(0,1) in bf16): relative error of a sum below 1e-5.  Results do not depend on the run.
+ * Accuracy (inputs ~N(0,1) in bf16): relative error of a sum below 1e-5 (in the tensor-core form up to 2^-25 more for every 128 rows where
+ * they are all alike).  Results do not depend on the run.
  * Not written: weights and order of keys on no live path's chain, and behind a node's end.
  * Errors (host): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE_TOO_SMALL, SS_ERR_CUDA.  Errors (device, via
  * ss_last_device_status; weights of the nodes concerned are unspecified): SS_ERR_UNSUPPORTED (depth, a step longer than its leaf, a longer
- * step of a leaf with other paths below it), SS_ERR_BAD_INPUT (index arrays out of range, paths below a node not contiguous), SS_ERR_TIMEOUT.
+ * step of a leaf with other paths below it), SS_ERR_BAD_INPUT (index arrays out of range, a page of -1 among them, paths below a node not
+ * contiguous), SS_ERR_TIMEOUT.
  * ======================================================================================================= */
 typedef struct ss_key_weights {
   uint32_t struct_size;              /* = sizeof(ss_key_weights_t) */
@@ -442,7 +445,7 @@ int32_t ss_key_weights(const ss_attn_desc_t* desc /* host */, const ss_key_weigh
  *                 overlap
  * Errors (host): SS_ERR_INVALID_ARG, SS_ERR_UNSUPPORTED, SS_ERR_WORKSPACE_TOO_SMALL, SS_ERR_CUDA.  Errors (device, via
  * ss_last_device_status): SS_ERR_BAD_INPUT (a node out of range, or a length that its pages do not hold: the node is left as it is; a node that is listed again; a page outside the
- * pool: its keys rank last, and nothing moves from or to it).
+ * pool, in a node that keeps nothing, too: its keys rank last, and nothing moves from or to it).
  * ======================================================================================================= */
 typedef struct ss_evict {
   uint32_t struct_size;              /* = sizeof(ss_evict_t) */

@@ -762,7 +762,8 @@ def make_logit_rules(*, logits, out=None, history=None, history_offsets=None, pr
 
 
 def ss_logit_rules(rules: ss_logit_rules_t, stream=None, check=True) -> int:
-    """Penalties of repeated tokens, biases and grammar masks on logits, in one pass (see the header)."""
+    """Penalties of repeated tokens, biases and grammar masks on logits: a copy of the rows (none in place without masks), then the tokens of
+    their lists (see the header)."""
     rc = _call(rules._device, lib().ss_logit_rules, ctypes.byref(rules), stream=stream)
     if check:
         _check(rc, "ss_logit_rules")

@@ -2,7 +2,7 @@
 //
 //   plan (one cluster: which paths are below a node, the table of query rows, the nodes with something to do and their steps)
 //     -> tensor-core kernel (key_weights_umma.cu), or the plain kernel: a warp per key, in fp32
-// The planner is bound by latency, four barriers of its cluster and some ten trips to memory: 14 us alone for 8 paths, 19 for 1024.
+// The planner is bound by latency, five barriers of its cluster and some ten trips to memory: 14 us alone for 8 paths, 19 for 1024.
 #include <math.h>
 #include <string.h>
 

@@ -123,7 +123,7 @@ constexpr uint32_t kInPrompt = 0x80000000u;    // the top bit of a token's word;
 
 // (Its code runs once or twice a block, so it is short: nothing is unrolled but the four tokens of a load, one loop goes through all three lists and
 // serves both tables.  With a loop for each, four loads ahead, the call took 21 us for eight rows instead of 15.  Three blocks fit an SM beside their
-// tables; bounded to three, with 39 registers instead of 31, it takes as long.)
+// tables; bounded to three it has 40 registers instead of 23, and takes as long.)
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_constant__ Args A) {
   ss::grid_dependency_enter();
@@ -154,8 +154,8 @@ __global__ void __launch_bounds__(kThreads, 4) rules_list_kernel(const __grid_co
   int* key = reinterpret_cast<int*>(entry + places);
   for (int64_t first64 = static_cast<int64_t>(part) * window; first64 < A.vocab; first64 += static_cast<int64_t>(A.parts) * window) {
     const int first = static_cast<int>(first64);
-    // (In 64 bits: of min(window, A.vocab - first) in 32, signed or not, nvcc 12.9 made code in a build of 39 registers that went on with the first
-    // window's number in the last one, whose tokens behind the vocabulary were then written behind the row.)
+    // (In 64 bits: of min(window, A.vocab - first) in 32, signed or not, nvcc 12.9 made code for a bound of three blocks that went on with the first
+    // window's number in the last one, and so wrote tokens behind the vocabulary behind the row.  This is right with either bound.)
     const uint32_t count = static_cast<uint32_t>(min(static_cast<int64_t>(window), A.vocab - first64));
 #pragma unroll 1
     for (int i = tid; i < kTable / 16; i += kThreads) smem[i] = hashed && i >= 2 * kSlots / 4 ? make_uint4(~0u, ~0u, ~0u, ~0u) : make_uint4(0, 0, 0, 0);
